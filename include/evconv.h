@@ -390,7 +390,8 @@ evconv_status evconv_debug_chip_probes(void* scratch /* DEVICE */, size_t scratc
  * switches EVCONV_FLAG_* of the description turn these off for tests and comparisons. */
 const char* evconv_node_kernel(const evconv_net* net, int32_t node);
 
-/* Text of the last error on this net (or of the last failed create when net is NULL). */
+/* Text of the last error on this net (or, when net is NULL, of the last failed create or call of
+ * evconv_ops.h). */
 const char* evconv_last_error(const evconv_net* net);
 
 #ifdef __cplusplus

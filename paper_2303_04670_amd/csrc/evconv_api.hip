@@ -14,6 +14,7 @@
 
 #include "../../include/evconv.h"
 #include "evconv_kernels.h"
+#include "ops_kernels.h"
 
 using namespace evk;
 
@@ -818,6 +819,14 @@ hipError_t prepare_fold(evconv_net* net, NodePlan& n, const void* weights, const
 }
 
 }  // namespace
+
+// The sequence operators (ops_api.hip) report their errors in the same place as the create calls.
+void evk::set_call_error(const char* text) noexcept {
+  try {
+    g_create_error = text;
+  } catch (...) {  // (no memory for the text: the status stands)
+  }
+}
 
 extern "C" {
 

@@ -1,0 +1,53 @@
+// Internal interface between the host side of the sequence operators (ops_api.hip) and their gfx950
+// kernels.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/evconv_ops.h"
+
+namespace evk {
+
+// Text of evconv_last_error(NULL) (evconv_api.hip).
+void set_call_error(const char* text) noexcept;
+
+// ---- gated delta rule ---------------------------------------------------------------------------
+constexpr int kDeltaChunk = 64;  // tokens of a chunk
+
+struct DeltaParams {
+  evconv_delta_args a;
+  int share;        // value heads per key head
+  int len;          // tokens of every sequence, or -1: seq_offsets
+  int short_len;    // sequences of up to so many tokens go token by token
+  int slots_total;  // chunk slots: n_tokens / kDeltaChunk + n_seq
+  int dkp;          // d_k, rounded up to whole 32
+  int vec;          // q, k rows may be read in 16-byte loads
+  // workspace
+  char* frag_k;     // per chunk slot and key head: K, Q and K' as matrix-core operands
+  char* frag_t;     // per chunk slot and value head: T and P
+  float* scal;      // per chunk slot and value head: kDeltaScalars
+};
+// Sizes in the workspace, per chunk slot and head.
+size_t delta_frag_k_bytes(int dtype, int dkp);
+size_t delta_frag_t_bytes(int dtype);
+constexpr int kDeltaScalars = 4 * kDeltaChunk + 64;
+void launch_delta_steps(const DeltaParams& p, hipStream_t s);
+void launch_delta_chunks(const DeltaParams& p, hipStream_t s);
+
+// ---- norms around a block, rows of 8-bit integers ------------------------------------------------
+// vectors of eight that a row takes (the lanes of a group that it does not fill among them), at most
+constexpr int kNormVectors = 2048;
+int block_norm_vectors(const evconv_norm_args& a);
+void launch_block_norm(const evconv_norm_args& a, bool vec, hipStream_t s);
+
+// ---- product in 8-bit integers -------------------------------------------------------------------
+struct QuantPlan {
+  int kind;       // which kernel
+  int split;      // workgroups that share a tile's sums
+  size_t bytes;   // workspace
+};
+QuantPlan plan_quant_matmul(const evconv_quant_args& a);
+void launch_quant_matmul(const evconv_quant_args& a, const QuantPlan& plan, void* workspace, hipStream_t s);
+
+}  // namespace evk
