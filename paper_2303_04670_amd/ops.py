@@ -18,8 +18,7 @@ import torch
 from .evconv import (ERR_INVALID_ARG, ERR_SHAPE, OK, EvConvError, lib)
 
 ABI_VERSION = 1
-EXPORTS = ["evconv_delta_rule_workspace", "evconv_delta_rule", "evconv_block_norm", "evconv_quant_matmul_workspace",
-           "evconv_quant_matmul"]
+EXPORTS = ["evconv_delta_rule_workspace", "evconv_delta_rule", "evconv_block_norm", "evconv_quant_matmul"]
 DELTA_NORMALIZE, DELTA_RAW_GATES = 1, 2
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 _NORMS = {"rms": 0, "layer": 1}
@@ -77,12 +76,10 @@ def _calls():
     global _entry
     if _entry is None:
         L = lib()
-        size = ctypes.POINTER(ctypes.c_size_t)
-        L.evconv_delta_rule_workspace.argtypes = [ctypes.POINTER(DeltaArgs), size]
-        L.evconv_delta_rule.argtypes = [ctypes.POINTER(DeltaArgs), _vp, ctypes.c_size_t, _vp]
-        L.evconv_block_norm.argtypes = [ctypes.POINTER(NormArgs), _vp]
-        L.evconv_quant_matmul_workspace.argtypes = [ctypes.POINTER(QuantArgs), size]
-        L.evconv_quant_matmul.argtypes = [ctypes.POINTER(QuantArgs), _vp, ctypes.c_size_t, _vp]
+        L.evconv_delta_rule_workspace.argtypes = [_vp, _vp]  # (byref() of the structures above)
+        L.evconv_delta_rule.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
+        L.evconv_block_norm.argtypes = [_vp, _vp]
+        L.evconv_quant_matmul.argtypes = [_vp, _vp]
         _entry = L
     return _entry
 
@@ -96,52 +93,58 @@ def _refuse(status, text):
     raise EvConvError(status, text)
 
 
-def _tensor(t, name, device, dtype, shape):
-    """A tensor of this device, type and shape with contiguous rows; None passes."""
-    if t is None:
-        return
-    if t.device != device or device.type != "cuda":
-        _refuse(ERR_INVALID_ARG, f"{name} is on {t.device}, expected one GPU ({device})")
+# The checks run before every launch, and a launch of few tokens takes a few microseconds: one comparison of each
+# property, the reasons only once one has failed.
+
+def _explain(t, name, gpu, dtype, shape):
+    if gpu < 0 or t.get_device() != gpu:
+        _refuse(ERR_INVALID_ARG, f"{name} is on {t.device}, expected " + (f"cuda:{gpu}" if gpu >= 0 else "a GPU"))
     if t.dtype != dtype:
         _refuse(ERR_INVALID_ARG, f"{name} is {t.dtype}, expected {dtype}")
     if t.shape != shape:
         _refuse(ERR_SHAPE, f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-        _refuse(ERR_SHAPE, f"{name}: the last dimension must be contiguous")
+    _refuse(ERR_SHAPE, f"{name}: strides {t.stride()}: rows (parameters and states: the whole tensor) must be contiguous")
 
 
-def _packed(t, name, device, dtype, shape):
-    _tensor(t, name, device, dtype, shape)
-    if t is not None and not t.is_contiguous():
-        _refuse(ERR_SHAPE, f"{name} must be contiguous")
+def _rows(t, name, gpu, dtype, shape):
+    """(address, strides) of a tensor of this GPU, type and shape whose last dimension is contiguous."""
+    stride = t.stride()
+    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
+        _explain(t, name, gpu, dtype, shape)
+    return t.data_ptr(), stride
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _packed(t, name, gpu, dtype, shape):
+    """Address of a contiguous tensor; None of None."""
+    if t is None:
+        return None
+    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _explain(t, name, gpu, dtype, shape)
+    return t.data_ptr()
 
 
 def _dtype(t, name):
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         _refuse(ERR_INVALID_ARG, f"{name} is {t.dtype}, expected float32 or bfloat16")
-    return _DTYPES[t.dtype]
+    return code
 
 
-def _enqueue(call, args, device, workspace_of=None):
-    """The call on the device's current stream, with a workspace of its own from the caching allocator
-    (which keeps it for this stream until the call's kernels are done)."""
-    with torch.cuda.device(device):
-        stream = torch.cuda.current_stream().cuda_stream
-        if workspace_of is None:
-            _check(call(ctypes.byref(args), stream))
-            return
-        n = ctypes.c_size_t(0)
-        _check(workspace_of(ctypes.byref(args), ctypes.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
-        _check(call(ctypes.byref(args), _ptr(ws), n.value, stream))
-
-
-def _set_heads(to, t):
-    to.data, to.token_stride, to.head_stride = t.data_ptr(), t.stride(0), t.stride(1)
+def _enqueue(call, args, gpu, workspace_of=None):
+    """The call on the GPU's current stream, with a workspace of its own from the caching allocator (which
+    keeps it for this stream until the call's kernels are done)."""
+    if torch.cuda.current_device() != gpu:
+        with torch.cuda.device(gpu):
+            return _enqueue(call, args, gpu, workspace_of)
+    stream, args = torch._C._cuda_getCurrentRawStream(gpu), ctypes.byref(args)
+    if workspace_of is None:
+        return _check(call(args, stream))
+    n = ctypes.c_size_t(0)
+    _check(workspace_of(args, ctypes.byref(n)))
+    if n.value:
+        ws = torch.empty(n.value, dtype=torch.uint8, device=gpu)
+        return _check(call(args, ws.data_ptr(), n.value, stream))
+    _check(call(args, None, 0, stream))
 
 
 def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq_offsets=None, slots=None, n_seq=None,
@@ -157,49 +160,43 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
     by default d_k ** -0.5.  normalize: q and k are divided by their norms first."""
     if q.dim() != 3 or v.dim() != 3 or gate.dim() != 2:
         _refuse(ERR_SHAPE, f"q {tuple(q.shape)}, v {tuple(v.shape)}, gate {tuple(gate.shape)}: expected three, three and two dimensions")
-    device, (n, hk, dk), (hv, dv) = v.device, q.shape, v.shape[1:]
-    a = DeltaArgs(abi_version=ABI_VERSION, dtype=_dtype(v, "v"), gate_dtype=_dtype(gate, "gate"),
-                  flags=(DELTA_NORMALIZE if normalize else 0) | (DELTA_RAW_GATES if a_scale is not None or dt_bias is not None else 0),
-                  heads_k=hk, heads_v=hv, d_k=dk, d_v=dv, n_tokens=n, scale=dk ** -0.5 if scale is None else scale)
-    for t, name, dtype, shape in ((q, "q", v.dtype, q.shape), (k, "k", v.dtype, q.shape), (v, "v", v.dtype, (n, hv, dv)),
-                                  (gate, "gate", gate.dtype, (n, hv)), (beta, "beta", gate.dtype, (n, hv)), (out, "out", v.dtype, v.shape)):
-        if name in ("gate", "beta"):  # (single values: any strides)
-            if t.device != device or t.dtype != dtype or t.shape != shape:
-                _refuse(ERR_SHAPE, f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}, expected {shape} {dtype} on {device}")
-        else:
-            _tensor(t, name, device, dtype, shape)
-    _packed(a_scale, "a_scale", device, torch.float32, (hv,))
-    _packed(dt_bias, "dt_bias", device, torch.float32, (hv,))
+    gpu, dtype, gate_dtype, q_shape, v_shape = v.get_device(), v.dtype, gate.dtype, q.shape, v.shape
+    (n, hk, dk), (hv, dv) = q_shape, v_shape[1:]
+    if v_shape[0] != n:
+        _explain(v, "v", gpu, dtype, (n, hv, dv))
+    raw = a_scale is not None or dt_bias is not None
+    a = DeltaArgs()
+    a.abi_version, a.dtype, a.gate_dtype = ABI_VERSION, _dtype(v, "v"), _dtype(gate, "gate")
+    a.flags = (DELTA_NORMALIZE if normalize else 0) | (DELTA_RAW_GATES if raw else 0)
+    a.heads_k, a.heads_v, a.d_k, a.d_v, a.n_tokens, a.scale = hk, hv, dk, dv, n, dk ** -0.5 if scale is None else scale
+    for to, t, name, shape in ((a.q, q, "q", q_shape), (a.k, k, "k", q_shape), (a.v, v, "v", v_shape)):
+        to.data, (to.token_stride, to.head_stride, _) = _rows(t, name, gpu, dtype, shape)
+    for to, t, name in ((a.gate, gate, "gate"), (a.beta, beta, "beta")):  # (single values: any strides)
+        if t.get_device() != gpu or t.dtype is not gate_dtype or t.shape != (n, hv):
+            _explain(t, name, gpu, gate_dtype, (n, hv))
+        to.data, (to.token_stride, to.head_stride) = t.data_ptr(), t.stride()
+    if raw:
+        a.a_scale, a.dt_bias = _packed(a_scale, "a_scale", gpu, torch.float32, (hv,)), _packed(dt_bias, "dt_bias", gpu, torch.float32, (hv,))
     if seq_offsets is not None:
         n_seq = seq_offsets.numel() - 1
-        _packed(seq_offsets, "seq_offsets", device, torch.int32, (n_seq + 1,))
+        a.seq_offsets = _packed(seq_offsets, "seq_offsets", gpu, torch.int32, (n_seq + 1,))
     elif n_seq is None:
-        n_seq = slots.numel() if slots is not None else state.shape[0] if state is not None else 1
-    _packed(slots, "slots", device, torch.int32, (n_seq,))
+        n_seq = slots.numel() if slots is not None else state.shape[0] if state is not None and state.dim() else 1
+    a.slots = _packed(slots, "slots", gpu, torch.int32, (n_seq,))
     some = state if state is not None else state_out
     n_slots = some.shape[0] if some is not None and some.dim() else n_seq
-    for t, name in ((state, "state"), (state_out, "state_out")):
-        _packed(t, name, device, torch.float32, (n_slots, hv, dk, dv))
+    shape = (n_slots, hv, dk, dv)
+    a.state_in = _packed(state, "state", gpu, torch.float32, shape)
     if state_out is None:
-        state_out = state if state is not None and slots is not None else \
-            torch.empty(n_slots, hv, dk, dv, dtype=torch.float32, device=device)
+        state_out = state if state is not None and slots is not None else torch.empty(shape, dtype=torch.float32, device=gpu)
+    a.state_out = _packed(state_out, "state_out", gpu, torch.float32, shape)
     if out is None:
-        out = torch.empty(n, hv, dv, dtype=v.dtype, device=device)
+        out = torch.empty(v_shape, dtype=dtype, device=gpu)
+    a.o, (a.o_token_stride, a.o_head_stride, _) = _rows(out, "out", gpu, dtype, v_shape)
     a.n_seq, a.n_slots = n_seq, n_slots
-    for to, t in ((a.q, q), (a.k, k), (a.v, v), (a.gate, gate), (a.beta, beta)):
-        _set_heads(to, t)
-    a.o, a.o_token_stride, a.o_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
-    a.a_scale, a.dt_bias, a.seq_offsets, a.slots = _ptr(a_scale), _ptr(dt_bias), _ptr(seq_offsets), _ptr(slots)
-    a.state_in, a.state_out = _ptr(state), state_out.data_ptr()
     L = _calls()
-    _enqueue(L.evconv_delta_rule, a, device, L.evconv_delta_rule_workspace)
+    _enqueue(L.evconv_delta_rule, a, gpu, L.evconv_delta_rule_workspace)
     return out, state_out
-
-
-def _quant_rows(rows, dim, device):
-    stride = -(-dim // 128) * 128
-    return QuantRows(torch.empty(rows, stride, dtype=torch.int8, device=device),
-                     torch.empty(rows, dtype=torch.float32, device=device), dim)
 
 
 def block_norm(x=None, branch=None, gate=None, *, post_weight=None, post_bias=None, gate_act=None, group=None, res_scale=None,
@@ -211,43 +208,59 @@ def block_norm(x=None, branch=None, gate=None, *, post_weight=None, post_bias=No
     x, branch, gate: [rows, dim] with contiguous rows; gate_act: "none", "sigmoid" or "silu" (default: "silu" if there is a
     gate).  want: which outputs, letters of "xhq": x', h, and h as rows of 8-bit integers; by default "xh" (without
     pre_norm "x").  Returns NormResult(x, h, q), None for what is not wanted.  x_out may be x."""
-    rows_of = x if x is not None else branch
-    if rows_of is None or rows_of.dim() != 2:
+    first = x if x is not None else branch
+    if first is None or first.dim() != 2:
         _refuse(ERR_SHAPE, "block norm: x or branch as [rows, dim]")
-    device, dtype, (rows, dim) = rows_of.device, rows_of.dtype, rows_of.shape
-    group = dim if group is None else group
+    gpu, dtype, shape = first.get_device(), first.dtype, first.shape
+    rows, dim = shape
+    if group is None:
+        group = dim
     if pre_norm is None:
         pre_norm = pre_weight is not None or pre_bias is not None
-    gate_act = ("none" if gate is None else "silu") if gate_act is None else gate_act
+    if gate_act is None:
+        gate_act = "none" if gate is None else "silu"
     if want is None:
         want = "xh" if pre_norm else "x"
-    if kind not in _NORMS or gate_act not in _GATES or not want or set(want) - set("xhq"):
+    if kind not in _NORMS or gate_act not in _GATES or not want or want.strip("xhq"):
         _refuse(ERR_INVALID_ARG, f"block norm: kind {kind!r}, gate_act {gate_act!r}, want {want!r}")
-    for t, name in ((x, "x"), (branch, "branch"), (gate, "gate"), (x_out, "x_out"), (h_out, "h_out")):
-        _tensor(t, name, device, dtype, (rows, dim))
-    for t, name, size in ((post_weight, "post_weight", group), (post_bias, "post_bias", group), (res_scale, "res_scale", dim),
-                          (pre_weight, "pre_weight", dim), (pre_bias, "pre_bias", dim)):
-        _packed(t, name, device, torch.float32, (size,))
-    if "x" in want and x_out is None:
-        x_out = torch.empty(rows, dim, dtype=dtype, device=device)
-    if "h" in want and h_out is None:
-        h_out = torch.empty(rows, dim, dtype=dtype, device=device)
-    q = _quant_rows(rows, dim, device) if "q" in want else None
-    a = NormArgs(abi_version=ABI_VERSION, dtype=_dtype(rows_of, "x"), norm=_NORMS[kind], gate_act=_GATES[gate_act],
-                 pre_norm=1 if pre_norm else 0, dim=dim, group=group, eps=eps, rows=rows, x=_ptr(x), branch=_ptr(branch), gate=_ptr(gate),
-                 post_weight=_ptr(post_weight), post_bias=_ptr(post_bias), res_scale=_ptr(res_scale),
-                 pre_weight=_ptr(pre_weight), pre_bias=_ptr(pre_bias))
-    for name, t in (("x", x), ("branch", branch), ("gate", gate)):
-        if t is not None:
-            setattr(a, name + "_stride", t.stride(0))
-    if "x" in want:
-        a.x_out, a.x_out_stride = x_out.data_ptr(), x_out.stride(0)
-    if "h" in want:
-        a.h_out, a.h_out_stride = h_out.data_ptr(), h_out.stride(0)
-    if q is not None:
-        a.q, a.q_stride, a.q_scale = q.q.data_ptr(), q.q.stride(0), q.scale.data_ptr()
-    _enqueue(_calls().evconv_block_norm, a, device)
-    return NormResult(x_out if "x" in want else None, h_out if "h" in want else None, q)
+    a, f32 = NormArgs(), torch.float32
+    a.abi_version, a.dtype, a.norm, a.gate_act, a.pre_norm = ABI_VERSION, _dtype(first, "x"), _NORMS[kind], _GATES[gate_act], bool(pre_norm)
+    a.dim, a.group, a.eps, a.rows = dim, group, eps, rows
+    if x is not None:
+        a.x, (a.x_stride, _) = _rows(x, "x", gpu, dtype, shape)
+    if branch is not None:
+        a.branch, (a.branch_stride, _) = _rows(branch, "branch", gpu, dtype, shape)
+    if gate is not None:
+        a.gate, (a.gate_stride, _) = _rows(gate, "gate", gpu, dtype, shape)
+    if post_weight is not None:
+        a.post_weight = _packed(post_weight, "post_weight", gpu, f32, (group,))
+    if post_bias is not None:
+        a.post_bias = _packed(post_bias, "post_bias", gpu, f32, (group,))
+    if res_scale is not None:
+        a.res_scale = _packed(res_scale, "res_scale", gpu, f32, (dim,))
+    if pre_weight is not None:
+        a.pre_weight = _packed(pre_weight, "pre_weight", gpu, f32, (dim,))
+    if pre_bias is not None:
+        a.pre_bias = _packed(pre_bias, "pre_bias", gpu, f32, (dim,))
+    if "x" not in want:
+        x_out = None
+    else:
+        if x_out is None:
+            x_out = torch.empty(shape, dtype=dtype, device=gpu)
+        a.x_out, (a.x_out_stride, _) = _rows(x_out, "x_out", gpu, dtype, shape)
+    if "h" not in want:
+        h_out = None
+    else:
+        if h_out is None:
+            h_out = torch.empty(shape, dtype=dtype, device=gpu)
+        a.h_out, (a.h_out_stride, _) = _rows(h_out, "h_out", gpu, dtype, shape)
+    q = None
+    if "q" in want:
+        a.q_stride = -(-dim // 128) * 128
+        q = QuantRows(torch.empty((rows, a.q_stride), dtype=torch.int8, device=gpu), torch.empty(rows, dtype=f32, device=gpu), dim)
+        a.q, a.q_scale = q.q.data_ptr(), q.scale.data_ptr()
+    _enqueue(_calls().evconv_block_norm, a, gpu)
+    return NormResult(x_out, h_out, q)
 
 
 def quantize_rows(x) -> QuantRows:
@@ -258,21 +271,25 @@ def quantize_rows(x) -> QuantRows:
 def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype=torch.float32, out=None):
     """act(a b' + bias) of rows of 8-bit integers (evconv_quant_matmul): [rows of a, rows of b].  act: "none",
     "relu", "sigmoid" or "tanh"."""
-    (m, sa), (n, sb), device = a.q.shape, b.q.shape, a.q.device
-    if a.k != b.k:
-        _refuse(ERR_SHAPE, f"quantised product: rows of {a.k} and {b.k} values")
+    aq, a_scale, k = a
+    bq, b_scale, bk = b
+    if aq.dim() != 2 or bq.dim() != 2 or k != bk:
+        _refuse(ERR_SHAPE, f"quantised product: rows {tuple(aq.shape)} of {k} and {tuple(bq.shape)} of {bk} values")
     if act not in _ACTS:
         _refuse(ERR_INVALID_ARG, f"quantised product: act {act!r}")
-    for r, name, rows in ((a, "a", m), (b, "b", n)):
-        _tensor(r.q, name + ".q", device, torch.int8, r.q.shape)
-        _packed(r.scale, name + ".scale", device, torch.float32, (rows,))
-    _packed(bias, "bias", device, torch.float32, (n,))
+    gpu, m, n, f32 = aq.get_device(), aq.shape[0], bq.shape[0], torch.float32
+    args = QuantArgs()
+    args.abi_version, args.act, args.n, args.k, args.m = ABI_VERSION, _ACTS[act], n, k, m
+    args.a, (args.a_stride, _) = _rows(aq, "a.q", gpu, torch.int8, aq.shape)
+    args.b, (args.b_stride, _) = _rows(bq, "b.q", gpu, torch.int8, bq.shape)
+    if aq.shape[1] < -(-k // 128) * 128 or bq.shape[1] < -(-k // 128) * 128:
+        _refuse(ERR_SHAPE, f"quantised product: rows of {aq.shape[1]} and {bq.shape[1]} bytes for {k} values")
+    args.a_scale, args.b_scale = _packed(a_scale, "a.scale", gpu, f32, (m,)), _packed(b_scale, "b.scale", gpu, f32, (n,))
+    if bias is not None:
+        args.bias = _packed(bias, "bias", gpu, f32, (n,))
     if out is None:
-        out = torch.empty(m, n, dtype=out_dtype, device=device)
-    _tensor(out, "out", device, out.dtype, (m, n))
-    args = QuantArgs(abi_version=ABI_VERSION, dtype=_dtype(out, "out"), act=_ACTS[act], n=n, k=a.k, m=m, a=a.q.data_ptr(), b=b.q.data_ptr(),
-                     a_stride=a.q.stride(0), b_stride=b.q.stride(0), a_scale=a.scale.data_ptr(), b_scale=b.scale.data_ptr(),
-                     bias=_ptr(bias), y=out.data_ptr(), y_stride=out.stride(0))
-    L = _calls()
-    _enqueue(L.evconv_quant_matmul, args, device, L.evconv_quant_matmul_workspace)
+        out = torch.empty((m, n), dtype=out_dtype, device=gpu)
+    args.dtype = _dtype(out, "out")
+    args.y, (args.y_stride, _) = _rows(out, "out", gpu, out.dtype, (m, n))
+    _enqueue(_calls().evconv_quant_matmul, args, gpu)
     return out
