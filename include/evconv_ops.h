@@ -148,10 +148,7 @@ typedef struct {
   int64_t y_stride;     /* elements, at least n */
 } evconv_quant_args;
 
-/* Bytes of device workspace the call needs: room for the partial sums where few tokens meet a long k. */
-evconv_status evconv_quant_matmul_workspace(const evconv_quant_args* args, size_t* bytes);
-evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* workspace, size_t workspace_bytes,
-                                  void* hip_stream);
+evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -109,7 +109,7 @@ evconv_status check_quant(const evconv_quant_args* a) {
   if (!float_type(a->dtype)) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: dtype %d", a->dtype);
   if (a->act < EVCONV_ACT_NONE || a->act > EVCONV_ACT_TANH) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: act %d", a->act);
   if (a->m < 0 || a->n < 1 || a->k < 1) return refuse(EVCONV_ERR_SHAPE, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
-  if (a->m >= 1ll << 31 || a->k > 131072 || a->n > 1 << 24) return refuse(EVCONV_ERR_UNSUPPORTED, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
+  if (a->m >= 1ll << 31 || a->k > 131072 || a->n > 1 << 24 || ((a->m + 255) / 256) * ((a->n + 255) / 256) >= 1ll << 31) return refuse(EVCONV_ERR_UNSUPPORTED, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
   if (!a->m) return EVCONV_OK;
   if (!a->a || !a->b || !a->a_scale || !a->b_scale || !a->y) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: null tensor");
   const int64_t row = (a->k + 127) / 128 * 128;
@@ -159,20 +159,10 @@ evconv_status evconv_block_norm(const evconv_norm_args* args, void* hip_stream) 
   return launched("block norm");
 }
 
-evconv_status evconv_quant_matmul_workspace(const evconv_quant_args* args, size_t* bytes) {
-  if (!bytes) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: null bytes");
-  const evconv_status st = check_quant(args);
-  if (st == EVCONV_OK) *bytes = args->m ? plan_quant_matmul(*args).bytes : 0;
-  return st;
-}
-
-evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* workspace, size_t workspace_bytes, void* hip_stream) {
+evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* hip_stream) {
   const evconv_status st = check_quant(args);
   if (st != EVCONV_OK || !args->m) return st;
-  const QuantPlan plan = plan_quant_matmul(*args);
-  if (plan.bytes && (!workspace || workspace_bytes < plan.bytes || !aligned(workspace, 256)))
-    return refuse(EVCONV_ERR_WORKSPACE, "quantised product: needs %zu bytes of workspace at a multiple of 256, got %zu", plan.bytes, workspace ? workspace_bytes : 0);
-  launch_quant_matmul(*args, plan, workspace, (hipStream_t)hip_stream);
+  launch_quant_matmul(*args, (hipStream_t)hip_stream);
   return launched("quantised product");
 }
 

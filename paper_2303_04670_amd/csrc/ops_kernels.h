@@ -42,12 +42,6 @@ int block_norm_vectors(const evconv_norm_args& a);
 void launch_block_norm(const evconv_norm_args& a, bool vec, hipStream_t s);
 
 // ---- product in 8-bit integers -------------------------------------------------------------------
-struct QuantPlan {
-  int kind;       // which kernel
-  int split;      // workgroups that share a tile's sums
-  size_t bytes;   // workspace
-};
-QuantPlan plan_quant_matmul(const evconv_quant_args& a);
-void launch_quant_matmul(const evconv_quant_args& a, const QuantPlan& plan, void* workspace, hipStream_t s);
+void launch_quant_matmul(const evconv_quant_args& a, hipStream_t s);
 
 }  // namespace evk

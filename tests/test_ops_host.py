@@ -109,16 +109,13 @@ def quant_args(**kw):
     (dict(a=None), ev.ERR_INVALID_ARG), (dict(b_scale=None), ev.ERR_INVALID_ARG), (dict(a_stride=100), ev.ERR_SHAPE),
     (dict(k=129), ev.ERR_SHAPE), (dict(b=FAKE + 8), ev.ERR_SHAPE), (dict(y_stride=7), ev.ERR_SHAPE)])
 def test_quant_matmul_refusals(change, status):
-    n = ctypes.c_size_t(0)
-    a = quant_args(**change)
-    assert ops._calls().evconv_quant_matmul_workspace(ctypes.byref(a), ctypes.byref(n)) == status
-    assert ops._calls().evconv_quant_matmul(ctypes.byref(a), FAKE, 1 << 40, None) == status
+    assert ops._calls().evconv_quant_matmul(ctypes.byref(quant_args(**change)), None) == status
     assert ev.lib().evconv_last_error(None).decode().startswith("quantised product")
 
 
 def test_nothing_to_do_is_ok():
     assert ops._calls().evconv_block_norm(ctypes.byref(norm_args(rows=0, x=None, branch=None)), None) == ev.OK
-    assert ops._calls().evconv_quant_matmul(ctypes.byref(quant_args(m=0, a=None, y=None)), None, 0, None) == ev.OK
+    assert ops._calls().evconv_quant_matmul(ctypes.byref(quant_args(m=0, a=None, y=None)), None) == ev.OK
 
 
 def test_binding_refuses_tensors_on_the_host():
