@@ -19,52 +19,10 @@
 // rows, applied to the sums), everything else that reaches the state as three bf16 parts, which hold
 // 24 bits; outputs of bf16 calls are summed from two parts.  G is summed in 64 bits: the difference of two
 // sums over a chunk would lose the bits that its exponential needs.
-#include "ops_device.h"
-#include "ops_kernels.h"
+#include "delta_device.h"
 
 namespace evk {
 namespace {
-
-constexpr int C = kDeltaChunk;
-constexpr int kFrag = 1024;            // bytes of one matrix-core operand: 64 lanes x 8 bf16
-constexpr int kTri = 6;                // 16 x 32 blocks of a 64 x 64 matrix that a lower triangle reaches
-constexpr float kLeastLog = -1e5f;     // log decays are not below: e^x is 0, and differences of sums stay finite
-constexpr float kBf16Overflow = 3.3961775e38f;  // the smallest value that rounds to an infinite bf16
-
-__host__ __device__ constexpr int parts_in(bool f32) { return f32 ? 3 : 1; }    // of keys and queries
-__host__ __device__ constexpr int parts_out(bool f32) { return f32 ? 3 : 2; }   // of what reaches o only
-
-struct Span { int first, len; };
-__device__ __forceinline__ Span span_of(const DeltaParams& p, int seq) {
-  if (p.len >= 0) return {seq * p.len, p.len};
-  const int n = (int)p.a.n_tokens;
-  const int a = min(max(p.a.seq_offsets[seq], 0), n), b = min(max(p.a.seq_offsets[seq + 1], 0), n);
-  return {a, max(b - a, 0)};
-}
-// First chunk slot of a sequence: no two sequences' slots meet, and none is behind n_tokens / C + n_seq - 1.
-__device__ __forceinline__ int first_slot(const Span& s, int seq) { return s.first / C + seq; }
-
-// Offset of a sequence's state, or -1: it has none.
-__device__ __forceinline__ int64_t state_at(const DeltaParams& p, int seq, int head) {
-  const int slot = p.a.slots ? p.a.slots[seq] : seq;
-  if (slot < 0 || slot >= p.a.n_slots) return -1;
-  return ((int64_t)slot * p.a.heads_v + head) * p.a.d_k * p.a.d_v;
-}
-
-struct Gates { float g, beta; };
-__device__ __forceinline__ Gates gates_of(const DeltaParams& p, int64_t token, int head) {
-  const bool bf16 = p.a.gate_dtype == EVCONV_BF16;
-  Gates r;
-  r.g = load_any(p.a.gate.data, token * p.a.gate.token_stride + head * p.a.gate.head_stride, bf16);
-  r.beta = load_any(p.a.beta.data, token * p.a.beta.token_stride + head * p.a.beta.head_stride, bf16);
-  if (p.a.flags & EVCONV_DELTA_RAW_GATES) {
-    const float x = r.g + p.a.dt_bias[head];
-    r.g = -p.a.a_scale[head] * (x > 20.0f ? x : log1pf(expf(x)));
-    r.beta = 1.0f / (1.0f + expf(-r.beta));
-  }
-  if (r.g < kLeastLog) r.g = kLeastLog;
-  return r;
-}
 
 // ---- token by token -------------------------------------------------------------------------------
 // A wave: one sequence, one head, 32 columns; 8 lanes x 4 columns across, 8 groups of ROWS rows down.
@@ -165,17 +123,6 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
 }
 
 // ---- chunks: what does not depend on the state ------------------------------------------------------
-// Operands of the 16 x 16 x 32 matrix instruction: a lane (m = lane % 16, g = lane / 16) holds row m of the left
-// operand (column m of the right one) at the contraction's places 8 g .. 8 g + 7, and column m, rows
-// 4 g .. 4 g + 3 of the result.  Let block b of a result's rows hold, at its row 4 g + i, the row
-//   place(b, 4 g + i) = 32 (b / 2) + 8 g + 4 (b % 2) + i.
-// Then the eight values that a lane has of blocks 2 s and 2 s + 1 are the ones that it needs as right operand
-// at step s of a contraction over those rows: S, R and D go from result to operand without leaving
-// their lane.  K, Q, K', T and P are laid out for that by delta_prepare.
-__host__ __device__ __forceinline__ int place(int block, int m) { return 32 * (block >> 1) + 8 * (m >> 2) + 4 * (block & 1) + (m & 3); }
-// Index of T's (P's) 16 x 32 block of result block b and contraction step s.
-__device__ __forceinline__ constexpr int tri(int b, int s) { return b < 2 ? b : 2 + (b - 2) * 2 + s; }
-
 // Eight values of a token's row from column c on, as bf16 parts
 template <bool F32, bool VEC>
 __device__ __forceinline__ void load_parts(const evconv_heads& h, int head, int d, int64_t token, bool live, int c, b16x8 (&out)[parts_in(F32)]) {
@@ -478,26 +425,8 @@ __global__ __launch_bounds__(64) void delta_chain(DeltaParams p) {
         if (!(fabsf(R[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
       }
     }
-    // A value that is not finite would reach earlier tokens through the zeros of T and P: what follows
-    // a column's first such token is left out of the products and made NaN behind them.
     int first_bad = C;
-    auto cut = [&](f32x4 (&x)[4], unsigned which) __attribute__((always_inline)) {
-      int first = first_bad;
-#pragma unroll
-      for (int b = 3; b >= 0; --b)
-#pragma unroll
-        for (int i = 3; i >= 0; --i)
-          if (which >> (b * 4 + i) & 1) first = min(first, place(b, 4 * g) + i);
-      first = min(first, __shfl_xor(first, 16));
-      first = min(first, __shfl_xor(first, 32));
-      first_bad = first;
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (place(b, 4 * g) + i >= first) x[b][i] = 0.0f;
-    };
-    if (__ballot(bad != 0)) cut(R, bad);
+    if (__ballot(bad != 0)) cut_columns(R, bad, first_bad, g);
     // D = T R
     b16x8 Rp[2][3];
     f32x4 D[4];
@@ -526,7 +455,7 @@ __global__ __launch_bounds__(64) void delta_chain(DeltaParams p) {
       for (int i = 0; i < 4; ++i)
         if (!(fabsf(D[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
     }
-    if (__ballot(bad != 0 || first_bad < C)) cut(D, bad);
+    if (__ballot(bad != 0 || first_bad < C)) cut_columns(D, bad, first_bad, g);
     // O += P D;  S = e^G S + K' (w D)
     const float decay = scal[4 * C];
 #pragma unroll

@@ -1,0 +1,748 @@
+// The gated delta rule in chunks, one launch (bf16 keys of up to 128 channels; formulas and precision: kernels_delta.hip).
+//
+// A workgroup owns a sequence's value head and NC strips of 16 state columns, a wave each (a consumer), and goes
+// through the chunks; two further waves (producers) take turns at preparing the chunks ahead: T and P, which do
+// not depend on the state.  Nothing that is computed once leaves the compute unit: keys and queries are read once into LDS
+// (the transposed operand K' comes from the same rows by transposing LDS reads), T and P go from producer to
+// consumer through a ring of three slots, S, R and D stay in their lanes (kernels_delta.hip: place).
+//
+// In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a producer
+// computes K K', Q K' and A of chunk c + 2, the other one T of chunk c + 1.
+#include "delta_device.h"
+
+namespace evk {
+namespace {
+
+constexpr int kStrideA = 68;  // floats between the rows of A and T: rows of a load instruction in different banks
+
+// Orders what lanes of one wave hand to each other through LDS (which serves a wave's requests in order).
+__device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
+
+template <int DKP, int NC>
+struct FusedShape {
+  static constexpr int kSteps = DKP / 32;
+  static constexpr int kOffP = kTri * 3 * kFrag, kOffScal = kOffP + kTri * 2 * kFrag, kSlot = kOffScal + 5 * C * 4;
+  static constexpr int kRows = C * DKP * 2;  // bytes of a chunk's K (or Q)
+  static constexpr int kOffK = 3 * kSlot, kBytes = kOffK + 4 * kRows;
+  static constexpr int kThreads = (NC + 2) * 64;
+  static_assert(C * kStrideA * 4 <= kOffP && kBytes <= 160 * 1024, "LDS");
+};
+// Place of the 16-byte piece c of row `row` of K (Q) in LDS: the 16 rows of an operand load, and the four rows of a
+// transposing one, in different banks.
+template <int DKP>
+__device__ __forceinline__ int at_rows(int row, int c) {
+  const int f = DKP == 128 ? (row & 3) << 2 | (row >> 3 & 3) : (row >> 1 & 1) << 2 | (row >> 3 & 3);
+  return row * DKP * 2 + ((c ^ f) << 4);
+}
+
+// Addresses: a part that is the same for a whole wave (64 bits, scalar registers) and a lane's bytes (32 bits).
+// A value that is the same for a whole wave, kept out of the compiler's sight: it would otherwise add a lane's part once
+// before the loop and hold dozens of 64-bit addresses in vector registers through it.
+// (Global by type: the compiler could not tell any more, and loads that may be LDS wait for LDS, too.)
+#define EVK_GLOBAL __attribute__((address_space(1)))
+__device__ __forceinline__ EVK_GLOBAL char* uniform(const void* q) {
+  EVK_GLOBAL char* r = (EVK_GLOBAL char*)q;
+  asm volatile("" : "+s"(r));
+  return r;
+}
+// base + a lane's bytes, by an instruction that adds the two itself (the extension to 64 bits has to be in sight of it)
+template <class T>
+__device__ __forceinline__ EVK_GLOBAL T* lane_at(const void* base, unsigned lane_bytes) {
+  asm volatile("" : "+v"(lane_bytes));
+  return (EVK_GLOBAL T*)(uniform(base) + lane_bytes);
+}
+// This wave's lane, likewise out of sight: what is derived from it is computed where it is used, not kept for all of a loop.
+__device__ __forceinline__ int own_lane() {
+  int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));  // (not of the thread's index, which would be)
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+// Eight bf16 of a row as they are, the first of `left` that the row has from there on
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+template <bool VEC>
+__device__ __forceinline__ u32x4 load_raw(const char* base, unsigned lane_bytes, int left) {
+  u32x4 u = {0, 0, 0, 0};
+  if (left <= 0) return u;
+  if (VEC) {
+    u = *lane_at<const u32x4>(base, lane_bytes);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) u[j / 2] |= (unsigned)*lane_at<const uint16_t>(base + j * 2, lane_bytes) << (j % 2 * 16);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return u;
+}
+// Whether one of eight bf16 is not finite, as bits 15 and 31 of the result
+__device__ __forceinline__ unsigned not_finite(const u32x4& u) {
+  unsigned r = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r |= (u[i] & 0x7f807f80u) + 0x00800080u;
+  return r & 0x80008000u;
+}
+// Rows of a head: of a chunk's first token, and the bytes from token to token
+struct Rows {
+  const char* at;
+  int step;
+  __device__ __forceinline__ void next(int chunks) { at += (int64_t)chunks * C * step; }
+};
+__device__ __forceinline__ Rows rows_of(const evconv_heads& h, int size, int head, int64_t token) {
+  return {(const char*)h.data + (token * h.token_stride + head * h.head_stride) * size, (int)h.token_stride * size};
+}
+
+// What a producer reads.
+template <bool VEC>
+struct Source {
+  Rows k, q, gate, beta;
+  int d_k, left;          // tokens from the first of k on
+  float a_scale, dt_bias;
+  bool gate_bf16;
+};
+// What it holds of a chunk ahead of its turn: block b of an operand is the tokens place(b, .), so that a pair of blocks spans
+// 32 tokens.
+template <int DKP>
+struct Ahead {
+  b16x8 k[4][DKP / 32], q[2][DKP / 32];
+  float gate, beta;  // as they are in memory
+};
+template <int DKP, bool VEC>
+__device__ __forceinline__ void request_blocks(const Rows& r, int d_k, int left, int block0, b16x8 (*to)[DKP / 32], int blocks) {
+  const int lane = own_lane(), m = lane & 15, g = lane >> 4;
+  if (VEC && d_k == DKP) {
+    // (loads under conditions of their own would be waited for one by one: tokens behind the end are the last one again, whose
+    // rows of A and P count for nothing)
+#pragma unroll
+    for (int b = 0; b < blocks; ++b) {
+      const unsigned at = (unsigned)(min(place(block0 + b, m), left - 1) * r.step + 16 * g);
+#pragma unroll
+      for (int s = 0; s < DKP / 32; ++s) to[b][s] = *lane_at<const b16x8>(r.at + 64 * s, at);
+    }
+    return;
+  }
+#pragma unroll
+  for (int b = 0; b < blocks; ++b)
+#pragma unroll
+    for (int s = 0; s < DKP / 32; ++s)
+      to[b][s] = __builtin_bit_cast(b16x8, load_raw<VEC>(r.at + 64 * s, (unsigned)(place(block0 + b, m) * r.step + 16 * g), place(block0 + b, m) < left ? d_k - 32 * s - 8 * g : 0));
+}
+template <int DKP, bool VEC>
+__device__ __forceinline__ void request_ahead(const Source<VEC>& f, Ahead<DKP>& to) {
+  request_blocks<DKP, VEC>(f.k, f.d_k, f.left, 0, to.k, 4);
+  request_blocks<DKP, VEC>(f.q, f.d_k, f.left, 0, to.q, 1);
+  const int t = own_lane();
+  const EVK_GLOBAL char *const gates = uniform(f.gate.at), *const betas = uniform(f.beta.at);
+  unsigned at_g = (unsigned)(t * f.gate.step), at_b = (unsigned)(t * f.beta.step);
+  asm volatile("" : "+v"(at_g), "+v"(at_b));
+  to.gate = to.beta = 0.0f;
+  if (t < f.left) {
+    if (f.gate_bf16) {
+      to.gate = bf16_low(*(const EVK_GLOBAL uint16_t*)(gates + at_g));
+      to.beta = bf16_low(*(const EVK_GLOBAL uint16_t*)(betas + at_b));
+    } else {
+      to.gate = *(const EVK_GLOBAL float*)(gates + at_g);
+      to.beta = *(const EVK_GLOBAL float*)(betas + at_b);
+    }
+  }
+}
+
+// First half of a chunk's preparation: A (fp32, in the place of T), P, the factors of the rows.
+template <int DKP, bool VEC>
+__device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slot, const Source<VEC>& f, int left, Ahead<DKP>& x) {
+  typedef FusedShape<DKP, 8> F;
+  constexpr int STEPS = F::kSteps;
+  const evconv_delta_args& a = p.a;
+  const int lane = own_lane(), m = lane & 15, g = lane >> 4;
+  float* const s_a = (float*)slot;
+  float* const scal = (float*)(slot + F::kOffScal);
+  float *const s_hi = scal, *const s_lo = scal + C, *const s_rk = scal + 2 * C, *const s_rq = scal + 3 * C, *const s_beta = scal + 4 * C;
+  request_blocks<DKP, VEC>(f.q, f.d_k, left, 1, &x.q[1], 1);
+  // ---- a token to a lane: sums of log2 decays, as two floats each, so that differences keep their bits
+  Gates gate = {0.0f, 0.0f};
+  if (lane < left) gate = gates_from(a.flags & EVCONV_DELTA_RAW_GATES, x.gate, x.beta, f.a_scale, f.dt_bias);
+  double sum = (double)gate.g * 1.44269504088896340736;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const double other = __shfl_up(sum, d);
+    if (lane >= d) sum += other;
+  }
+  const float hi = (float)sum, lo = isfinite(hi) ? (float)(sum - (double)hi) : 0.0f;
+  s_hi[lane] = hi;
+  s_lo[lane] = lo;
+  s_beta[lane] = gate.beta;
+  // ---- norms: diagonals of K K' and Q Q', which lanes with m / 4 == g hold
+  const bool normalize = a.flags & EVCONV_DELTA_NORMALIZE;
+  auto diagonal = [&](const b16x8 (&v)[STEPS]) __attribute__((always_inline)) {
+    f32x4 u = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) u = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[s], v[s], u, 0, 0, 0);
+    return m & 2 ? (m & 1 ? u[3] : u[2]) : (m & 1 ? u[1] : u[0]);
+  };
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const float u = diagonal(x.k[b]);
+    if (m >> 2 == g) s_rk[place(b, m)] = u;
+  }
+  wave_order();
+  // A token whose row of A cannot be finite: from the first one on the rows are NaN, by their beta, and zero in A, whose
+  // zeros would otherwise carry them to rows above them.  (A sum of squares bounds the products of its key.)
+  const float square = s_rk[lane];
+  const uint64_t wrong = __ballot(!(fabsf(square) < INFINITY) || !(fabsf(gate.beta) < INFINITY) || !(fabsf(hi) < INFINITY));
+  const int bad = wrong ? (int)__builtin_ctzll(wrong) : C;
+  const float rk = normalize ? 1.0f / sqrtf(square + 1e-6f) : 1.0f;
+  s_rk[lane] = rk;
+  if (lane >= bad) s_beta[lane] = 0.0f;
+  __builtin_amdgcn_sched_barrier(0);
+  // ---- rows 16 at a time
+#pragma unroll
+  for (int bi = 0; bi < 4; ++bi) {
+    const b16x8 (&q)[STEPS] = x.q[bi & 1];
+    if (normalize) {
+      const float u = diagonal(q);
+      if (m >> 2 == g) s_rq[place(bi, m)] = a.scale / sqrtf(u + 1e-6f);
+    } else if (g == 0) {
+      s_rq[place(bi, m)] = a.scale;
+    }
+    wave_order();
+    // a lane holds of block j the row i = place(bi, m) of A and P, columns j0 .. j0 + 3
+    const int i = place(bi, m);
+    const bool good = i < bad;
+    const float hi_i = s_hi[i], lo_i = s_lo[i], rq = s_rq[i], br = s_beta[i] * s_rk[i];
+#pragma unroll
+    for (int pair = 0; pair < 1 + (bi >> 1); ++pair) {
+      const bool below = pair < bi >> 1;  // all of these columns are of earlier tokens
+      // there e^{G_i - G_j} is a factor of the row times one of the column, both of token 31's distance
+      const float hi_m = s_hi[31], lo_m = s_lo[31];
+      float bru = br, rqu = rq;
+      if (below) {
+        const float u = __builtin_amdgcn_exp2f((hi_i - hi_m) + (lo_i - lo_m));
+        bru *= u;
+        rqu *= u;
+      }
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = 2 * pair + h, j0 = place(j, 4 * g);
+        f32x4 kk = {0, 0, 0, 0}, kq = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], x.k[bi][s], kk, 0, 0, 0);
+          kq = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], q[s], kq, 0, 0, 0);
+        }
+        const f32x4 hi_j = *(const f32x4*)(s_hi + j0), lo_j = *(const f32x4*)(s_lo + j0), rk_j = *(const f32x4*)(s_rk + j0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float f = rk_j[e] * __builtin_amdgcn_exp2f(below ? (hi_m - hi_j[e]) + (lo_m - lo_j[e]) : (hi_i - hi_j[e]) + (lo_i - lo_j[e]));
+          // (selected, not multiplied: what is above the diagonal, or of bad rows, may be anything)
+          kk[e] = good && (below || j0 + e < i) ? bru * f * kk[e] : 0.0f;
+          v[4 * h + e] = below || j0 + e <= i ? rqu * f * kq[e] : 0.0f;
+        }
+        *(f32x4*)(s_a + i * kStrideA + j0) = kk;
+      }
+      b16x8 out[2];
+      split8(v, out);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) *(b16x8*)(slot + F::kOffP + (tri(bi, pair) * 2 + part) * kFrag + lane * 16) = out[part];
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (bi < 2) request_blocks<DKP, VEC>(f.q, f.d_k, left, bi + 2, &x.q[bi], 1);
+  }
+  wave_order();
+  const float rq = s_rq[lane];
+  const double last = __shfl(sum, 63);
+  wave_order();
+  scal[lane] = lane < bad ? gate.beta : NAN;
+  scal[C + lane] = gate.beta * rk * __builtin_amdgcn_exp2f(hi);
+  scal[2 * C + lane] = rq * __builtin_amdgcn_exp2f(hi);
+  scal[3 * C + lane] = rk * __builtin_amdgcn_exp2f((float)(last - sum));
+  scal[4 * C + lane] = __builtin_amdgcn_exp2f((float)last);
+}
+
+// Second half: T = (I + A)^-1 in A's place (the method: delta_prepare), then as left operands.
+template <int DKP>
+__device__ __forceinline__ void prepare_inverse(char* slot) {
+  const int lane = own_lane(), m = lane & 15, g = lane >> 4;
+  float* const t = (float*)slot;
+  {
+    // diagonal block g, column m
+    float x[16];
+    const float* const at = t + g * 16 * kStrideA + g * 16;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float sum = i == m ? 1.0f : 0.0f;
+#pragma unroll
+      for (int l = 0; l < i; ++l) sum = fmaf(-at[i * kStrideA + l], x[l], sum);
+      x[i] = sum;
+      if (i & 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    wave_order();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[(g * 16 + i) * kStrideA + g * 16 + m] = x[i];
+    wave_order();
+  }
+  // a 16 x 16 block of X Y, n blocks of 16 deep; blocks by their row and column
+  auto product = [&](f32x4& acc, int xr, int xc, int yr, int yc, int n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < n * 16; c += 4)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t[(xr * 16 + m) * kStrideA + xc * 16 + c + g], t[(yr * 16 + c + g) * kStrideA + yc * 16 + m], acc, 0, 0, 0);
+  };
+  auto put = [&](const f32x4& v, int r, int c, float sign) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[(r * 16 + 4 * g + i) * kStrideA + c * 16 + m] = sign * v[i];
+  };
+  const f32x4 zero = {0, 0, 0, 0};
+  {
+    f32x4 x[2] = {zero, zero}, y[2] = {zero, zero};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) product(x[h], 2 * h + 1, 2 * h, 2 * h, 2 * h, 1);
+    wave_order();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put(x[h], 2 * h + 1, 2 * h, 1.0f);
+    wave_order();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) product(y[h], 2 * h + 1, 2 * h + 1, 2 * h + 1, 2 * h, 1);
+    wave_order();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put(y[h], 2 * h + 1, 2 * h, -1.0f);
+    wave_order();
+  }
+  {
+    f32x4 x[2][2] = {{zero, zero}, {zero, zero}}, y[2][2] = {{zero, zero}, {zero, zero}};
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      product(x[r][0], 2 + r, 0, 0, 0, 2);
+      product(x[r][1], 2 + r, 1, 1, 1, 1);  // (the block above T11's diagonal is zero)
+    }
+    wave_order();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) put(x[r][c], 2 + r, c, 1.0f);
+    wave_order();
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      product(y[0][c], 2, 2, 2, c, 1);
+      product(y[1][c], 3, 2, 2, c, 2);
+    }
+    wave_order();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) put(y[r][c], 2 + r, c, -1.0f);
+    wave_order();
+  }
+  float v[kTri][8];
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int f = 0; f < kTri; ++f) {
+    const int b = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) % 2;
+    const int row = place(b, m), col = 32 * s + 8 * g;
+    const f32x4 u = *(const f32x4*)(t + row * kStrideA + col), w = *(const f32x4*)(t + row * kStrideA + col + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[f][e] = e < 4 ? u[e] : w[e - 4];  // (zeros above the diagonal are there)
+  }
+  wave_order();
+#pragma unroll
+  for (int f = 0; f < kTri; ++f) {
+    b16x8 out[3];
+    split8(v[f], out);
+#pragma unroll
+    for (int part = 0; part < 3; ++part) *(b16x8*)(slot + (f * 3 + part) * kFrag + lane * 16) = out[part];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <int DKP, int NC, bool VEC>
+__global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
+  typedef FusedShape<DKP, NC> F;
+  constexpr int STEPS = F::kSteps, PIECES = 2 * C * (DKP / 8) / (NC * 64);
+  extern __shared__ __align__(16) char s_mem[];
+  const evconv_delta_args& a = p.a;
+  const int strips = (a.d_v + 15) / 16, parts = (strips + NC - 1) / NC;
+  const int64_t pair = blockIdx.x / parts;
+  const int part = blockIdx.x % parts;
+  const int seq = (int)(pair / a.heads_v), head = (int)(pair % a.heads_v), hk = head / p.share;
+  const Span span = span_of(p, seq);
+  if (span.len <= p.short_len) return;
+  const int chunks = (span.len + C - 1) / C;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto meet = [] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (wave >= NC) {  // a producer
+    // its chunks are every other one: the first half of chunk x in step x - 2, the second in step x - 1
+    int x = wave - NC, left = chunks + 2;  // steps to come
+    if (x == 1) {
+      meet();
+      --left;
+    }
+    __builtin_amdgcn_s_setprio(2);  // (the others wait for it)
+    Source<VEC> f;
+    f.gate_bf16 = a.gate_dtype == EVCONV_BF16;
+    // (where it has no further chunk it requests its last, or the sequence's last, once more: every request is for tokens that exist)
+    const int from = min(x, chunks - 1);
+    const int64_t first = span.first + (int64_t)from * C;
+    f.k = rows_of(a.k, 2, hk, first);
+    f.q = rows_of(a.q, 2, hk, first);
+    f.gate = rows_of(a.gate, f.gate_bf16 ? 2 : 4, head, first);
+    f.beta = rows_of(a.beta, f.gate_bf16 ? 2 : 4, head, first);
+    f.d_k = a.d_k;
+    f.left = span.len - from * C;
+    f.a_scale = a.flags & EVCONV_DELTA_RAW_GATES ? a.a_scale[head] : 0.0f;
+    f.dt_bias = a.flags & EVCONV_DELTA_RAW_GATES ? a.dt_bias[head] : 0.0f;
+    Ahead<DKP> ahead;
+    request_ahead(f, ahead);
+#pragma unroll 1
+    for (; left > 0; x += 2) {
+      char* const slot = s_mem + x % 3 * F::kSlot;
+      if (x < chunks) prepare_products<DKP, VEC>(p, slot, f, f.left, ahead);
+      meet();
+      if (--left == 0) break;
+      const int on = x + 2 < chunks ? 2 : 0;
+      f.k.next(on);
+      f.q.next(on);
+      f.gate.next(on);
+      f.beta.next(on);
+      f.left -= on * C;
+      request_ahead(f, ahead);
+      if (x < chunks) prepare_inverse<DKP>(slot);
+      meet();
+      --left;
+    }
+    return;
+  }
+  // (the two consumers of a SIMD out of step, so that one's vector instructions run beside the other's matrix instructions)
+
+  const int strip = part * NC + wave;
+  const bool works = strip < strips;
+  const int64_t at = state_at(p, seq, head);
+  f32x4 S[2 * STEPS];
+  {
+    const int lane = own_lane(), col = strip * 16 + (lane & 15), g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < 2 * STEPS; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = place(b, 4 * g + i);
+        S[b][i] = at >= 0 && a.state_in && row < a.d_k && col < a.d_v ? ((const EVK_GLOBAL float*)(a.state_in + at))[row * a.d_v + col] : 0.0f;
+      }
+#pragma unroll
+    for (int b = 0; b < 2 * STEPS; ++b) asm volatile("" : "+v"(S[b]));  // (waited for here, or the loop would wait in every turn)
+  }
+  const int64_t before = span.first - (int64_t)C;
+  Rows k_rows = rows_of(a.k, 2, hk, before), q_rows = rows_of(a.q, 2, hk, before);  // of chunk c + 1
+  Rows v_rows = rows_of(a.v, 2, head, before);
+  Rows o_rows = {(const char*)a.o + ((before - C) * a.o_token_stride + head * a.o_head_stride) * 2, (int)a.o_token_stride * 2};  // of c
+  u32x4 value[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};  // this lane's part of v, see `unit`
+  constexpr int HALF = PIECES / 2, PIECE_ROWS = NC * 64 / (DKP / 8);  // K's pieces, then Q's; rows of one round of them
+  // The chunk's values as left operands: 16 bytes of a token's row to a lane, of blocks 2 p and 2 p + 1 of tokens (their columns as
+  // the contraction's first and last 16 places).  A product with half a unit matrix brings them into the layout of results,
+  // and o's values back out of it: two loads and four stores a chunk where lanes' own places would take 16 of two bytes each.
+  // (Not where some value is not finite: the zeros would carry it to others.)
+  auto unit = [](int half) __attribute__((always_inline)) {
+    const int lane = own_lane(), n = lane & 15, at = 8 * (lane >> 4) - 16 * half;  // places at .. at + 7
+    u32x4 u;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) u[d] = n >> 1 == (at >> 1) + d ? (n & 1 ? 0x3f800000u : 0x3f80u) : 0u;
+    return __builtin_bit_cast(b16x8, u);
+  };
+#pragma unroll 1
+  for (int c = -2; c < chunks; ++c) {
+    const int64_t token0 = span.first + (int64_t)c * C;
+    const int count = min(span.len - c * C, C);
+    const char* const slot = s_mem + (c + 3) % 3 * F::kSlot;
+    const float* const scal = (const float*)(slot + F::kOffScal);
+    const char* const rows = s_mem + F::kOffK + (c & 1) * 2 * F::kRows;
+    const bool now = c >= 0 && works, more = c + 1 >= 0 && c + 1 < chunks;
+    // ---- rows of the next chunk, into the buffer that the last step has done with
+    if (more) {
+      const int left = span.len - (c + 1) * C, lane = own_lane();
+      char* const to = s_mem + F::kOffK + ((c + 1) & 1) * 2 * F::kRows;
+      if (VEC && a.d_k == DKP) {
+        // straight into LDS, a wave 64 neighbouring places, which at_rows' exclusive or makes those of other pieces of the row.
+        // (A token behind the end is the last one again: its rows of R and D are zero.)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const Rows& r = i < HALF ? k_rows : q_rows;
+          const int first = i % HALF * PIECE_ROWS + wave * (512 / DKP), row = first + lane / (DKP / 8), at = lane % (DKP / 8) * 16;
+          const int piece = at ^ (at_rows<DKP>(row, 0) - row * DKP * 2);
+          __builtin_amdgcn_global_load_lds(lane_at<const u32x4>(r.at, (unsigned)(min(row, left - 1) * r.step + piece)),
+                                           (__attribute__((address_space(3))) void*)(to + (i < HALF ? 0 : F::kRows) + first * DKP * 2), 16, 0, 0);
+        }
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < PIECES; ++i) {
+          const Rows& r = i < HALF ? k_rows : q_rows;
+          const int row = i % HALF * PIECE_ROWS + wave * (512 / DKP) + lane / (DKP / 8), piece = lane % (DKP / 8);
+          *(u32x4*)(to + (i < HALF ? 0 : F::kRows) + at_rows<DKP>(row, piece)) =
+              load_raw<VEC>(r.at, (unsigned)(row * r.step + piece * 16), row < left ? a.d_k - piece * 8 : 0);
+        }
+      }
+    }
+    f32x4 R[4], O[4];
+    if (now) {
+      // ---- K S and Q S
+      const int lane = own_lane(), n = lane & 15, g = lane >> 4;
+      const int at_k = at_rows<DKP>(place(0, n), g);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) R[b] = O[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        // (operands requested, S split while they come, products: left alone, each read would be waited for by itself)
+        const char* const at_s = rows + (at_k ^ (s << 6));  // (another piece of the row, by exclusive or; blocks of rows by addition)
+        b16x8 k[4][1], q[4][1];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          k[b][0] = *(const b16x8*)(at_s + place(b, 0) * DKP * 2);
+          q[b][0] = *(const b16x8*)(at_s + F::kRows + place(b, 0) * DKP * 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = S[2 * s][i];
+          v[4 + i] = S[2 * s + 1][i];
+        }
+        b16x8 Sp[3];
+        split8(v, Sp);
+        __builtin_amdgcn_sched_barrier(0);
+        mfma_parts<1, 4>(O, q, Sp);
+        mfma_parts<2, 4>(R, k, Sp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // ---- R = beta v - beta e^G K S;  e^G Q S   (behind the sequence's end all of them are zero)
+      const bool plain_v = !__ballot((not_finite(value[0]) | not_finite(value[1])) != 0);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int t0 = place(b, 4 * g);  // this lane's tokens: t0 .. t0 + 3
+        f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, value[b >> 1]), unit(b & 1), f32x4{0, 0, 0, 0}, 0, 0, 0);
+        if (!plain_v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] = t0 + i < count && strip * 16 + n < a.d_v ? load_one<true>(a.v.data, (token0 + t0 + i) * a.v.token_stride + head * a.v.head_stride + strip * 16 + n) : 0.0f;
+        const f32x4 beta = *(const f32x4*)(scal + t0), kf = *(const f32x4*)(scal + C + t0), qf = *(const f32x4*)(scal + 2 * C + t0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          R[b][i] = beta[i] * v[i] - kf[i] * R[b][i];
+          O[b][i] *= qf[i];
+        }
+        if (b & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // ---- values of the next chunk
+    if (more && works) {
+      const int left = span.len - (c + 1) * C;
+      const int lane = own_lane(), m = lane & 15, g = lane >> 4, own = strip * 16 + (g & 1) * 8;
+#pragma unroll
+      for (int pair = 0; pair < 2; ++pair) {
+        const int t = 32 * pair + place(g >> 1, m);
+        if (VEC) value[pair] = *lane_at<const u32x4>(v_rows.at, (unsigned)(min(t, left - 1) * v_rows.step + (own < a.d_v ? own : 0) * 2));
+        else value[pair] = load_raw<VEC>(v_rows.at, (unsigned)(t * v_rows.step + own * 2), t < left ? a.d_v - own : 0);
+      }
+    }
+    int first_bad = C;
+    f32x4 D[4];
+    if (now) {
+      const int lane = own_lane(), g = lane >> 4;
+      auto frag = [&](int off) __attribute__((always_inline)) { return *(const b16x8*)(slot + lane * 16 + off); };
+      // ---- D = T R; a second time, without the columns' rows from the first bad one on, where some value is not finite
+      auto apply_t = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) D[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          b16x8 t[2][3];
+          auto read_t = [&](int b0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int part = 0; part < 3; ++part) t[b][part] = frag((tri(b0 + b, s) * 3 + part) * kFrag);
+            __builtin_amdgcn_sched_barrier(0);
+          };
+          read_t(2 * s);
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = R[2 * s][i];
+            v[4 + i] = R[2 * s + 1][i];
+          }
+          b16x8 Rp[3];
+          split8(v, Rp);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int b0 = 2 * s; b0 < 4; b0 += 2) {
+            if (b0 > 2 * s) read_t(b0);
+            mfma_parts<2, 2>(D + b0, t, Rp);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      apply_t();
+      uint64_t wrong = 0;  // (a value of R that is not finite, or that a bf16 rounds to infinity, is in D too)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wrong |= __ballot(!(fabsf(D[b][i]) < kBf16Overflow));
+      if (wrong) {
+        cut_columns(R, bad_values(R), first_bad, g);
+        apply_t();
+        cut_columns(D, bad_values(D), first_bad, g);
+      }
+    }
+    if (now) {
+      const int lane = own_lane(), n = lane & 15, g = lane >> 4;
+      auto frag = [&](int off) __attribute__((always_inline)) { return *(const b16x8*)(slot + lane * 16 + off); };
+      // ---- O += P D;  S = e^G S + K' (w D)
+      const float decay = scal[4 * C];
+      const int at_t = at_rows<DKP>(8 * g + (n >> 2), n & 3);
+#pragma unroll
+      for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        b16x8 pp[4][2], kt[STEPS][1];
+        // tokens 32 s + 8 g .. + 7 of the channels place(b, .): two transposing reads of four tokens
+        auto read_k = [&](int b0) __attribute__((always_inline)) {
+#pragma unroll
+          for (int b = 0; b < STEPS; ++b) {
+            const char* const q = rows + (at_t ^ (((b0 + b) >> 1) << 6)) + 32 * s * DKP * 2 + ((b0 + b) & 1) * 8;
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)q);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * DKP * 2));
+            kt[b][0] = __builtin_bit_cast(b16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int b = 2 * s; b < 4; ++b)
+#pragma unroll
+          for (int part = 0; part < 2; ++part) pp[b][part] = frag(F::kOffP + (tri(b, s) * 2 + part) * kFrag);
+        __builtin_amdgcn_sched_barrier(0);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = D[2 * s][i];
+          v[4 + i] = D[2 * s + 1][i];
+        }
+        b16x8 Dp[2];
+        split8(v, Dp);
+        read_k(0);
+        if (s == 0) mfma_parts<1, 4>(O, pp, Dp);
+        else mfma_parts<1, 2>(O + 2, pp + 2, Dp);
+        __builtin_amdgcn_sched_barrier(0);
+        const f32x4 w0 = *(const f32x4*)(scal + 3 * C + place(2 * s, 4 * g)), w1 = *(const f32x4*)(scal + 3 * C + place(2 * s + 1, 4 * g));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] *= w0[i];
+          v[4 + i] *= w1[i];
+        }
+        b16x8 Dw[3];
+        split8(v, Dw);
+        __builtin_amdgcn_sched_barrier(0);
+        mfma_parts<2, STEPS>(S, kt, Dw);
+        __builtin_amdgcn_sched_barrier(0);
+        read_k(STEPS);
+        mfma_parts<2, STEPS>(S + STEPS, kt, Dw);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (__ballot(first_bad < C)) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (place(b, 4 * g) + i >= first_bad) O[b][i] = NAN;
+        if (first_bad < C)
+#pragma unroll
+          for (int b = 0; b < 2 * STEPS; ++b) S[b] = f32x4{NAN, NAN, NAN, NAN};
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the next chunk's rows are in LDS (o's stores, which come now, are not waited for)
+    if (now) {
+      const int lane = own_lane(), n = lane & 15, g = lane >> 4;
+      // ---- o, rounded; transposed by unit matrices (as left operand, so that a lane gets a token's neighbouring columns)
+#pragma unroll
+      for (int pair = 0; pair < 2; ++pair) {
+        u32x4 u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          u[i] = pack_bf16(O[2 * pair][2 * i], O[2 * pair][2 * i + 1]);
+          u[2 + i] = pack_bf16(O[2 * pair + 1][2 * i], O[2 * pair + 1][2 * i + 1]);
+        }
+        if (__ballot(not_finite(u) != 0)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int t = 32 * pair + 8 * g + i;
+            if (t < count && strip * 16 + n < a.d_v)
+              ((uint16_t*)a.o)[(token0 + t) * a.o_token_stride + head * a.o_head_stride + strip * 16 + n] = (uint16_t)(u[i / 2] >> (i % 2 * 16));
+          }
+          continue;
+        }
+        const int own = strip * 16 + 4 * g;  // this lane's columns: own .. own + 3
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const f32x4 w = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, u), unit(half), f32x4{0, 0, 0, 0}, 0, 0, 0);
+          const int t = 32 * pair + 16 * half;  // + n: this lane's token
+          const char* const q = o_rows.at + t * o_rows.step;
+          const unsigned at = (unsigned)(n * o_rows.step + own * 2);
+          if (t + n < count) {
+            if (VEC) {
+              if (own < a.d_v) *lane_at<u32x2>(q, at) = u32x2{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (own + i < a.d_v) *lane_at<uint16_t>(q + i * 2, at) = (uint16_t)pack_bf16(w[i], 0.0f);
+            }
+          }
+        }
+      }
+    }
+    k_rows.next(1);
+    q_rows.next(1);
+    v_rows.next(1);
+    o_rows.next(1);
+    meet();
+  }
+  if (at >= 0 && a.state_out) {
+    const int lane = own_lane(), col = strip * 16 + (lane & 15), g = lane >> 4;
+    EVK_GLOBAL float* const to = (EVK_GLOBAL float*)uniform(a.state_out + at);
+    if (col < a.d_v)
+#pragma unroll
+      for (int b = 0; b < 2 * STEPS; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = place(b, 4 * g + i);
+          if (row < a.d_k) to[row * a.d_v + col] = S[b][i];
+        }
+  }
+}
+
+template <int DKP, int NC, bool VEC>
+void start(const DeltaParams& p, hipStream_t s) {
+  const int strips = (p.a.d_v + 15) / 16, parts = (strips + NC - 1) / NC;
+  const unsigned grid = (unsigned)((int64_t)p.a.n_seq * p.a.heads_v * parts);
+  typedef FusedShape<DKP, NC> F;
+  delta_fused<DKP, NC, VEC><<<grid, F::kThreads, F::kBytes, s>>>(p);
+}
+template <int DKP>
+void start_keys(const DeltaParams& p, hipStream_t s) {
+  if (!p.vec || !p.vec_v) start<DKP, 8, false>(p, s);
+  else if (p.a.d_v > 64) start<DKP, 8, true>(p, s);
+  else start<DKP, 4, true>(p, s);
+}
+}  // namespace
+
+bool delta_fused_supported(const DeltaParams& p) {
+  // (a lane's bytes into a chunk are 32 bits)
+  auto near = [](int64_t stride) { return stride >= 0 && stride <= 1 << 23; };
+  return p.a.dtype == EVCONV_BF16 && p.a.d_k <= 128 && near(p.a.q.token_stride) && near(p.a.k.token_stride) &&
+         near(p.a.v.token_stride) && near(p.a.o_token_stride) && near(p.a.gate.token_stride) && near(p.a.beta.token_stride);
+}
+
+void launch_delta_fused(const DeltaParams& p, hipStream_t s) {
+  if (p.dkp == 64) start_keys<64>(p, s);
+  else start_keys<128>(p, s);
+}
+
+}  // namespace evk

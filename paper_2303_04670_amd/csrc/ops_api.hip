@@ -36,7 +36,7 @@ constexpr int kShort = 16;
 
 struct DeltaPlan {
   DeltaParams p;
-  bool steps, chunks;
+  bool steps, chunks, fused;
   size_t off_t, off_scal, bytes;
 };
 
@@ -65,13 +65,17 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.slots_total = (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
   d.p.dkp = a->d_k <= 64 ? 64 : a->d_k <= 128 ? 128 : 256;
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
+  d.p.vec_v = a->d_v % 8 == 0 && wide(a->dtype, a->v) && aligned(a->o, 8) && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0;
   d.steps = d.p.len < 0 || d.p.len <= kShort;
   d.chunks = d.p.len < 0 ? a->n_tokens > kShort : !d.steps;
   d.off_t = d.off_scal = d.bytes = 0;
+  d.fused = d.chunks && delta_fused_supported(d.p);
   if (d.chunks) {
     const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8 * ((a->d_v + 15) / 16);
     if (pairs >= 1ll << 31 || (int64_t)d.p.slots_total * a->heads_v >= 1ll << 31)
       return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens of %d sequences and %d heads are more than one launch takes", (long long)a->n_tokens, a->n_seq, a->heads_v);
+  }
+  if (d.chunks && !d.fused) {
     d.off_t = (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);
     d.off_scal = d.off_t + (size_t)d.p.slots_total * a->heads_v * delta_frag_t_bytes(a->dtype);
     d.bytes = d.off_scal + (size_t)d.p.slots_total * a->heads_v * kDeltaScalars * sizeof(float);
@@ -135,7 +139,7 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
   DeltaPlan d;
   const evconv_status st = plan_delta(args, &d);
   if (st != EVCONV_OK) return st;
-  if (d.chunks) {
+  if (d.chunks && !d.fused) {
     if (!workspace || workspace_bytes < d.bytes || !aligned(workspace, 256))
       return refuse(EVCONV_ERR_WORKSPACE, "delta rule: needs %zu bytes of workspace at a multiple of 256, got %zu", d.bytes, workspace ? workspace_bytes : 0);
     d.p.frag_k = (char*)workspace;
@@ -143,7 +147,8 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
     d.p.scal = (float*)((char*)workspace + d.off_scal);
   }
   if (d.steps && (args->n_tokens || args->state_out)) launch_delta_steps(d.p, (hipStream_t)hip_stream);
-  if (d.chunks) launch_delta_chunks(d.p, (hipStream_t)hip_stream);
+  if (d.fused) launch_delta_fused(d.p, (hipStream_t)hip_stream);
+  else if (d.chunks) launch_delta_chunks(d.p, (hipStream_t)hip_stream);
   return launched("delta rule");
 }
 

@@ -100,18 +100,25 @@ __device__ __forceinline__ void split8(const float (&x)[8], b16x8 (&out)[PARTS])
   }
 }
 
-// acc += a b over operands of PA and PB parts, the smallest terms first; of the products of parts those
+// acc[i] += a[i] b over operands of PA and PB parts, the smallest terms first; of the products of parts those
 // whose places add up to at most ORDER (0: high * high) are taken: what ORDER 2 leaves out is less than 2^-24
-// of a product, ORDER 1 less than 2^-15.
-template <int ORDER, int PA, int PB>
-__device__ __forceinline__ void mfma_parts(f32x4& acc, const b16x8 (&a)[PA], const b16x8 (&b)[PB]) {
+// of a product, ORDER 1 less than 2^-15.  Neighbouring instructions are of different sums: one that continues the last one's
+// would wait for it.
+template <int ORDER, int N, int PA, int PB>
+__device__ __forceinline__ void mfma_parts(f32x4* acc, const b16x8 (*a)[PA], const b16x8 (&b)[PB]) {
 #pragma unroll
   for (int o = ORDER; o >= 0; --o)
 #pragma unroll
     for (int i = 0; i < PA; ++i) {
       const int j = o - i;
-      if (j >= 0 && j < PB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc, 0, 0, 0);
+      if (j >= 0 && j < PB)
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n][i], b[j], acc[n], 0, 0, 0);
     }
+}
+template <int ORDER, int PA, int PB>
+__device__ __forceinline__ void mfma_parts(f32x4& acc, const b16x8 (&a)[PA], const b16x8 (&b)[PB]) {
+  mfma_parts<ORDER, 1>(&acc, &a, b);
 }
 
 }  // namespace evk

@@ -23,6 +23,7 @@ struct DeltaParams {
   int slots_total;  // chunk slots: n_tokens / kDeltaChunk + n_seq
   int dkp;          // d_k, rounded up to whole 32
   int vec;          // q, k rows may be read in 16-byte loads
+  int vec_v;        // v rows too, and o rows written in 8-byte stores
   // workspace
   char* frag_k;     // per chunk slot and key head: K, Q and K' as matrix-core operands
   char* frag_t;     // per chunk slot and value head: T and P
@@ -34,6 +35,9 @@ size_t delta_frag_t_bytes(int dtype);
 constexpr int kDeltaScalars = 4 * kDeltaChunk + 64;
 void launch_delta_steps(const DeltaParams& p, hipStream_t s);
 void launch_delta_chunks(const DeltaParams& p, hipStream_t s);
+// chunks in one launch, without workspace
+bool delta_fused_supported(const DeltaParams& p);
+void launch_delta_fused(const DeltaParams& p, hipStream_t s);
 
 // ---- norms around a block, rows of 8-bit integers ------------------------------------------------
 // vectors of eight that a row takes (the lanes of a group that it does not fill among them), at most
