@@ -8,6 +8,8 @@
 //
 // In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a producer
 // computes K K', Q K' and A of chunk c + 2, the other one T of chunk c + 1.
+#include <algorithm>
+
 #include "delta_device.h"
 
 namespace evk {
@@ -126,10 +128,10 @@ __device__ __forceinline__ void request_blocks(const Rows& r, int d_k, int left,
     for (int s = 0; s < DKP / 32; ++s)
       to[b][s] = __builtin_bit_cast(b16x8, load_raw<VEC>(r.at + 64 * s, (unsigned)(place(block0 + b, m) * r.step + 16 * g), place(block0 + b, m) < left ? d_k - 32 * s - 8 * g : 0));
 }
-template <int DKP, bool VEC>
+template <int DKP, bool VEC, bool TRANS>
 __device__ __forceinline__ void request_ahead(const Source<VEC>& f, Ahead<DKP>& to) {
   request_blocks<DKP, VEC>(f.k, f.d_k, f.left, 0, to.k, 4);
-  request_blocks<DKP, VEC>(f.q, f.d_k, f.left, 0, to.q, 1);
+  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, f.left, 0, to.q, 1);
   const int t = own_lane();
   const EVK_GLOBAL char *const gates = uniform(f.gate.at), *const betas = uniform(f.beta.at);
   unsigned at_g = (unsigned)(t * f.gate.step), at_b = (unsigned)(t * f.beta.step);
@@ -147,7 +149,7 @@ __device__ __forceinline__ void request_ahead(const Source<VEC>& f, Ahead<DKP>& 
 }
 
 // First half of a chunk's preparation: A (fp32, in the place of T), P, the factors of the rows.
-template <int DKP, bool VEC>
+template <int DKP, bool VEC, bool TRANS>
 __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slot, const Source<VEC>& f, int left, Ahead<DKP>& x) {
   typedef FusedShape<DKP, 8> F;
   constexpr int STEPS = F::kSteps;
@@ -156,7 +158,7 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
   float* const s_a = (float*)slot;
   float* const scal = (float*)(slot + F::kOffScal);
   float *const s_hi = scal, *const s_lo = scal + C, *const s_rk = scal + 2 * C, *const s_rq = scal + 3 * C, *const s_beta = scal + 4 * C;
-  request_blocks<DKP, VEC>(f.q, f.d_k, left, 1, &x.q[1], 1);
+  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, left, 1, &x.q[1], 1);
   // ---- a token to a lane: sums of log2 decays, as two floats each, so that differences keep their bits
   Gates gate = {0.0f, 0.0f};
   if (lane < left) gate = gates_from(a.flags & EVCONV_DELTA_RAW_GATES, x.gate, x.beta, f.a_scale, f.dt_bias);
@@ -197,7 +199,8 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
 #pragma unroll
   for (int bi = 0; bi < 4; ++bi) {
     const b16x8 (&q)[STEPS] = x.q[bi & 1];
-    if (normalize) {
+    if (TRANS) {
+    } else if (normalize) {
       const float u = diagonal(q);
       if (m >> 2 == g) s_rq[place(bi, m)] = a.scale / sqrtf(u + 1e-6f);
     } else if (g == 0) {
@@ -227,7 +230,7 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
           kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], x.k[bi][s], kk, 0, 0, 0);
-          kq = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], q[s], kq, 0, 0, 0);
+          if (!TRANS) kq = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], q[s], kq, 0, 0, 0);
         }
         const f32x4 hi_j = *(const f32x4*)(s_hi + j0), lo_j = *(const f32x4*)(s_lo + j0), rk_j = *(const f32x4*)(s_rk + j0);
 #pragma unroll
@@ -241,11 +244,12 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
       }
       b16x8 out[2];
       split8(v, out);
+      if (!TRANS)
 #pragma unroll
       for (int part = 0; part < 2; ++part) *(b16x8*)(slot + F::kOffP + (tri(bi, pair) * 2 + part) * kFrag + lane * 16) = out[part];
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (bi < 2) request_blocks<DKP, VEC>(f.q, f.d_k, left, bi + 2, &x.q[bi], 1);
+    if (!TRANS && bi < 2) request_blocks<DKP, VEC>(f.q, f.d_k, left, bi + 2, &x.q[bi], 1);
   }
   wave_order();
   const float rq = s_rq[lane];
@@ -352,18 +356,32 @@ __device__ __forceinline__ void prepare_inverse(char* slot) {
   }
 }
 
-template <int DKP, int NC, bool VEC>
+// Few heads and long sequences: segments of a sequence side by side (p.segs of p.seg_chunks chunks).  What a segment does to the
+// state it starts from is S -> M S + N, so a first launch (TRANS: no outputs) runs the segments from zero, which gives N, and
+// with the columns of the unit matrix as further columns of a state and no values, which gives M (the first
+// segment from the given state; the last one is not needed); delta_join goes through them; the second launch runs
+// every segment from its start.
+template <int DKP, int NC, bool VEC, bool TRANS>
 __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
   typedef FusedShape<DKP, NC> F;
   constexpr int STEPS = F::kSteps, PIECES = 2 * C * (DKP / 8) / (NC * 64);
   extern __shared__ __align__(16) char s_mem[];
   const evconv_delta_args& a = p.a;
-  const int strips = (a.d_v + 15) / 16, parts = (strips + NC - 1) / NC;
-  const int64_t pair = blockIdx.x / parts;
-  const int part = blockIdx.x % parts;
+  const int strips_v = (a.d_v + 15) / 16, strips = strips_v + (TRANS ? (a.d_k + 15) / 16 : 0), parts = (strips + NC - 1) / NC;
+  const int part = blockIdx.x % parts, segs = TRANS ? p.segs - 1 : p.segs, seg = blockIdx.x / parts % segs;
+  const int64_t pair = blockIdx.x / parts / segs;
   const int seq = (int)(pair / a.heads_v), head = (int)(pair % a.heads_v), hk = head / p.share;
-  const Span span = span_of(p, seq);
+  Span span = span_of(p, seq);
   if (span.len <= p.short_len) return;
+  {
+    const int64_t skip = (int64_t)seg * p.seg_chunks * C;
+    if (span.len <= skip + (TRANS ? p.seg_chunks * C : 0)) return;  // (TRANS: nothing behind it)
+    if (TRANS && seg == 0 && part * NC >= strips_v) return;
+    span.first += (int)skip;
+    span.len -= (int)skip;
+  }
+  const bool last = span.len <= p.seg_chunks * C;
+  span.len = min(span.len, p.seg_chunks * C);
   const int chunks = (span.len + C - 1) / C;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   auto meet = [] {
@@ -393,11 +411,11 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
     f.a_scale = a.flags & EVCONV_DELTA_RAW_GATES ? a.a_scale[head] : 0.0f;
     f.dt_bias = a.flags & EVCONV_DELTA_RAW_GATES ? a.dt_bias[head] : 0.0f;
     Ahead<DKP> ahead;
-    request_ahead(f, ahead);
+    request_ahead<DKP, VEC, TRANS>(f, ahead);
 #pragma unroll 1
     for (; left > 0; x += 2) {
       char* const slot = s_mem + x % 3 * F::kSlot;
-      if (x < chunks) prepare_products<DKP, VEC>(p, slot, f, f.left, ahead);
+      if (x < chunks) prepare_products<DKP, VEC, TRANS>(p, slot, f, f.left, ahead);
       meet();
       if (--left == 0) break;
       const int on = x + 2 < chunks ? 2 : 0;
@@ -406,7 +424,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
       f.gate.next(on);
       f.beta.next(on);
       f.left -= on * C;
-      request_ahead(f, ahead);
+      request_ahead<DKP, VEC, TRANS>(f, ahead);
       if (x < chunks) prepare_inverse<DKP>(slot);
       meet();
       --left;
@@ -416,18 +434,39 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
   // (the two consumers of a SIMD out of step, so that one's vector instructions run beside the other's matrix instructions)
 
   const int strip = part * NC + wave;
-  const bool works = strip < strips;
+  const bool unit_columns = TRANS && strip >= strips_v;
+  const bool works = strip < strips && !(unit_columns && seg == 0);
   const int64_t at = state_at(p, seq, head);
+  const int ld = TRANS ? strips * 16 : (strips_v + (a.d_k + 15) / 16) * 16;  // floats between the rows of p.trans
+  float* const trans = p.trans + (pair * p.segs + seg) * a.d_k * (int64_t)ld;  // N, M; behind delta_join N is the next segment's start
+  float* const start0 = p.start0 + pair * a.d_k * (int64_t)(strips_v * 16);    // (the first segment's: its place may be state_out's)
   f32x4 S[2 * STEPS];
   {
     const int lane = own_lane(), col = strip * 16 + (lane & 15), g = lane >> 4;
+    const float* from = a.state_in ? a.state_in + at : nullptr;
+    int width = a.d_v;
+    bool there = at >= 0 && a.state_in && col < a.d_v;
+    if (TRANS) there &= seg == 0;
+    else if (seg || !last) {
+      from = seg ? p.trans + (pair * p.segs + seg - 1) * a.d_k * (int64_t)ld : start0;
+      width = seg ? ld : strips_v * 16;
+      there = strip < strips_v;
+    }
 #pragma unroll
     for (int b = 0; b < 2 * STEPS; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = place(b, 4 * g + i);
-        S[b][i] = at >= 0 && a.state_in && row < a.d_k && col < a.d_v ? ((const EVK_GLOBAL float*)(a.state_in + at))[row * a.d_v + col] : 0.0f;
+        S[b][i] = there && row < a.d_k ? ((const EVK_GLOBAL float*)from)[row * width + col] : unit_columns && row == col - strips_v * 16 ? 1.0f : 0.0f;
       }
+    if (TRANS && seg == 0 && works)
+#pragma unroll
+      for (int b = 0; b < 2 * STEPS; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = place(b, 4 * g + i);
+          if (row < a.d_k) start0[row * strips_v * 16 + col] = S[b][i];
+        }
 #pragma unroll
     for (int b = 0; b < 2 * STEPS; ++b) asm volatile("" : "+v"(S[b]));  // (waited for here, or the loop would wait in every turn)
   }
@@ -464,7 +503,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
         // straight into LDS, a wave 64 neighbouring places, which at_rows' exclusive or makes those of other pieces of the row.
         // (A token behind the end is the last one again: its rows of R and D are zero.)
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
+        for (int i = 0; i < (TRANS ? HALF : PIECES); ++i) {
           const Rows& r = i < HALF ? k_rows : q_rows;
           const int first = i % HALF * PIECE_ROWS + wave * (512 / DKP), row = first + lane / (DKP / 8), at = lane % (DKP / 8) * 16;
           const int piece = at ^ (at_rows<DKP>(row, 0) - row * DKP * 2);
@@ -473,7 +512,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
         }
       } else {
 #pragma unroll 1
-        for (int i = 0; i < PIECES; ++i) {
+        for (int i = 0; i < (TRANS ? HALF : PIECES); ++i) {
           const Rows& r = i < HALF ? k_rows : q_rows;
           const int row = i % HALF * PIECE_ROWS + wave * (512 / DKP) + lane / (DKP / 8), piece = lane % (DKP / 8);
           *(u32x4*)(to + (i < HALF ? 0 : F::kRows) + at_rows<DKP>(row, piece)) =
@@ -496,7 +535,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           k[b][0] = *(const b16x8*)(at_s + place(b, 0) * DKP * 2);
-          q[b][0] = *(const b16x8*)(at_s + F::kRows + place(b, 0) * DKP * 2);
+          if (!TRANS) q[b][0] = *(const b16x8*)(at_s + F::kRows + place(b, 0) * DKP * 2);
         }
         __builtin_amdgcn_sched_barrier(0);
         float v[8];
@@ -508,7 +547,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
         b16x8 Sp[3];
         split8(v, Sp);
         __builtin_amdgcn_sched_barrier(0);
-        mfma_parts<1, 4>(O, q, Sp);
+        if (!TRANS) mfma_parts<1, 4>(O, q, Sp);
         mfma_parts<2, 4>(R, k, Sp);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -532,7 +571,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
       }
     }
     // ---- values of the next chunk
-    if (more && works) {
+    if (more && works && !unit_columns) {
       const int left = span.len - (c + 1) * C;
       const int lane = own_lane(), m = lane & 15, g = lane >> 4, own = strip * 16 + (g & 1) * 8;
 #pragma unroll
@@ -615,6 +654,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
           }
           __builtin_amdgcn_sched_barrier(0);
         };
+        if (!TRANS)
 #pragma unroll
         for (int b = 2 * s; b < 4; ++b)
 #pragma unroll
@@ -629,7 +669,8 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
         b16x8 Dp[2];
         split8(v, Dp);
         read_k(0);
-        if (s == 0) mfma_parts<1, 4>(O, pp, Dp);
+        if (TRANS) {
+        } else if (s == 0) mfma_parts<1, 4>(O, pp, Dp);
         else mfma_parts<1, 2>(O + 2, pp + 2, Dp);
         __builtin_amdgcn_sched_barrier(0);
         const f32x4 w0 = *(const f32x4*)(scal + 3 * C + place(2 * s, 4 * g)), w1 = *(const f32x4*)(scal + 3 * C + place(2 * s + 1, 4 * g));
@@ -659,7 +700,7 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the next chunk's rows are in LDS (o's stores, which come now, are not waited for)
-    if (now) {
+    if (!TRANS && now) {
       const int lane = own_lane(), n = lane & 15, g = lane >> 4;
       // ---- o, rounded; transposed by unit matrices (as left operand, so that a lane gets a token's neighbouring columns)
 #pragma unroll
@@ -704,31 +745,111 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
     o_rows.next(1);
     meet();
   }
-  if (at >= 0 && a.state_out) {
-    const int lane = own_lane(), col = strip * 16 + (lane & 15), g = lane >> 4;
-    EVK_GLOBAL float* const to = (EVK_GLOBAL float*)uniform(a.state_out + at);
-    if (col < a.d_v)
+  float* const out = TRANS ? trans : at >= 0 && a.state_out && last ? a.state_out + at : nullptr;
+  if (out && works) {
+    const int lane = own_lane(), col = strip * 16 + (lane & 15), g = lane >> 4, width = TRANS ? ld : a.d_v;
+    EVK_GLOBAL float* const to = (EVK_GLOBAL float*)uniform(out);
+    if (TRANS || col < a.d_v)
 #pragma unroll
       for (int b = 0; b < 2 * STEPS; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int row = place(b, 4 * g + i);
-          if (row < a.d_k) to[row * a.d_v + col] = S[b][i];
+          if (row < a.d_k) to[row * width + col] = S[b][i];
         }
   }
 }
 
+// The states that the segments start from: N_j becomes M_j (the start of segment j) + N_j, for one segment after the other.  A
+// workgroup has 16 columns of one head, its waves DKP / 64 blocks of 16 rows each; fp32 matrix instructions, the next M on its way.
+template <int DKP>
+__global__ __launch_bounds__(256) void delta_join(DeltaParams p) {
+  constexpr int BLOCKS = DKP / 64, DEEP = DKP / 16;
+  __shared__ float s_state[DKP][17];
+  const evconv_delta_args& a = p.a;
+  const int strips_v = (a.d_v + 15) / 16, ld = (strips_v + (a.d_k + 15) / 16) * 16;
+  const int strip = blockIdx.x % strips_v;
+  const int64_t pair = blockIdx.x / strips_v;
+  const Span span = span_of(p, (int)(pair / a.heads_v));
+  const int segs = (span.len + p.seg_chunks * C - 1) / (p.seg_chunks * C);
+  if (span.len <= p.short_len || segs < 3) return;  // (N of the first segment is the second one's start)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4, col = strip * 16 + m;
+  auto segment = [&](int j) { return p.trans + (pair * p.segs + j) * a.d_k * (int64_t)ld; };
+  f32x4 S[BLOCKS], N[BLOCKS], M[BLOCKS][DEEP];
+  auto request = [&](int j) __attribute__((always_inline)) {
+    const float* const q = segment(j);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      const int row0 = (wave * BLOCKS + b) * 16;
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d)  // columns 16 d + 4 g .. + 3 of row m (behind d_k they are zero up to whole 16)
+        M[b][d] = row0 + m < a.d_k && 16 * d < a.d_k ? *(const f32x4*)(q + (row0 + m) * ld + strips_v * 16 + 16 * d + 4 * g) : f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) N[b][i] = row0 + 4 * g + i < a.d_k ? q[(row0 + 4 * g + i) * ld + col] : 0.0f;
+    }
+  };
+  {
+    const float* const q = segment(0);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = (wave * BLOCKS + b) * 16 + 4 * g + i;
+        S[b][i] = row < a.d_k ? q[row * ld + col] : 0.0f;
+      }
+  }
+  request(1);
+  for (int j = 1; j < segs - 1; ++j) {
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_state[(wave * BLOCKS + b) * 16 + 4 * g + i][m] = S[b][i];
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) S[b] = N[b];
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = s_state[16 * d + 4 * g + e][m];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(M[b][d][e], x, S[b], 0, 0, 0);
+      }
+    __syncthreads();
+    if (j + 1 < segs - 1) request(j + 1);
+    float* const q = segment(j);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = (wave * BLOCKS + b) * 16 + 4 * g + i;
+        if (row < a.d_k) q[row * ld + col] = S[b][i];
+      }
+  }
+}
+
+// Consumer waves of a workgroup.
+int delta_fused_waves(const DeltaParams& p) { return p.vec && p.vec_v && p.a.d_v <= 64 ? 4 : 8; }
+template <int DKP, int NC, bool VEC, bool TRANS>
+void start_pass(const DeltaParams& p, hipStream_t s) {
+  typedef FusedShape<DKP, NC> F;
+  const int strips = (p.a.d_v + 15) / 16 + (TRANS ? (p.a.d_k + 15) / 16 : 0), parts = (strips + NC - 1) / NC;
+  const int64_t grid = (int64_t)p.a.n_seq * p.a.heads_v * (TRANS ? p.segs - 1 : p.segs) * parts;
+  delta_fused<DKP, NC, VEC, TRANS><<<(unsigned)grid, F::kThreads, F::kBytes, s>>>(p);
+}
 template <int DKP, int NC, bool VEC>
 void start(const DeltaParams& p, hipStream_t s) {
-  const int strips = (p.a.d_v + 15) / 16, parts = (strips + NC - 1) / NC;
-  const unsigned grid = (unsigned)((int64_t)p.a.n_seq * p.a.heads_v * parts);
-  typedef FusedShape<DKP, NC> F;
-  delta_fused<DKP, NC, VEC><<<grid, F::kThreads, F::kBytes, s>>>(p);
+  if (p.segs > 1) {
+    start_pass<DKP, NC, VEC, true>(p, s);
+    const int64_t grid = (int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 15) / 16);
+    delta_join<DKP><<<(unsigned)grid, 256, 0, s>>>(p);
+  }
+  start_pass<DKP, NC, VEC, false>(p, s);
 }
 template <int DKP>
 void start_keys(const DeltaParams& p, hipStream_t s) {
   if (!p.vec || !p.vec_v) start<DKP, 8, false>(p, s);
-  else if (p.a.d_v > 64) start<DKP, 8, true>(p, s);
+  else if (delta_fused_waves(p) == 8) start<DKP, 8, true>(p, s);
   else start<DKP, 4, true>(p, s);
 }
 }  // namespace
@@ -738,6 +859,32 @@ bool delta_fused_supported(const DeltaParams& p) {
   auto near = [](int64_t stride) { return stride >= 0 && stride <= 1 << 23; };
   return p.a.dtype == EVCONV_BF16 && p.a.d_k <= 128 && near(p.a.q.token_stride) && near(p.a.k.token_stride) &&
          near(p.a.v.token_stride) && near(p.a.o_token_stride) && near(p.a.gate.token_stride) && near(p.a.beta.token_stride);
+}
+
+// A workgroup of the unsplit launch per head and strips; where they leave most of the chip idle and sequences are long, segments,
+// as many as give every compute unit one, of 16 chunks at least.  Three segments cost what they save: every
+// chunk is worked on twice, the first time with twice the columns (us, heads of 128 x 128, whole / in segments:
+// see delta_fused).
+size_t plan_delta_segments(DeltaParams& p) {
+  const int waves = delta_fused_waves(p), strips_v = (p.a.d_v + 15) / 16, parts = (strips_v + waves - 1) / waves;
+  const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, groups = pairs * parts;
+  const int64_t most = p.len >= 0 ? (p.len + C - 1) / C : p.a.n_tokens / C + 1;                          // chunks of a sequence
+  const int64_t sum = p.len >= 0 ? most * p.a.n_seq : p.a.n_tokens / C + p.a.n_seq;                      // of all
+  p.segs = 1;
+  p.seg_chunks = (int)most;
+  if (groups >= 128 || sum / p.a.n_seq < 64) return 0;
+  const int64_t chunks = std::max<int64_t>(16, (sum * p.a.heads_v * parts + 255) / 256), segs = (most + chunks - 1) / chunks;
+  const int64_t state = (int64_t)p.a.d_k * (strips_v + (p.a.d_k + 15) / 16) * 16 * 4, start = (int64_t)p.a.d_k * strips_v * 16 * 4;
+  const int64_t bytes = pairs * (segs * state + start);
+  if (segs < 4 || bytes > 2ll << 30 || pairs * segs * parts * 8 >= 1ll << 31) return 0;
+  p.segs = (int)segs;
+  p.seg_chunks = (int)chunks;
+  return (size_t)bytes;
+}
+void place_delta_segments(DeltaParams& p, char* workspace) {
+  const int strips_v = (p.a.d_v + 15) / 16;
+  p.trans = (float*)workspace;
+  p.start0 = p.trans + (int64_t)p.a.n_seq * p.a.heads_v * p.segs * p.a.d_k * (strips_v + (p.a.d_k + 15) / 16) * 16;
 }
 
 void launch_delta_fused(const DeltaParams& p, hipStream_t s) {

@@ -75,6 +75,7 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
     if (pairs >= 1ll << 31 || (int64_t)d.p.slots_total * a->heads_v >= 1ll << 31)
       return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens of %d sequences and %d heads are more than one launch takes", (long long)a->n_tokens, a->n_seq, a->heads_v);
   }
+  if (d.fused) d.bytes = plan_delta_segments(d.p);
   if (d.chunks && !d.fused) {
     d.off_t = (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);
     d.off_scal = d.off_t + (size_t)d.p.slots_total * a->heads_v * delta_frag_t_bytes(a->dtype);
@@ -139,9 +140,10 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
   DeltaPlan d;
   const evconv_status st = plan_delta(args, &d);
   if (st != EVCONV_OK) return st;
+  if (d.bytes && (!workspace || workspace_bytes < d.bytes || !aligned(workspace, 256)))
+    return refuse(EVCONV_ERR_WORKSPACE, "delta rule: needs %zu bytes of workspace at a multiple of 256, got %zu", d.bytes, workspace ? workspace_bytes : 0);
+  if (d.fused && d.p.segs > 1) place_delta_segments(d.p, (char*)workspace);
   if (d.chunks && !d.fused) {
-    if (!workspace || workspace_bytes < d.bytes || !aligned(workspace, 256))
-      return refuse(EVCONV_ERR_WORKSPACE, "delta rule: needs %zu bytes of workspace at a multiple of 256, got %zu", d.bytes, workspace ? workspace_bytes : 0);
     d.p.frag_k = (char*)workspace;
     d.p.frag_t = (char*)workspace + d.off_t;
     d.p.scal = (float*)((char*)workspace + d.off_scal);

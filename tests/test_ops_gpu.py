@@ -107,6 +107,38 @@ def test_delta_rule_long_sequence():
     close(s, want_s)
 
 
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 64), (2, 2, 128, 128), (1, 1, 40, 24), (1, 1, 37, 70), (1, 1, 128, 17)])
+def test_delta_rule_in_segments(hk, hv, dk, dv):
+    """Sequences long enough, and heads few enough, to be worked on in segments side by side; states in place."""
+    torch, ops = torch_ops()
+    for lens in ([4500], [70, 9000, 0, 5, 3100]):
+        x = delta_inputs(16 + dk, sum(lens), len(lens), hk, hv, dk, dv, "bf16", True)
+        d = {n: a.cuda() for n, a in x.items()}
+        o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], state_out=d["state"], seq_offsets=offsets(lens),
+                              normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
+        c = numbers(x)
+        want_o, want_s = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], c["state"], spans_of(lens), dk ** -0.5, True,
+                                            c["a_scale"], c["dt_bias"])
+        close(o, want_o, True)
+        close(s, want_s)
+    # no state to begin with, none to leave, and a value that is not finite in one column of one segment
+    n = 4500
+    x = delta_inputs(17, n, 1, hk, hv, dk, dv, "bf16", True)
+    d = {name: a.cuda() for name, a in x.items()}
+    kw = dict(normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
+    o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], 0 * d["state"], n_seq=1, **kw)
+    p, t = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], **kw)
+    assert torch.equal(o, p) and torch.equal(s, t)
+    p, t = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], n_seq=1,
+                          slots=torch.full((1,), -1, dtype=torch.int32, device="cuda"), state_out=torch.full_like(s, 5.0), **kw)
+    assert torch.equal(o, p) and (t == 5.0).all()
+    d["v"][2000, 0, 3] = np.nan
+    p, t = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], **kw)
+    rest = [i for i in range(dv) if i != 3]
+    assert torch.equal(p[:, :, rest], o[:, :, rest]) and torch.equal(p[:2000], o[:2000]) and torch.equal(p[:, 1:], o[:, 1:])
+    assert torch.equal(t[..., rest], s[..., rest]) and t[0, 0, :, 3].isnan().all() and p[2000:, 0, 3].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_delta_rule_reads_slices_of_a_projection(dtype):
     """q, k, v and the gates as strided views, rows at odd addresses too, give the bits of contiguous ones."""
