@@ -1,13 +1,13 @@
 // The gated delta rule in chunks, one launch (bf16 keys of up to 128 channels; formulas and precision: kernels_delta.hip).
 //
 // A workgroup owns a sequence's value head and NC strips of 16 state columns, a wave each (a consumer), and goes
-// through the chunks; two further waves (producers) take turns at preparing the chunks ahead: T and P, which do
+// through the chunks; two pairs of further waves (producers) take turns at preparing the chunks ahead: T and P, which do
 // not depend on the state.  Nothing that is computed once leaves the compute unit: keys and queries are read once into LDS
 // (the transposed operand K' comes from the same rows by transposing LDS reads), T and P go from producer to
 // consumer through a ring of three slots, S, R and D stay in their lanes (kernels_delta.hip: place).
 //
-// In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a producer
-// computes K K', Q K' and A of chunk c + 2, the other one T of chunk c + 1.
+// In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a pair of producers
+// computes K K', Q K' and A of chunk c + 2, the other pair T of chunk c + 1.
 #include <algorithm>
 
 #include "delta_device.h"
@@ -25,8 +25,8 @@ struct FusedShape {
   static constexpr int kSteps = DKP / 32;
   static constexpr int kOffP = kTri * 3 * kFrag, kOffScal = kOffP + kTri * 2 * kFrag, kSlot = kOffScal + 5 * C * 4;
   static constexpr int kRows = C * DKP * 2;  // bytes of a chunk's K (or Q)
-  static constexpr int kOffK = 3 * kSlot, kBytes = kOffK + 4 * kRows;
-  static constexpr int kThreads = (NC + 2) * 64;
+  static constexpr int kOffK = 3 * kSlot, kOffTemp = kOffK + 4 * kRows, kBytes = kOffTemp + 2 * 3 * C * 4;
+  static constexpr int kThreads = (NC + 4) * 64;
   static_assert(C * kStrideA * 4 <= kOffP && kBytes <= 160 * 1024, "LDS");
 };
 // Place of the 16-byte piece c of row `row` of K (Q) in LDS: the 16 rows of an operand load, and the four rows of a
@@ -128,10 +128,12 @@ __device__ __forceinline__ void request_blocks(const Rows& r, int d_k, int left,
     for (int s = 0; s < DKP / 32; ++s)
       to[b][s] = __builtin_bit_cast(b16x8, load_raw<VEC>(r.at + 64 * s, (unsigned)(place(block0 + b, m) * r.step + 16 * g), place(block0 + b, m) < left ? d_k - 32 * s - 8 * g : 0));
 }
-template <int DKP, bool VEC, bool TRANS>
+// Row blocks of A and P that each of the two producers of a chunk computes: as many products each.
+__device__ __forceinline__ constexpr int row_block(int role, int n) { return role == 0 ? 3 * n : 1 + n; }
+template <int DKP, bool VEC, bool TRANS, int ROLE>
 __device__ __forceinline__ void request_ahead(const Source<VEC>& f, Ahead<DKP>& to) {
   request_blocks<DKP, VEC>(f.k, f.d_k, f.left, 0, to.k, 4);
-  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, f.left, 0, to.q, 1);
+  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, f.left, row_block(ROLE, 0), to.q, 1);
   const int t = own_lane();
   const EVK_GLOBAL char *const gates = uniform(f.gate.at), *const betas = uniform(f.beta.at);
   unsigned at_g = (unsigned)(t * f.gate.step), at_b = (unsigned)(t * f.beta.step);
@@ -148,17 +150,17 @@ __device__ __forceinline__ void request_ahead(const Source<VEC>& f, Ahead<DKP>& 
   }
 }
 
-// First half of a chunk's preparation: A (fp32, in the place of T), P, the factors of the rows.
-template <int DKP, bool VEC, bool TRANS>
-__device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slot, const Source<VEC>& f, int left, Ahead<DKP>& x) {
+// First half of a chunk's preparation, by two waves: A (fp32, in the place of T), P, the factors of the rows.
+template <int DKP, bool VEC, bool TRANS, int ROLE>
+__device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slot, float* temp, const Source<VEC>& f, int left, Ahead<DKP>& x) {
   typedef FusedShape<DKP, 8> F;
   constexpr int STEPS = F::kSteps;
   const evconv_delta_args& a = p.a;
   const int lane = own_lane(), m = lane & 15, g = lane >> 4;
   float* const s_a = (float*)slot;
   float* const scal = (float*)(slot + F::kOffScal);
-  float *const s_hi = scal, *const s_lo = scal + C, *const s_rk = scal + 2 * C, *const s_rq = scal + 3 * C, *const s_beta = scal + 4 * C;
-  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, left, 1, &x.q[1], 1);
+  float *const s_hi = temp, *const s_lo = temp + C, *const s_rk = temp + 2 * C;
+  if (!TRANS) request_blocks<DKP, VEC>(f.q, f.d_k, left, row_block(ROLE, 1), &x.q[1], 1);
   // ---- a token to a lane: sums of log2 decays, as two floats each, so that differences keep their bits
   Gates gate = {0.0f, 0.0f};
   if (lane < left) gate = gates_from(a.flags & EVCONV_DELTA_RAW_GATES, x.gate, x.beta, f.a_scale, f.dt_bias);
@@ -171,7 +173,6 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
   const float hi = (float)sum, lo = isfinite(hi) ? (float)(sum - (double)hi) : 0.0f;
   s_hi[lane] = hi;
   s_lo[lane] = lo;
-  s_beta[lane] = gate.beta;
   // ---- norms: diagonals of K K' and Q Q', which lanes with m / 4 == g hold
   const bool normalize = a.flags & EVCONV_DELTA_NORMALIZE;
   auto diagonal = [&](const b16x8 (&v)[STEPS]) __attribute__((always_inline)) {
@@ -193,24 +194,22 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
   const int bad = wrong ? (int)__builtin_ctzll(wrong) : C;
   const float rk = normalize ? 1.0f / sqrtf(square + 1e-6f) : 1.0f;
   s_rk[lane] = rk;
-  if (lane >= bad) s_beta[lane] = 0.0f;
+  const float beta_rk = lane < bad ? gate.beta * rk : 0.0f;
   __builtin_amdgcn_sched_barrier(0);
   // ---- rows 16 at a time
 #pragma unroll
-  for (int bi = 0; bi < 4; ++bi) {
-    const b16x8 (&q)[STEPS] = x.q[bi & 1];
-    if (TRANS) {
-    } else if (normalize) {
-      const float u = diagonal(q);
-      if (m >> 2 == g) s_rq[place(bi, m)] = a.scale / sqrtf(u + 1e-6f);
-    } else if (g == 0) {
-      s_rq[place(bi, m)] = a.scale;
-    }
+  for (int n = 0; n < 2; ++n) {
+    const int bi = row_block(ROLE, n), i = place(bi, m);
+    const b16x8 (&q)[STEPS] = x.q[n];
     wave_order();
-    // a lane holds of block j the row i = place(bi, m) of A and P, columns j0 .. j0 + 3
-    const int i = place(bi, m);
+    const float hi_i = s_hi[i], lo_i = s_lo[i], br = __shfl(beta_rk, i);
     const bool good = i < bad;
-    const float hi_i = s_hi[i], lo_i = s_lo[i], rq = s_rq[i], br = s_beta[i] * s_rk[i];
+    float rq = a.scale;
+    if (!TRANS) {
+      if (normalize) rq = a.scale / sqrtf(__shfl(diagonal(q), (m >> 2) << 4 | m) + 1e-6f);
+      if (g == 0) scal[2 * C + i] = rq * __builtin_amdgcn_exp2f(hi_i);
+    }
+    // a lane holds of block j the row i = place(bi, m) of A and P, columns j0 .. j0 + 3
 #pragma unroll
     for (int pair = 0; pair < 1 + (bi >> 1); ++pair) {
       const bool below = pair < bi >> 1;  // all of these columns are of earlier tokens
@@ -222,44 +221,46 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
         bru *= u;
         rqu *= u;
       }
+      f32x4 kk[2], kq[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) kk[h] = kq[h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          kk[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[2 * pair + h][s], x.k[bi][s], kk[h], 0, 0, 0);
+          if (!TRANS) kq[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[2 * pair + h][s], q[s], kq[h], 0, 0, 0);
+        }
       float v[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int j = 2 * pair + h, j0 = place(j, 4 * g);
-        f32x4 kk = {0, 0, 0, 0}, kq = {0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          kk = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], x.k[bi][s], kk, 0, 0, 0);
-          if (!TRANS) kq = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[j][s], q[s], kq, 0, 0, 0);
-        }
+        const int j0 = place(2 * pair + h, 4 * g);
         const f32x4 hi_j = *(const f32x4*)(s_hi + j0), lo_j = *(const f32x4*)(s_lo + j0), rk_j = *(const f32x4*)(s_rk + j0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float f = rk_j[e] * __builtin_amdgcn_exp2f(below ? (hi_m - hi_j[e]) + (lo_m - lo_j[e]) : (hi_i - hi_j[e]) + (lo_i - lo_j[e]));
+          const float w = rk_j[e] * __builtin_amdgcn_exp2f(below ? (hi_m - hi_j[e]) + (lo_m - lo_j[e]) : (hi_i - hi_j[e]) + (lo_i - lo_j[e]));
           // (selected, not multiplied: what is above the diagonal, or of bad rows, may be anything)
-          kk[e] = good && (below || j0 + e < i) ? bru * f * kk[e] : 0.0f;
-          v[4 * h + e] = below || j0 + e <= i ? rqu * f * kq[e] : 0.0f;
+          kk[h][e] = good && (below || j0 + e < i) ? bru * w * kk[h][e] : 0.0f;
+          v[4 * h + e] = below || j0 + e <= i ? rqu * w * kq[h][e] : 0.0f;
         }
-        *(f32x4*)(s_a + i * kStrideA + j0) = kk;
+        *(f32x4*)(s_a + i * kStrideA + j0) = kk[h];
       }
-      b16x8 out[2];
-      split8(v, out);
-      if (!TRANS)
+      if (!TRANS) {
+        b16x8 out[2];
+        split8(v, out);
 #pragma unroll
-      for (int part = 0; part < 2; ++part) *(b16x8*)(slot + F::kOffP + (tri(bi, pair) * 2 + part) * kFrag + lane * 16) = out[part];
+        for (int part = 0; part < 2; ++part) *(b16x8*)(slot + F::kOffP + (tri(bi, pair) * 2 + part) * kFrag + lane * 16) = out[part];
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (!TRANS && bi < 2) request_blocks<DKP, VEC>(f.q, f.d_k, left, bi + 2, &x.q[bi], 1);
   }
-  wave_order();
-  const float rq = s_rq[lane];
-  const double last = __shfl(sum, 63);
-  wave_order();
-  scal[lane] = lane < bad ? gate.beta : NAN;
-  scal[C + lane] = gate.beta * rk * __builtin_amdgcn_exp2f(hi);
-  scal[2 * C + lane] = rq * __builtin_amdgcn_exp2f(hi);
-  scal[3 * C + lane] = rk * __builtin_amdgcn_exp2f((float)(last - sum));
-  scal[4 * C + lane] = __builtin_amdgcn_exp2f((float)last);
+  if (ROLE == 0) {
+    const double last = __shfl(sum, 63);
+    scal[lane] = lane < bad ? gate.beta : NAN;
+    scal[C + lane] = gate.beta * rk * __builtin_amdgcn_exp2f(hi);
+    scal[3 * C + lane] = rk * __builtin_amdgcn_exp2f((float)(last - sum));
+    scal[4 * C + lane] = __builtin_amdgcn_exp2f((float)last);
+  }
 }
 
 // Second half: T = (I + A)^-1 in A's place (the method: delta_prepare), then as left operands.
@@ -356,13 +357,67 @@ __device__ __forceinline__ void prepare_inverse(char* slot) {
   }
 }
 
+// All waves of a workgroup; what they wrote to LDS is there behind it.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// A producer: every other chunk; the first half of chunk x in step x - 2, the second in step x - 1 (ROLE 0; the other
+// one of the pair has nothing to do there).
+template <int DKP, int NC, bool VEC, bool TRANS, int ROLE>
+__device__ __forceinline__ void produce(const DeltaParams& p, char* s_mem, const Span& span, int chunks, int x, int head, int hk) {
+  typedef FusedShape<DKP, NC> F;
+  const evconv_delta_args& a = p.a;
+  float* const temp = (float*)(s_mem + F::kOffTemp) + ROLE * 3 * C;
+  int left = chunks + 2;  // steps to come
+  if (x == 1) {
+    meet();
+    --left;
+  }
+  __builtin_amdgcn_s_setprio(2);  // (the consumers wait for it)
+  Source<VEC> f;
+  f.gate_bf16 = a.gate_dtype == EVCONV_BF16;
+  // (where it has no further chunk it requests its last, or the sequence's last, once more: every request is for tokens that exist)
+  const int from = min(x, chunks - 1);
+  const int64_t first = span.first + (int64_t)from * C;
+  f.k = rows_of(a.k, 2, hk, first);
+  f.q = rows_of(a.q, 2, hk, first);
+  f.gate = rows_of(a.gate, f.gate_bf16 ? 2 : 4, head, first);
+  f.beta = rows_of(a.beta, f.gate_bf16 ? 2 : 4, head, first);
+  f.d_k = a.d_k;
+  f.left = span.len - from * C;
+  f.a_scale = a.flags & EVCONV_DELTA_RAW_GATES ? a.a_scale[head] : 0.0f;
+  f.dt_bias = a.flags & EVCONV_DELTA_RAW_GATES ? a.dt_bias[head] : 0.0f;
+  Ahead<DKP> ahead;
+  request_ahead<DKP, VEC, TRANS, ROLE>(f, ahead);
+#pragma unroll 1
+  for (; left > 0; x += 2) {
+    char* const slot = s_mem + x % 3 * F::kSlot;
+    if (x < chunks) prepare_products<DKP, VEC, TRANS, ROLE>(p, slot, temp, f, f.left, ahead);
+    meet();
+    if (--left == 0) break;
+    const int on = x + 2 < chunks ? 2 : 0;
+    f.k.next(on);
+    f.q.next(on);
+    f.gate.next(on);
+    f.beta.next(on);
+    f.left -= on * C;
+    request_ahead<DKP, VEC, TRANS, ROLE>(f, ahead);
+    if (ROLE == 0 && x < chunks) prepare_inverse<DKP>(slot);
+    meet();
+    --left;
+  }
+}
+
 // Few heads and long sequences: segments of a sequence side by side (p.segs of p.seg_chunks chunks).  What a segment does to the
 // state it starts from is S -> M S + N, so a first launch (TRANS: no outputs) runs the segments from zero, which gives N, and
 // with the columns of the unit matrix as further columns of a state and no values, which gives M (the first
 // segment from the given state; the last one is not needed); delta_join goes through them; the second launch runs
 // every segment from its start.
 template <int DKP, int NC, bool VEC, bool TRANS>
-__global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
+__global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
   typedef FusedShape<DKP, NC> F;
   constexpr int STEPS = F::kSteps, PIECES = 2 * C * (DKP / 8) / (NC * 64);
   extern __shared__ __align__(16) char s_mem[];
@@ -384,51 +439,10 @@ __global__ __launch_bounds__((NC + 2) * 64) void delta_fused(DeltaParams p) {
   span.len = min(span.len, p.seg_chunks * C);
   const int chunks = (span.len + C - 1) / C;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  auto meet = [] {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
   if (wave >= NC) {  // a producer
-    // its chunks are every other one: the first half of chunk x in step x - 2, the second in step x - 1
-    int x = wave - NC, left = chunks + 2;  // steps to come
-    if (x == 1) {
-      meet();
-      --left;
-    }
-    __builtin_amdgcn_s_setprio(2);  // (the others wait for it)
-    Source<VEC> f;
-    f.gate_bf16 = a.gate_dtype == EVCONV_BF16;
-    // (where it has no further chunk it requests its last, or the sequence's last, once more: every request is for tokens that exist)
-    const int from = min(x, chunks - 1);
-    const int64_t first = span.first + (int64_t)from * C;
-    f.k = rows_of(a.k, 2, hk, first);
-    f.q = rows_of(a.q, 2, hk, first);
-    f.gate = rows_of(a.gate, f.gate_bf16 ? 2 : 4, head, first);
-    f.beta = rows_of(a.beta, f.gate_bf16 ? 2 : 4, head, first);
-    f.d_k = a.d_k;
-    f.left = span.len - from * C;
-    f.a_scale = a.flags & EVCONV_DELTA_RAW_GATES ? a.a_scale[head] : 0.0f;
-    f.dt_bias = a.flags & EVCONV_DELTA_RAW_GATES ? a.dt_bias[head] : 0.0f;
-    Ahead<DKP> ahead;
-    request_ahead<DKP, VEC, TRANS>(f, ahead);
-#pragma unroll 1
-    for (; left > 0; x += 2) {
-      char* const slot = s_mem + x % 3 * F::kSlot;
-      if (x < chunks) prepare_products<DKP, VEC, TRANS>(p, slot, f, f.left, ahead);
-      meet();
-      if (--left == 0) break;
-      const int on = x + 2 < chunks ? 2 : 0;
-      f.k.next(on);
-      f.q.next(on);
-      f.gate.next(on);
-      f.beta.next(on);
-      f.left -= on * C;
-      request_ahead<DKP, VEC, TRANS>(f, ahead);
-      if (x < chunks) prepare_inverse<DKP>(slot);
-      meet();
-      --left;
-    }
+    const int which = wave - NC;
+    if (which < 2) produce<DKP, NC, VEC, TRANS, 0>(p, s_mem, span, chunks, which & 1, head, hk);
+    else produce<DKP, NC, VEC, TRANS, 1>(p, s_mem, span, chunks, which & 1, head, hk);
     return;
   }
   // (the two consumers of a SIMD out of step, so that one's vector instructions run beside the other's matrix instructions)
