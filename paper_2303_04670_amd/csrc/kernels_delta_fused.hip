@@ -357,6 +357,18 @@ __device__ __forceinline__ void prepare_inverse(char* slot) {
   }
 }
 
+// The instructions since the last scheduling barrier in turns: a matrix instruction, then `vector` vector instructions, which run
+// beside it.
+template <int MATRIX, int VECTOR>
+__device__ __forceinline__ void beside() {
+#pragma unroll
+  for (int i = 0; i < MATRIX; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // All waves of a workgroup; what they wrote to LDS is there behind it.
 __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -494,11 +506,12 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
   // the contraction's first and last 16 places).  A product with half a unit matrix brings them into the layout of results,
   // and o's values back out of it: two loads and four stores a chunk where lanes' own places would take 16 of two bytes each.
   // (Not where some value is not finite: the zeros would carry it to others.)
-  auto unit = [](int half) __attribute__((always_inline)) {
-    const int lane = own_lane(), n = lane & 15, at = 8 * (lane >> 4) - 16 * half;  // places at .. at + 7
+  auto unit = [](int lane, int half) __attribute__((always_inline)) {
+    const int n = lane & 15, at = (n >> 1) - 4 * (lane >> 4) + 8 * half;  // which pair of this lane's places has the one
+    const unsigned one = n & 1 ? 0x3f800000u : 0x3f80u;
     u32x4 u;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) u[d] = n >> 1 == (at >> 1) + d ? (n & 1 ? 0x3f800000u : 0x3f80u) : 0u;
+    for (int d = 0; d < 4; ++d) u[d] = at == d ? one : 0u;
     return __builtin_bit_cast(b16x8, u);
   };
 #pragma unroll 1
@@ -541,9 +554,20 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
       const int at_k = at_rows<DKP>(place(0, n), g);
 #pragma unroll
       for (int b = 0; b < 4; ++b) R[b] = O[b] = f32x4{0, 0, 0, 0};
+      b16x8 Sp[2][3];
+      auto split_s = [&](int s) __attribute__((always_inline)) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = S[2 * s][i];
+          v[4 + i] = S[2 * s + 1][i];
+        }
+        split8(v, Sp[s & 1]);
+      };
+      split_s(0);
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) {
-        // (operands requested, S split while they come, products: left alone, each read would be waited for by itself)
+        // (operands requested together: left alone, each read would be waited for by itself)
         const char* const at_s = rows + (at_k ^ (s << 6));  // (another piece of the row, by exclusive or; blocks of rows by addition)
         b16x8 k[4][1], q[4][1];
 #pragma unroll
@@ -552,25 +576,18 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
           if (!TRANS) q[b][0] = *(const b16x8*)(at_s + F::kRows + place(b, 0) * DKP * 2);
         }
         __builtin_amdgcn_sched_barrier(0);
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = S[2 * s][i];
-          v[4 + i] = S[2 * s + 1][i];
-        }
-        b16x8 Sp[3];
-        split8(v, Sp);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!TRANS) mfma_parts<1, 4>(O, q, Sp);
-        mfma_parts<2, 4>(R, k, Sp);
-        __builtin_amdgcn_sched_barrier(0);
+        if (s + 1 < STEPS) split_s(s + 1);
+        mfma_parts<2, 4>(R, k, Sp[s & 1]);
+        if (!TRANS) mfma_parts<1, 4>(O, q, Sp[s & 1]);
+        beside<TRANS ? 12 : 20, 2>();
       }
       // ---- R = beta v - beta e^G K S;  e^G Q S   (behind the sequence's end all of them are zero)
+      const b16x8 half[2] = {unit(lane, 0), unit(lane, 1)};
       const bool plain_v = !__ballot((not_finite(value[0]) | not_finite(value[1])) != 0);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int t0 = place(b, 4 * g);  // this lane's tokens: t0 .. t0 + 3
-        f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, value[b >> 1]), unit(b & 1), f32x4{0, 0, 0, 0}, 0, 0, 0);
+        f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, value[b >> 1]), half[b & 1], f32x4{0, 0, 0, 0}, 0, 0, 0);
         if (!plain_v)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -604,33 +621,34 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
       auto apply_t = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) D[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          b16x8 t[2][3];
-          auto read_t = [&](int b0) __attribute__((always_inline)) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int part = 0; part < 3; ++part) t[b][part] = frag((tri(b0 + b, s) * 3 + part) * kFrag);
-            __builtin_amdgcn_sched_barrier(0);
-          };
-          read_t(2 * s);
+        b16x8 Rp[2][3], t[2][3];
+        auto split_r = [&](int s) __attribute__((always_inline)) {
           float v[8];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             v[i] = R[2 * s][i];
             v[4 + i] = R[2 * s + 1][i];
           }
-          b16x8 Rp[3];
-          split8(v, Rp);
-          __builtin_amdgcn_sched_barrier(0);
+          split8(v, Rp[s]);
+        };
+        auto read_t = [&](int b0, int s) __attribute__((always_inline)) {
 #pragma unroll
-          for (int b0 = 2 * s; b0 < 4; b0 += 2) {
-            if (b0 > 2 * s) read_t(b0);
-            mfma_parts<2, 2>(D + b0, t, Rp);
-          }
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int part = 0; part < 3; ++part) t[b][part] = frag((tri(b0 + b, s) * 3 + part) * kFrag);
           __builtin_amdgcn_sched_barrier(0);
-        }
+        };
+        read_t(0, 0);
+        split_r(0);
+        __builtin_amdgcn_sched_barrier(0);
+        split_r(1);
+        mfma_parts<2, 2>(D, t, Rp[0]);
+        beside<12, 4>();
+        read_t(2, 0);
+        mfma_parts<2, 2>(D + 2, t, Rp[0]);
+        read_t(2, 1);
+        mfma_parts<2, 2>(D + 2, t, Rp[1]);
+        __builtin_amdgcn_sched_barrier(0);
       };
       apply_t();
       uint64_t wrong = 0;  // (a value of R that is not finite, or that a bf16 rounds to infinity, is in D too)
@@ -650,58 +668,75 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
       // ---- O += P D;  S = e^G S + K' (w D)
       const float decay = scal[4 * C];
       const int at_t = at_rows<DKP>(8 * g + (n >> 2), n & 3);
+      b16x8 pp[4][2], kt[STEPS][1], Dp[2], Dw[3];
+      // tokens 32 s + 8 g .. + 7 of the channels place(b, .): two transposing reads of four tokens
+      auto read_k = [&](int s, int b0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        b16x8 pp[4][2], kt[STEPS][1];
-        // tokens 32 s + 8 g .. + 7 of the channels place(b, .): two transposing reads of four tokens
-        auto read_k = [&](int b0) __attribute__((always_inline)) {
-#pragma unroll
-          for (int b = 0; b < STEPS; ++b) {
-            const char* const q = rows + (at_t ^ (((b0 + b) >> 1) << 6)) + 32 * s * DKP * 2 + ((b0 + b) & 1) * 8;
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)q);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * DKP * 2));
-            kt[b][0] = __builtin_bit_cast(b16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        };
+        for (int b = 0; b < STEPS; ++b) {
+          const char* const q = rows + (at_t ^ (((b0 + b) >> 1) << 6)) + 32 * s * DKP * 2 + ((b0 + b) & 1) * 8;
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef short s16x8 __attribute__((ext_vector_type(8)));
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)q);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q + 4 * DKP * 2));
+          kt[b][0] = __builtin_bit_cast(b16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      };
+      auto read_p = [&](int s) __attribute__((always_inline)) {
         if (!TRANS)
 #pragma unroll
-        for (int b = 2 * s; b < 4; ++b)
+          for (int b = 2 * s; b < 4; ++b)
 #pragma unroll
-          for (int part = 0; part < 2; ++part) pp[b][part] = frag(F::kOffP + (tri(b, s) * 2 + part) * kFrag);
-        __builtin_amdgcn_sched_barrier(0);
+            for (int part = 0; part < 2; ++part) pp[b][part] = frag(F::kOffP + (tri(b, s) * 2 + part) * kFrag);
+      };
+      auto split_d = [&](int s) __attribute__((always_inline)) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[i] = D[2 * s][i];
           v[4 + i] = D[2 * s + 1][i];
         }
-        b16x8 Dp[2];
         split8(v, Dp);
-        read_k(0);
-        if (TRANS) {
-        } else if (s == 0) mfma_parts<1, 4>(O, pp, Dp);
-        else mfma_parts<1, 2>(O + 2, pp + 2, Dp);
-        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto split_w = [&](int s) __attribute__((always_inline)) {
         const f32x4 w0 = *(const f32x4*)(scal + 3 * C + place(2 * s, 4 * g)), w1 = *(const f32x4*)(scal + 3 * C + place(2 * s + 1, 4 * g));
+        float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          v[i] *= w0[i];
-          v[4 + i] *= w1[i];
+          v[i] = D[2 * s][i] * w0[i];
+          v[4 + i] = D[2 * s + 1][i] * w1[i];
         }
-        b16x8 Dw[3];
         split8(v, Dw);
-        __builtin_amdgcn_sched_barrier(0);
-        mfma_parts<2, STEPS>(S, kt, Dw);
-        __builtin_amdgcn_sched_barrier(0);
-        read_k(STEPS);
-        mfma_parts<2, STEPS>(S + STEPS, kt, Dw);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      };
+      // (vector instructions in turns with matrix instructions that do not need them)
+      read_p(0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!TRANS) split_d(0);
+      __builtin_amdgcn_sched_barrier(0);
+      split_w(0);
+#pragma unroll
+      for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
+      if (!TRANS) mfma_parts<1, 4>(O, pp, Dp);
+      beside<12, 6>();
+      read_k(0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!TRANS) split_d(1);
+      mfma_parts<2, STEPS>(S, kt, Dw);
+      beside<3 * STEPS, 3>();
+      read_k(0, STEPS);
+      read_p(1);
+      __builtin_amdgcn_sched_barrier(0);
+      mfma_parts<2, STEPS>(S + STEPS, kt, Dw);
+      if (!TRANS) mfma_parts<1, 2>(O + 2, pp + 2, Dp);
+      __builtin_amdgcn_sched_barrier(0);
+      read_k(1, 0);
+      split_w(1);
+      __builtin_amdgcn_sched_barrier(0);
+      mfma_parts<2, STEPS>(S, kt, Dw);
+      __builtin_amdgcn_sched_barrier(0);
+      read_k(1, STEPS);
+      __builtin_amdgcn_sched_barrier(0);
+      mfma_parts<2, STEPS>(S + STEPS, kt, Dw);
+      __builtin_amdgcn_sched_barrier(0);
       if (__ballot(first_bad < C)) {
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -717,6 +752,7 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
     if (!TRANS && now) {
       const int lane = own_lane(), n = lane & 15, g = lane >> 4;
       // ---- o, rounded; transposed by unit matrices (as left operand, so that a lane gets a token's neighbouring columns)
+      const b16x8 part_of[2] = {unit(lane, 0), unit(lane, 1)};
 #pragma unroll
       for (int pair = 0; pair < 2; ++pair) {
         u32x4 u;
@@ -737,7 +773,7 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
         const int own = strip * 16 + 4 * g;  // this lane's columns: own .. own + 3
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const f32x4 w = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, u), unit(half), f32x4{0, 0, 0, 0}, 0, 0, 0);
+          const f32x4 w = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, u), part_of[half], f32x4{0, 0, 0, 0}, 0, 0, 0);
           const int t = 32 * pair + 16 * half;  // + n: this lane's token
           const char* const q = o_rows.at + t * o_rows.step;
           const unsigned at = (unsigned)(n * o_rows.step + own * 2);
