@@ -19,6 +19,8 @@
 // rows, applied to the sums), everything else that reaches the state as three bf16 parts, which hold
 // 24 bits; outputs of bf16 calls are summed from two parts.  G is summed in 64 bits: the difference of two
 // sums over a chunk would lose the bits that its exponential needs.
+#include <type_traits>
+
 #include "delta_device.h"
 
 namespace evk {
@@ -29,7 +31,8 @@ namespace {
 // o needs S'q after the update, which is e^g (S'q before it) + (k q) d: one pass over the strip gives both
 // products, one reduction over the groups sums them.
 // Bound by the state's bytes, read once and written once.
-template <bool BF16, int ROWS, bool VEC, bool SVEC>
+// ONE: every sequence has one token; otherwise the next token is on its way while one is applied.
+template <bool BF16, int ROWS, bool VEC, bool ONE>
 __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
   const evconv_delta_args& a = p.a;
   const int lane = threadIdx.x & 63;
@@ -50,7 +53,7 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
     S[i] = f32x4{0, 0, 0, 0};
     if (at >= 0 && a.state_in && row0 + i < a.d_k) {
       const float* q = a.state_in + at + (int64_t)(row0 + i) * a.d_v + col;
-      if (SVEC) {
+      if (VEC) {
         if (col < a.d_v) S[i] = *(const f32x4*)q;
       } else {
 #pragma unroll
@@ -60,13 +63,27 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
     }
   }
   const int hk = head / p.share;
-  for (int t = 0; t < s.len; ++t) {
+  struct Token {
+    float k[ROWS], q[ROWS], v[4], gate, beta;
+  };
+  const bool raw = a.flags & EVCONV_DELTA_RAW_GATES, gate_bf16 = a.gate_dtype == EVCONV_BF16;
+  const float a_scale = raw ? a.a_scale[head] : 0.0f, dt_bias = raw ? a.dt_bias[head] : 0.0f;
+  auto load = [&](int t, Token& x) __attribute__((always_inline)) {
     const int64_t token = s.first + t;
-    float k[ROWS], q[ROWS], v[4];
-    load_run<BF16, ROWS, VEC>(a.k.data, token * a.k.token_stride + hk * a.k.head_stride + row0, a.d_k - row0, k);
-    load_run<BF16, ROWS, VEC>(a.q.data, token * a.q.token_stride + hk * a.q.head_stride + row0, a.d_k - row0, q);
-    load_run<BF16, 4, false>(a.v.data, token * a.v.token_stride + head * a.v.head_stride + col, a.d_v - col, v);
-    const Gates gate = gates_of(p, token, head);
+    load_run<BF16, ROWS, VEC>(a.k.data, token * a.k.token_stride + hk * a.k.head_stride + row0, a.d_k - row0, x.k);
+    load_run<BF16, ROWS, VEC>(a.q.data, token * a.q.token_stride + hk * a.q.head_stride + row0, a.d_k - row0, x.q);
+    load_run<BF16, 4, false>(a.v.data, token * a.v.token_stride + head * a.v.head_stride + col, a.d_v - col, x.v);
+    x.gate = load_any(a.gate.data, token * a.gate.token_stride + head * a.gate.head_stride, gate_bf16);
+    x.beta = load_any(a.beta.data, token * a.beta.token_stride + head * a.beta.head_stride, gate_bf16);
+  };
+  Token next;
+  if (s.len > 0) load(0, next);
+  for (int t = 0; t < (ONE ? min(s.len, 1) : s.len); ++t) {
+    const int64_t token = s.first + t;
+    const Token now = next;
+    if (!ONE && t + 1 < s.len) load(t + 1, next);
+    const float(&k)[ROWS] = now.k, (&q)[ROWS] = now.q, (&v)[4] = now.v;
+    const Gates gate = gates_from(raw, now.gate, now.beta, a_scale, dt_bias);
     const float decay = expf(gate.g);
     float sum[11];  // S'k, S'q (four columns each), kq, kk, qq
 #pragma unroll
@@ -111,7 +128,7 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
     for (int i = 0; i < ROWS; ++i)
       if (row0 + i < a.d_k) {
         float* q = a.state_out + at + (int64_t)(row0 + i) * a.d_v + col;
-        if (SVEC) {
+        if (VEC) {
           if (col < a.d_v) *(f32x4*)q = S[i];
         } else {
 #pragma unroll
@@ -170,53 +187,40 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
     s_g[lane] = sum;
     s_beta[lane] = gate.beta;
   }
-  {
-    const int t = tid >> 2, part = tid & 3;  // four threads to a token
-    float rk = 1.0f, rq = 1.0f;
-    if (a.flags & EVCONV_DELTA_NORMALIZE) {
-      float kk = 0.0f, qq = 0.0f;
-      if (t < count)
-        for (int c = part * 8; c < a.d_k; c += 32) {
-          float k[8], q[8];
-          load_run<!F32, 8, VEC>(a.k.data, (token0 + t) * a.k.token_stride + hk * a.k.head_stride + c, a.d_k - c, k);
-          load_run<!F32, 8, VEC>(a.q.data, (token0 + t) * a.q.token_stride + hk * a.q.head_stride + c, a.d_k - c, q);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            kk = fmaf(k[j], k[j], kk);
-            qq = fmaf(q[j], q[j], qq);
-          }
-        }
-      kk += __shfl_xor(kk, 1);
-      kk += __shfl_xor(kk, 2);
-      qq += __shfl_xor(qq, 1);
-      qq += __shfl_xor(qq, 2);
-      rk = 1.0f / sqrtf(kk + 1e-6f);
-      rq = 1.0f / sqrtf(qq + 1e-6f);
-    }
-    if (part == 0) {
-      s_rk[t] = rk;
-      s_rq[t] = rq * a.scale;
-    }
-  }
   for (int i = tid; i < C * C; i += 256) s_t[i / C][i % C] = 0.0f;
   if (tid == 0) s_bad = C;
 
-  // ---- K K' and Q K', a wave 16 tokens' rows of them
-  f32x4 kk[4], qk[4];
+  // ---- K K' and Q K', a wave 16 tokens' rows of them, and the diagonal of Q Q'
+  f32x4 kk[4], qk[4], qq = {0, 0, 0, 0};
 #pragma unroll
   for (int b = 0; b < 4; ++b) kk[b] = qk[b] = f32x4{0, 0, 0, 0};
-  for (int c = 0; c < p.dkp; c += 32) {
-    b16x8 ka[PI], qa[PI], kb[PI];
+  {
     const int row = wave * 16 + m;
-    load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + row, row < count, c + 8 * g, ka);
-    load_parts<F32, VEC>(a.q, hk, a.d_k, token0 + row, row < count, c + 8 * g, qa);
+    for (int c = 0; c < p.dkp; c += 32) {
+      b16x8 ka[PI], qa[PI], kb[PI];
+      load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + row, row < count, c + 8 * g, ka);
+      load_parts<F32, VEC>(a.q, hk, a.d_k, token0 + row, row < count, c + 8 * g, qa);
+      mfma_parts<2>(qq, qa, qa);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      if (b > wave) break;
-      const int other = b * 16 + m;
-      load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + other, other < count, c + 8 * g, kb);
-      mfma_parts<2>(kk[b], ka, kb);
-      mfma_parts<2>(qk[b], qa, kb);
+      for (int b = 0; b < 4; ++b) {
+        if (b > wave) break;
+        const int other = b * 16 + m;
+        load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + other, other < count, c + 8 * g, kb);
+        mfma_parts<2>(kk[b], ka, kb);
+        mfma_parts<2>(qk[b], qa, kb);
+      }
+    }
+    // norms: the diagonals, which lanes with m / 4 == g hold
+    f32x4 own = kk[0];
+#pragma unroll
+    for (int b = 1; b < 4; ++b)
+      if (b == wave) own = kk[b];
+    const float u = m & 2 ? (m & 1 ? own[3] : own[2]) : (m & 1 ? own[1] : own[0]);
+    const float v = m & 2 ? (m & 1 ? qq[3] : qq[2]) : (m & 1 ? qq[1] : qq[0]);
+    if (m >> 2 == g) {
+      const bool normalize = a.flags & EVCONV_DELTA_NORMALIZE;
+      s_rk[row] = normalize ? 1.0f / sqrtf(u + 1e-6f) : 1.0f;
+      s_rq[row] = normalize ? a.scale / sqrtf(v + 1e-6f) : a.scale;
     }
   }
   __syncthreads();
@@ -342,163 +346,250 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
 }
 
 // ---- chunks: through a sequence ----------------------------------------------------------------------
-// A wave: one sequence, one value head, 16 columns of the state, which stay in its registers.
+// A workgroup: one sequence, one value head, up to eight (four) strips of 16 columns of the state, a wave each, which stay in its
+// registers.  The waves share the operands: a chunk's are K, Q, (T, P) and K' in turn, each brought into one of three
+// buffers in LDS two stages before it is used (K, Q and K' in halves where they are larger than a buffer).
 template <bool F32, int DKP>
-__global__ __launch_bounds__(64) void delta_chain(DeltaParams p) {
-  constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32, ORD = F32 ? 2 : 1;
+struct ChainShape {
+  static constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32;
+  static constexpr int kRows = 4 * STEPS * PI * kFrag;            // bytes of K; Q and K' alike
+  static constexpr int kHalves = kRows > 48 * 1024 ? 2 : 1;
+  static constexpr int kWaves = DKP == 256 ? 4 : 8;               // (256 rows of a strip do not fit half of a SIMD's registers)
+  static constexpr int kTp = kTri * kFrag * (3 + PO);
+  static constexpr int kBuffer = kRows / kHalves > kTp ? kRows / kHalves : kTp;
+  static constexpr int kStages = 3 * kHalves + 1;                 // of a chunk
+  static constexpr int kScalars = kDeltaScalars * 4;
+  static constexpr int kBytes = 3 * kBuffer + 2 * kScalars;
+  static_assert(kBytes <= 160 * 1024 && kScalars == 2 * kFrag, "LDS");
+  // pieces of 1 KB of a stage
+  static constexpr int pieces(int stage) { return (stage == 2 * kHalves ? kTp : kRows / kHalves) / kFrag; }
+};
+
+template <bool F32, int DKP>
+__global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParams p) {
+  typedef ChainShape<F32, DKP> H;
+  constexpr int PI = H::PI, PO = H::PO, STEPS = H::STEPS, ORD = F32 ? 2 : 1, HALVES = H::kHalves, BLOCKS = 4 / HALVES, WAVES = H::kWaves;
+  extern __shared__ __align__(16) char s_mem[];
   const evconv_delta_args& a = p.a;
-  const int strips = (a.d_v + 15) / 16;
-  // strips of a head on one XCD (workgroups go round the eight of them): they read the same operands
-  const int xcd = blockIdx.x & 7, r = blockIdx.x >> 3;
-  const int strip = r % strips;
-  const int64_t pair = (int64_t)(r / strips) * 8 + xcd;
-  if (pair >= (int64_t)a.n_seq * a.heads_v) return;
+  const int strips = (a.d_v + 15) / 16, groups = (strips + WAVES - 1) / WAVES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int strip = blockIdx.x % groups * WAVES + wave;
+  const int64_t pair = blockIdx.x / groups;
   const int seq = (int)(pair / a.heads_v), head = (int)(pair % a.heads_v), hk = head / p.share;
   const Span span = span_of(p, seq);
   if (span.len <= p.short_len) return;
-  const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
   const int col = strip * 16 + n;
-  const bool in = col < a.d_v;
+  const bool works = strip < strips, in = col < a.d_v;
   const int64_t at = state_at(p, seq, head);
   f32x4 S[2 * STEPS];
 #pragma unroll
-  for (int b = 0; b < 2 * STEPS; ++b)
+  for (int b = 0; b < 2 * STEPS; ++b) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = place(b, 4 * g + i);
       S[b][i] = at >= 0 && a.state_in && row < a.d_k && in ? a.state_in[at + (int64_t)row * a.d_v + col] : 0.0f;
     }
-  const size_t one = (size_t)4 * STEPS * PI * kFrag;
+    asm volatile("" : "+v"(S[b]));  // (waited for here, not in every turn of the loop)
+  }
   const int chunks = (span.len + C - 1) / C;
-  const int slot0 = first_slot(span, seq);
+  const size_t slot0 = first_slot(span, seq);
+  // a chunk's operands in memory
+  auto rows_at = [&](int chunk) { return p.frag_k + ((slot0 + chunk) * a.heads_k + hk) * (size_t)(3 * H::kRows); };
+  auto tp_at = [&](int chunk) { return p.frag_t + ((slot0 + chunk) * a.heads_v + head) * (size_t)H::kTp; };
+  auto copy = [&](const char* from, char* to) __attribute__((always_inline)) {  // 1 KB, straight into LDS
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + lane * 16), (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  };
+  char* const s_scal = s_mem + 3 * H::kBuffer;
+  // Stage `stage` of a chunk into buffer `buffer`
+  auto request = [&](int chunk, int stage, int buffer) __attribute__((always_inline)) {
+    if (chunk >= chunks) return;
+    // stages: K (halves), Q (halves), T and P, K' (halves)
+    const bool tp = stage == 2 * HALVES;
+    const char* const from = tp ? tp_at(chunk) : rows_at(chunk) + (size_t)(stage < 2 * HALVES ? stage : stage - 1) * (H::kRows / HALVES);
+    const int pieces = tp ? H::pieces(2 * HALVES) : H::pieces(0);
+    char* const to = s_mem + buffer * H::kBuffer;
+#pragma unroll 1
+    for (int i = wave; i < pieces; i += WAVES) copy(from + (size_t)i * kFrag, to + i * kFrag);
+    if (stage == 0 && wave < 2) copy((const char*)(p.scal + ((slot0 + chunk) * a.heads_v + head) * kDeltaScalars) + wave * kFrag, s_scal + (chunk & 1) * H::kScalars + wave * kFrag);
+  };
+  int buffer = 0;
+  request(0, 0, 0);
+  request(0, 1, 1);
+  f32x4 R[4], O[4], D[4];
+  float v[16];
+  int first_bad = C;
   for (int chunk = 0; chunk < chunks; ++chunk) {
-    const int64_t token0 = span.first + chunk * C;
+    const int64_t token0 = span.first + (int64_t)chunk * C;
     const int count = min(span.len - chunk * C, C);
-    const size_t slot = slot0 + chunk;
-    const char* const at_k = p.frag_k + (slot * a.heads_k + hk) * 3 * one + lane * 16;
-    const char* const at_t = p.frag_t + (slot * a.heads_v + head) * (kTri * kFrag * (3 + PO)) + lane * 16;
-    const float* const scal = p.scal + (slot * a.heads_v + head) * kDeltaScalars;
-    auto frag = [](const char* q, int i) __attribute__((always_inline)) { return *(const b16x8*)(q + (size_t)i * kFrag); };
-
-    // S as right operand
-    b16x8 Sp[STEPS][3];
+    const float* const scal = (const float*)(s_scal + (chunk & 1) * H::kScalars);
+    if (works) {
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      float v[8];
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = S[2 * s][i];
-        v[4 + i] = S[2 * s + 1][i];
-      }
-      split8(v, Sp[s]);
-    }
-    // R = beta v - beta e^G K S, and e^G Q S
-    f32x4 R[4], O[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      R[b] = O[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        b16x8 k[PI], q[PI];
-#pragma unroll
-        for (int part = 0; part < PI; ++part) {
-          k[part] = frag(at_k, (b * STEPS + s) * PI + part);
-          q[part] = frag(at_k + one, (b * STEPS + s) * PI + part);
+        for (int i = 0; i < 4; ++i) {
+          const int t = place(b, 4 * g) + i;
+          v[b * 4 + i] = t < count && in ? load_one<!F32>(a.v.data, (token0 + t) * a.v.token_stride + head * a.v.head_stride + col) : 0.0f;
         }
-        mfma_parts<2>(R[b], k, Sp[s]);
-        mfma_parts<ORD>(O[b], q, Sp[s]);
-      }
     }
-    unsigned bad = 0;
-    f32x4 w[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int t0 = place(b, 4 * g);  // this lane's tokens: t0 .. t0 + 3
-      const f32x4 beta = *(const f32x4*)(scal + t0), kf = *(const f32x4*)(scal + C + t0), qf = *(const f32x4*)(scal + 2 * C + t0);
-      w[b] = *(const f32x4*)(scal + 3 * C + t0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool live = t0 + i < count && in;
-        const float v = live ? load_one<!F32>(a.v.data, (token0 + t0 + i) * a.v.token_stride + head * a.v.head_stride + col) : 0.0f;
-        R[b][i] = t0 + i < count ? beta[i] * v - kf[i] * R[b][i] : 0.0f;
-        O[b][i] *= qf[i];
-        if (!(fabsf(R[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
+    auto run = [&](auto number) __attribute__((always_inline)) {
+      constexpr int stage = decltype(number)::value;
+      // everything that this stage reads has arrived; the stage before it is done with its buffer
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      {
+        constexpr int next = stage + 2;
+        const int to = buffer >= 1 ? buffer - 1 : 2;  // (two further on, of three)
+        if (next < H::kStages) request(chunk, next, to);
+        else request(chunk + 1, next - H::kStages, to);
       }
+      const char* const q = s_mem + buffer * H::kBuffer + lane * 16;
+      buffer = buffer == 2 ? 0 : buffer + 1;
+      if (!works) return;
+      auto frag = [&](int i) __attribute__((always_inline)) { return *(const b16x8*)(q + (size_t)i * kFrag); };
+      if constexpr (stage < 2 * HALVES) {  // K S, then Q S
+        constexpr bool keys = stage < HALVES;
+        constexpr int b0 = stage % HALVES * BLOCKS;
+        f32x4 acc[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) acc[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          b16x8 k[BLOCKS][PI], Sp[3];
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int part = 0; part < PI; ++part) k[b][part] = frag((b * STEPS + s) * PI + part);
+          __builtin_amdgcn_sched_barrier(0);
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = S[2 * s][i];
+            x[4 + i] = S[2 * s + 1][i];
+          }
+          split8(x, Sp);
+          if (keys) mfma_parts<2, BLOCKS>(acc, k, Sp);
+          else mfma_parts<ORD, BLOCKS>(acc, k, Sp);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+          if (keys) R[b0 + b] = acc[b];
+          else O[b0 + b] = acc[b];
+        }
+      } else if constexpr (stage == 2 * HALVES) {
+        // R = beta v - beta e^G K S;  e^G Q S;  D = T R;  O += P D
+        unsigned bad = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int t0 = place(b, 4 * g);  // this lane's tokens: t0 .. t0 + 3
+          const f32x4 beta = *(const f32x4*)(scal + t0), kf = *(const f32x4*)(scal + C + t0), qf = *(const f32x4*)(scal + 2 * C + t0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            R[b][i] = t0 + i < count ? beta[i] * v[b * 4 + i] - kf[i] * R[b][i] : 0.0f;
+            O[b][i] *= qf[i];
+            if (!(fabsf(R[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
+          }
+        }
+        first_bad = C;
+        if (__ballot(bad != 0)) cut_columns(R, bad, first_bad, g);
+        b16x8 Rp[2][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = R[2 * s][i];
+            x[4 + i] = R[2 * s + 1][i];
+          }
+          split8(x, Rp[s]);
+        }
+        bad = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          D[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < 1 + (b >> 1); ++s) {
+            b16x8 t[3];
+#pragma unroll
+            for (int part = 0; part < 3; ++part) t[part] = frag(tri(b, s) * 3 + part);
+            mfma_parts<2>(D[b], t, Rp[s]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(fabsf(D[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (__ballot(bad != 0 || first_bad < C)) cut_columns(D, bad, first_bad, g);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = D[2 * s][i];
+            x[4 + i] = D[2 * s + 1][i];
+          }
+          b16x8 Dp[PO];
+          split8(x, Dp);
+#pragma unroll
+          for (int b = 2 * s; b < 4; ++b) {
+            b16x8 pp[PO];
+#pragma unroll
+            for (int part = 0; part < PO; ++part) pp[part] = frag(kTri * 3 + tri(b, s) * PO + part);
+            mfma_parts<ORD>(O[b], pp, Dp);
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int t = place(b, 4 * g) + i;
+            if (t < count && in)
+              store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, t < first_bad ? O[b][i] : NAN);
+          }
+        const float decay = scal[4 * C];
+#pragma unroll
+        for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) D[b] *= *(const f32x4*)(scal + 3 * C + place(b, 4 * g));  // w D from here on
+      } else {  // S = e^G S + K' (w D)
+        constexpr int b0 = (stage - 2 * HALVES - 1) * (2 * STEPS / HALVES);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = D[2 * s][i];
+            x[4 + i] = D[2 * s + 1][i];
+          }
+          b16x8 Dw[3];
+          split8(x, Dw);
+#pragma unroll
+          for (int b = 0; b < 2 * STEPS / HALVES; b += 4) {
+            b16x8 kt[4][PI];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int part = 0; part < PI; ++part) kt[i][part] = frag(((b + i) * 2 + s) * PI + part);
+            __builtin_amdgcn_sched_barrier(0);
+            mfma_parts<2, 4>(&S[b0 + b], kt, Dw);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        if (stage == H::kStages - 1 && first_bad < C)
+#pragma unroll
+          for (int b = 0; b < 2 * STEPS; ++b) S[b] = f32x4{NAN, NAN, NAN, NAN};
+      }
+    };
+    run(std::integral_constant<int, 0>());
+    run(std::integral_constant<int, 1>());
+    run(std::integral_constant<int, 2>());
+    run(std::integral_constant<int, 3>());
+    if constexpr (HALVES == 2) {
+      run(std::integral_constant<int, 4>());
+      run(std::integral_constant<int, 5>());
+      run(std::integral_constant<int, 6>());
     }
-    int first_bad = C;
-    if (__ballot(bad != 0)) cut_columns(R, bad, first_bad, g);
-    // D = T R
-    b16x8 Rp[2][3];
-    f32x4 D[4];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = R[2 * s][i];
-        v[4 + i] = R[2 * s + 1][i];
-      }
-      split8(v, Rp[s]);
-    }
-    bad = 0;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      D[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < 1 + (b >> 1); ++s) {
-        b16x8 t[3];
-#pragma unroll
-        for (int part = 0; part < 3; ++part) t[part] = frag(at_t, tri(b, s) * 3 + part);
-        mfma_parts<2>(D[b], t, Rp[s]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (!(fabsf(D[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
-    }
-    if (__ballot(bad != 0 || first_bad < C)) cut_columns(D, bad, first_bad, g);
-    // O += P D;  S = e^G S + K' (w D)
-    const float decay = scal[4 * C];
-#pragma unroll
-    for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float v[8], vw[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = D[2 * s][i];
-        v[4 + i] = D[2 * s + 1][i];
-        vw[i] = v[i] * w[2 * s][i];
-        vw[4 + i] = v[4 + i] * w[2 * s + 1][i];
-      }
-      b16x8 Dp[PO], Dw[3];
-      split8(v, Dp);
-      split8(vw, Dw);
-#pragma unroll
-      for (int b = 2 * s; b < 4; ++b) {
-        b16x8 pp[PO];
-#pragma unroll
-        for (int part = 0; part < PO; ++part) pp[part] = frag(at_t + kTri * 3 * kFrag, tri(b, s) * PO + part);
-        mfma_parts<ORD>(O[b], pp, Dp);
-      }
-#pragma unroll
-      for (int b = 0; b < 2 * STEPS; ++b) {
-        b16x8 kt[PI];
-#pragma unroll
-        for (int part = 0; part < PI; ++part) kt[part] = frag(at_k + 2 * one, (b * 2 + s) * PI + part);
-        mfma_parts<2>(S[b], kt, Dw);
-      }
-    }
-    if (first_bad < C)
-#pragma unroll
-      for (int b = 0; b < 2 * STEPS; ++b) S[b] = f32x4{NAN, NAN, NAN, NAN};
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = place(b, 4 * g) + i;
-        if (t < count && in)
-          store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, t < first_bad ? O[b][i] : NAN);
-      }
   }
   if (at >= 0 && a.state_out && in)
 #pragma unroll
@@ -511,21 +602,27 @@ __global__ __launch_bounds__(64) void delta_chain(DeltaParams p) {
 }
 
 template <bool BF16, int ROWS>
-void steps_rows(const DeltaParams& p, bool svec, unsigned grid, hipStream_t s) {
-  if (p.vec && svec) delta_step<BF16, ROWS, true, true><<<grid, 256, 0, s>>>(p);
-  else delta_step<BF16, ROWS, false, false><<<grid, 256, 0, s>>>(p);
+void steps_rows(const DeltaParams& p, bool vec, unsigned grid, hipStream_t s) {
+  if (p.len == 1) {
+    if (vec) delta_step<BF16, ROWS, true, true><<<grid, 256, 0, s>>>(p);
+    else delta_step<BF16, ROWS, false, true><<<grid, 256, 0, s>>>(p);
+  } else {
+    if (vec) delta_step<BF16, ROWS, true, false><<<grid, 256, 0, s>>>(p);
+    else delta_step<BF16, ROWS, false, false><<<grid, 256, 0, s>>>(p);
+  }
 }
 template <bool BF16>
-void steps_type(const DeltaParams& p, bool svec, unsigned grid, hipStream_t s) {
-  if (p.a.d_k <= 32) steps_rows<BF16, 4>(p, svec, grid, s);
-  else if (p.a.d_k <= 64) steps_rows<BF16, 8>(p, svec, grid, s);
-  else if (p.a.d_k <= 128) steps_rows<BF16, 16>(p, svec, grid, s);
-  else steps_rows<BF16, 32>(p, svec, grid, s);
+void steps_type(const DeltaParams& p, bool vec, unsigned grid, hipStream_t s) {
+  if (p.a.d_k <= 32) steps_rows<BF16, 4>(p, vec, grid, s);
+  else if (p.a.d_k <= 64) steps_rows<BF16, 8>(p, vec, grid, s);
+  else if (p.a.d_k <= 128) steps_rows<BF16, 16>(p, vec, grid, s);
+  else steps_rows<BF16, 32>(p, vec, grid, s);
 }
 template <bool F32, int DKP>
 void chain(const DeltaParams& p, hipStream_t s) {
   const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, strips = (p.a.d_v + 15) / 16;
-  delta_chain<F32, DKP><<<(unsigned)((pairs + 7) / 8 * 8 * strips), 64, 0, s>>>(p);
+  constexpr int waves = ChainShape<F32, DKP>::kWaves;
+  delta_chain<F32, DKP><<<(unsigned)(pairs * ((strips + waves - 1) / waves)), waves * 64, ChainShape<F32, DKP>::kBytes, s>>>(p);
 }
 template <bool F32>
 void chunks_type(const DeltaParams& p, hipStream_t s) {
@@ -544,11 +641,11 @@ size_t delta_frag_k_bytes(int dtype, int dkp) { return (size_t)3 * 4 * (dkp / 32
 size_t delta_frag_t_bytes(int dtype) { return (size_t)kTri * kFrag * (3 + parts_out(dtype == EVCONV_F32)); }
 
 void launch_delta_steps(const DeltaParams& p, hipStream_t s) {
-  const bool svec = p.a.d_v % 4 == 0 && ((uintptr_t)p.a.state_in | (uintptr_t)p.a.state_out) % 16 == 0;
+  const bool vec = p.vec && p.a.d_v % 4 == 0 && ((uintptr_t)p.a.state_in | (uintptr_t)p.a.state_out) % 16 == 0;
   const int64_t waves = (int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 31) / 32);
   const unsigned grid = (unsigned)((waves + 3) / 4);
-  if (p.a.dtype == EVCONV_BF16) steps_type<true>(p, svec, grid, s);
-  else steps_type<false>(p, svec, grid, s);
+  if (p.a.dtype == EVCONV_BF16) steps_type<true>(p, vec, grid, s);
+  else steps_type<false>(p, vec, grid, s);
 }
 
 void launch_delta_chunks(const DeltaParams& p, hipStream_t s) {

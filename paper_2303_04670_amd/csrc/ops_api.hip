@@ -31,8 +31,10 @@ bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 bool wide(int dtype, const void* p, int64_t stride) { return aligned(p, 16) && stride * (int64_t)type_size(dtype) % 16 == 0; }
 bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token_stride) && wide(dtype, h.data, h.head_stride); }
 
-// Sequences of up to this many tokens go token by token.
-constexpr int kShort = 16;
+// Sequences of up to this many tokens go token by token (of calls that the one-launch kernel takes otherwise, of others).  us for
+// 16 sequences of 4 heads of 64 x 64, 64 of 16 of 128 x 128, token by token / in chunks: bf16, 6 tokens 18 / 14, 59 / 76, 8
+// tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 137, 12 tokens 26 / 27, 80 / 136.
+constexpr int kShortFused = 6, kShort = 12;
 
 struct DeltaPlan {
   DeltaParams p;
@@ -61,15 +63,16 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.a = *a;
   d.p.share = a->heads_v / a->heads_k;
   d.p.len = a->seq_offsets ? -1 : (int)(a->n_tokens / a->n_seq);
-  d.p.short_len = kShort;
   d.p.slots_total = (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
   d.p.dkp = a->d_k <= 64 ? 64 : a->d_k <= 128 ? 128 : 256;
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
   d.p.vec_v = a->d_v % 8 == 0 && wide(a->dtype, a->v) && aligned(a->o, 8) && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0;
-  d.steps = d.p.len < 0 || d.p.len <= kShort;
-  d.chunks = d.p.len < 0 ? a->n_tokens > kShort : !d.steps;
+  const bool one_launch = delta_fused_supported(d.p);
+  d.p.short_len = one_launch ? kShortFused : kShort;
+  d.steps = d.p.len < 0 || d.p.len <= d.p.short_len;
+  d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
   d.off_t = d.off_scal = d.bytes = 0;
-  d.fused = d.chunks && delta_fused_supported(d.p);
+  d.fused = d.chunks && one_launch;
   if (d.chunks) {
     const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8 * ((a->d_v + 15) / 16);
     if (pairs >= 1ll << 31 || (int64_t)d.p.slots_total * a->heads_v >= 1ll << 31)

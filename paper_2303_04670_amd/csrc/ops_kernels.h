@@ -34,7 +34,7 @@ struct DeltaParams {
 // Sizes in the workspace, per chunk slot and head.
 size_t delta_frag_k_bytes(int dtype, int dkp);
 size_t delta_frag_t_bytes(int dtype);
-constexpr int kDeltaScalars = 4 * kDeltaChunk + 64;
+constexpr int kDeltaScalars = 512;  // four factors of every token, the decay; up to whole 1 KB
 void launch_delta_steps(const DeltaParams& p, hipStream_t s);
 void launch_delta_chunks(const DeltaParams& p, hipStream_t s);
 // chunks in one launch; workspace for segments only
