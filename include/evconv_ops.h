@@ -96,9 +96,9 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
  *   t = t * act(gate)                              act: 1, sigmoid(z) or z * sigmoid(z)
  *   x' = x + res_scale * t                         (x NULL: x' = res_scale * t;  branch NULL: x' = x)
  *   h = norm(x') * pre_weight + pre_bias           over the whole row, if pre_norm is set (else h = x')
- *   q = rint(h * (127 / m)), q_scale = m / 127     m = max |h| of the row; a row of zeros has q = 0 and
- *                                                  scale 0, one with a value that is not finite q = 0 and scale NaN;
- *                                                  where 127 / m overflows, q = 0
+ *   q = rint(h * (127 * (1 / m))), q_scale = m / 127   each operation rounded to fp32; m = max |h| of the row;
+ *                                                  a row of zeros has q = 0 and scale 0, one with a value that is
+ *                                                  not finite q = 0 and scale NaN; where 1 / m overflows, q = 0
  * norm: EVCONV_NORM_RMS x / sqrt(mean(x^2) + eps), EVCONV_NORM_LAYER (x - mean) / sqrt(variance + eps).
  * Every operand that is NULL is left out of its formula; outputs that are NULL are not written.  x_out may be x. */
 typedef enum { EVCONV_NORM_RMS = 0, EVCONV_NORM_LAYER = 1 } evconv_norm;

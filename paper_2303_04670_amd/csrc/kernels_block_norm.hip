@@ -218,7 +218,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
   big = row_max<T>(big, s_part);
   const float m = __uint_as_float(big);
   const bool finite = big < 0x7f800000u;
-  float inverse = finite && big ? 127.0f / m : 0.0f;
+  float inverse = finite && big ? 127.0f * (1.0f / m) : 0.0f;
   if (!(inverse < INFINITY)) inverse = 0.0f;
   int8_t* const q = a.q + row * a.q_stride;
 #pragma unroll

@@ -73,7 +73,7 @@ def quantize_rows(x):
     x = np.asarray(x, np.float32)
     with np.errstate(all="ignore"):
         big = np.abs(x).max(axis=1)
-        inverse = np.where(big > 0, np.float32(127) / big, np.float32(0)).astype(np.float32)
+        inverse = np.where(big > 0, np.float32(127) * (np.float32(1) / big), np.float32(0)).astype(np.float32)
         bad = ~np.isfinite(big)
         q = np.rint(x * inverse[:, None])
         q[bad | ~np.isfinite(inverse)] = 0
