@@ -1,6 +1,8 @@
 // The norms around a block (evconv_block_norm) on gfx950: a row stays in the registers of its threads
 // from its one read to its one write, so the kernel is bound by the rows' bytes (few rows: by the
-// chain of a launch, a read, one to five reductions and a write).
+// chain of a launch, a read, one to five reductions and a write).  In fp32 it runs at 4.9 to 5.1 TB/s,
+// the rate of a large copy; in bf16 at 4.3 to 4.9: half the bytes to the same exponentials, roundings and
+// fp32 weights.  The sums go over a row twice (mean, then squares of differences), so no cancellation.
 #include "ops_device.h"
 #include "ops_kernels.h"
 
@@ -69,6 +71,14 @@ __device__ __forceinline__ void store_run(void* q, int64_t i, int left, const fl
   }
 }
 
+// 1 / (1 + exp(-z)).  Of bf16 outputs with the hardware's exponential and reciprocal, whose errors (2^-23, and 2^-24 |z| in the
+// exponent, which counts only where the sum is near 1 or the exponential itself is the result) stay far under the outputs' 2^-9.
+template <bool BF16>
+__device__ __forceinline__ float sigmoid_of(float z) {
+  if constexpr (BF16) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+  else return 1.0f / (1.0f + expf(-z));
+}
+
 // T threads to a row (64: a wave, several rows to a workgroup), NV vectors of eight values each.
 // GROUPED: the branch's norm is over groups (heads) of p.a.group values, each held by p.lanes lanes of one
 // wave; otherwise over the row.
@@ -94,6 +104,8 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
       in_group[v] = at[v];
     }
   }
+  // whether value j of vector v is inside (vectors of a multiple of eight are so as a whole)
+  auto inside = [&](int v, int j) __attribute__((always_inline)) { return VEC ? left[v] > 0 : j < left[v]; };
   float y[NV][8], x[NV][8];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
@@ -117,7 +129,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
         float s = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < left[v]) s += of(v, j);
+          if (inside(v, j)) s += of(v, j);
         if (GROUPED) out[v] = lanes_sum(s, p.lanes);
         all += s;
       }
@@ -152,7 +164,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
       if (a.gate)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float s = 1.0f / (1.0f + expf(-z[v][j]));
+          const float s = sigmoid_of<BF16>(z[v][j]);
           y[v][j] *= a.gate_act == EVCONV_GATE_SILU ? z[v][j] * s : s;
         }
       if (a.res_scale) {
@@ -182,7 +194,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < left[v]) s += square ? (y[v][j] - mean) * (y[v][j] - mean) : y[v][j];
+          if (inside(v, j)) s += square ? (y[v][j] - mean) * (y[v][j] - mean) : y[v][j];
       return row_sum<T>(s, s_part);
     };
     const float mean = a.norm == EVCONV_NORM_LAYER ? sum(0.0f, false) / (float)dim : 0.0f;
@@ -214,7 +226,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (j < left[v]) big = max(big, __float_as_uint(y[v][j]) & 0x7fffffffu);
+      if (inside(v, j)) big = max(big, __float_as_uint(y[v][j]) & 0x7fffffffu);
   big = row_max<T>(big, s_part);
   const float m = __uint_as_float(big);
   const bool finite = big < 0x7f800000u;
@@ -246,14 +258,20 @@ void start(const NormParams& p, hipStream_t s) {
   else block_norm<BF16, VEC, T, NV, true><<<grid, threads, 0, s>>>(p);
 }
 
+// How a row is laid over threads, by its vectors.  More values to a thread save barriers and shared reductions; fewer leave
+// room for the waves that hide the reads (four vectors: 3 waves per SIMD; one: 8).  us for 32 Mi values of x' and h from x, branch
+// and SiLU gate with three weights, rms (336 MB in bf16, 671 MB in fp32: 64 and 128 at the rate of a large copy), bf16 / fp32:
+//   dim 1024    64 x 2 69 / 133, 128 x 1 70 / 132          dim 2048   64 x 4 88 / -, 256 x 1 76 / 136
+//   dim 4096   256 x 2 75 / 140, 512 x 1 79 / 134          dim 8192  256 x 4 95 / 144, 512 x 2 78 / 139
+// and 1024 x 2 at 16384 93 / 169 (one row to a CU at a time).
 template <bool BF16, bool VEC>
 void start_size(const NormParams& p, hipStream_t s) {
   const int vectors = block_norm_vectors(p.a);
   if (vectors <= 64) start<BF16, VEC, 64, 1>(p, s);
   else if (vectors <= 128) start<BF16, VEC, 64, 2>(p, s);
-  else if (vectors <= 256) start<BF16, VEC, 64, 4>(p, s);
+  else if (vectors <= 256) start<BF16, VEC, 256, 1>(p, s);
   else if (vectors <= 512) start<BF16, VEC, 256, 2>(p, s);
-  else if (vectors <= 1024) start<BF16, VEC, 256, 4>(p, s);
+  else if (vectors <= 1024) start<BF16, VEC, 512, 2>(p, s);
   else start<BF16, VEC, 1024, 2>(p, s);
 }
 }  // namespace
