@@ -49,7 +49,8 @@ extern "C" {
  *
  * A value that is not finite makes what depends on it NaN (or infinite): outputs of its sequence and
  * head from its token on, and the state; never an earlier token's output or another sequence's.
- * A finite value of 3.39e38 and more counts as infinite. */
+ * A finite value of 3.39e38 and more counts as infinite, and so may a query or a key whose sum of squares
+ * is beyond fp32. */
 #define EVCONV_DELTA_NORMALIZE 1u
 #define EVCONV_DELTA_RAW_GATES 2u
 
@@ -84,7 +85,8 @@ typedef struct {
   float* state_out;           /* the same, may be state_in; or NULL.  Slots of no sequence stay as they are */
 } evconv_delta_args;
 
-/* Bytes of device workspace the call needs (0 for calls of single tokens). */
+/* Bytes of device workspace the call needs: 0 where nothing passes between launches (a few tokens to a
+ * sequence; bf16 keys of up to 128 channels, unless few long sequences are split over the chip). */
 evconv_status evconv_delta_rule_workspace(const evconv_delta_args* args, size_t* bytes);
 /* `workspace`: 256-byte aligned, free to be used again once the call's kernels are done. */
 evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, size_t workspace_bytes,
