@@ -135,8 +135,8 @@ evconv_status evconv_block_norm(const evconv_norm_args* args, void* hip_stream);
  *   y[m][n] = act(a_scale[m] * b_scale[n] * sum_k a[m][k] b[n][k] + bias[n])
  * The sums are exact (int32), the rest is fp32, rounded once to `dtype`.  a and b are rows of int8 as
  * evconv_block_norm writes them: 16-byte aligned, strides multiples of 128 bytes of at least k, zeros behind
- * column k (of one of the two at least).  A weight is quantised by the same call: its rows are the output
- * channels.  act: EVCONV_ACT_NONE, RELU, SIGMOID, TANH. */
+ * column k (of one of the two at least), no value -128.  A weight is quantised by the same call: its rows are
+ * the output channels.  act: EVCONV_ACT_NONE, RELU, SIGMOID, TANH. */
 typedef struct {
   int32_t abi_version;  /* EVCONV_OPS_ABI_VERSION */
   int32_t dtype;        /* of y: EVCONV_F32 or EVCONV_BF16 */

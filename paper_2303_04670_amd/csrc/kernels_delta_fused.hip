@@ -6,6 +6,12 @@
 // (the transposed operand K' comes from the same rows by transposing LDS reads), T and P go from producer to
 // consumer through a ring of three slots, S, R and D stay in their lanes (kernels_delta.hip: place).
 //
+// Bound by the vector units: a step of the chip full of workgroups (heads of 128 x 128) takes 9 us, 18 thousand cycles, of which
+// a SIMD spends 9 to 11 thousand on vector instructions (parts of S, R and D, exponentials, T's substitution), 7 thousand on matrix
+// instructions and waits in LDS reads and the step's meeting for the rest.  8 sequences of 4096 tokens and 32 heads: 0.58 ms,
+// where the rows and states alone would take 0.16; prepared by a launch of its own they took 3.6.
+// Measured without gain: a pair of producers instead of two in workgroups of four strips; more priority to half of the consumers (slower).
+//
 // In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a pair of producers
 // computes K K', Q K' and A of chunk c + 2, the other pair T of chunk c + 1.
 #include <algorithm>
@@ -457,8 +463,6 @@ __global__ __launch_bounds__((NC + 4) * 64) void delta_fused(DeltaParams p) {
     else produce<DKP, NC, VEC, TRANS, 1>(p, s_mem, span, chunks, which & 1, head, hk);
     return;
   }
-  // (the two consumers of a SIMD out of step, so that one's vector instructions run beside the other's matrix instructions)
-
   const int strip = part * NC + wave;
   const bool unit_columns = TRANS && strip >= strips_v;
   const bool works = strip < strips && !(unit_columns && seg == 0);
@@ -913,8 +917,9 @@ bool delta_fused_supported(const DeltaParams& p) {
 
 // A workgroup of the unsplit launch per head and strips; where they leave most of the chip idle and sequences are long, segments,
 // as many as give every compute unit one, of 16 chunks at least.  Three segments cost what they save: every
-// chunk is worked on twice, the first time with twice the columns (us, heads of 128 x 128, whole / in segments:
-// see delta_fused).
+// chunk is worked on twice, the first time with twice the columns.  us, heads of 128 x 128 / 64 x 64, whole and in segments:
+//   1 sequence of 32 heads, 4096 tokens 502, 258 / 303, 159;  8192 1007, 399 / 599, 235;  32768 4040, 1399 / 2444, 818
+//   2 sequences of 8192 1025, 714 / 604, 421;  3 (three segments) 1031, 1287 / 622, 775;  4 (two) 1033, 1004 / 625, 571
 size_t plan_delta_segments(DeltaParams& p) {
   const int waves = delta_fused_waves(p), strips_v = (p.a.d_v + 15) / 16, parts = (strips_v + waves - 1) / waves;
   const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, groups = pairs * parts;

@@ -3,6 +3,7 @@
 // y[m][n] = act(sa[m] sb[n] sum_k a[m][k] b[n][k] + bias[n]).  The sums are those of the 16 x 16 x 64 integer matrix
 // instruction: exact, so neither tiles nor splits change a bit of y.  b's rows are the instruction's left operand, so
 // that a lane holds values of one row of y: with b's rows taken in the order of weight_row, eight neighbouring ones.
+// Few rows: bound by the weights' bytes and the launch; many: by the matrix units (figures at `start`).
 #include "ops_device.h"
 #include "ops_kernels.h"
 
