@@ -86,7 +86,7 @@ typedef struct {
 } evconv_delta_args;
 
 /* Bytes of device workspace the call needs: 0 where nothing passes between launches (a few tokens to a
- * sequence; bf16 keys of up to 128 channels, unless few long sequences are split over the chip). */
+ * sequence; bf16 keys of up to 128 channels, unless few sequences of some length are split over the chip). */
 evconv_status evconv_delta_rule_workspace(const evconv_delta_args* args, size_t* bytes);
 /* `workspace`: 256-byte aligned, free to be used again once the call's kernels are done. */
 evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, size_t workspace_bytes,

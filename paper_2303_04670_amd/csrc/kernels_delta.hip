@@ -369,34 +369,60 @@ struct ChainShape {
   static constexpr int pieces(int stage) { return (stage == 2 * kHalves ? kTp : kRows / kHalves) / kFrag; }
 };
 
-template <bool F32, int DKP>
+//
+// Segments and TRANS: kernels_delta_fused.hip, at delta_fused.
+template <bool F32, int DKP, bool TRANS>
 __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParams p) {
   typedef ChainShape<F32, DKP> H;
   constexpr int PI = H::PI, PO = H::PO, STEPS = H::STEPS, ORD = F32 ? 2 : 1, HALVES = H::kHalves, BLOCKS = 4 / HALVES, WAVES = H::kWaves;
   extern __shared__ __align__(16) char s_mem[];
   const evconv_delta_args& a = p.a;
-  const int strips = (a.d_v + 15) / 16, groups = (strips + WAVES - 1) / WAVES;
+  const int strips_v = (a.d_v + 15) / 16, strips = strips_v + (TRANS ? (a.d_k + 15) / 16 : 0), groups = (strips + WAVES - 1) / WAVES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int strip = blockIdx.x % groups * WAVES + wave;
-  const int64_t pair = blockIdx.x / groups;
+  const int segs = TRANS ? p.segs - 1 : p.segs, seg = blockIdx.x / groups % segs;
+  const int64_t pair = blockIdx.x / groups / segs;
   const int seq = (int)(pair / a.heads_v), head = (int)(pair % a.heads_v), hk = head / p.share;
-  const Span span = span_of(p, seq);
+  Span span = span_of(p, seq);
   if (span.len <= p.short_len) return;
+  const size_t slot0 = (size_t)first_slot(span, seq) + (size_t)seg * p.seg_chunks;
+  {
+    const int64_t skip = (int64_t)seg * p.seg_chunks * C;
+    if (span.len <= skip + (TRANS ? p.seg_chunks * C : 0)) return;  // (TRANS: nothing behind it)
+    if (TRANS && seg == 0 && (int)(blockIdx.x % groups) * WAVES >= strips_v) return;
+    span.first += (int)skip;
+    span.len -= (int)skip;
+  }
+  const bool last = span.len <= p.seg_chunks * C;
+  span.len = min(span.len, p.seg_chunks * C);
   const int col = strip * 16 + n;
-  const bool works = strip < strips, in = col < a.d_v;
+  const bool unit_columns = TRANS && strip >= strips_v;
+  const bool works = strip < strips && !(unit_columns && seg == 0), in = col < a.d_v && !unit_columns;
   const int64_t at = state_at(p, seq, head);
+  const int ld = (strips_v + (a.d_k + 15) / 16) * 16;  // floats between the rows of p.trans
   f32x4 S[2 * STEPS];
-#pragma unroll
-  for (int b = 0; b < 2 * STEPS; ++b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = place(b, 4 * g + i);
-      S[b][i] = at >= 0 && a.state_in && row < a.d_k && in ? a.state_in[at + (int64_t)row * a.d_v + col] : 0.0f;
+  {
+    const float* from = a.state_in ? a.state_in + at : nullptr;
+    int width = a.d_v;
+    bool there = at >= 0 && a.state_in && in;
+    if (TRANS) there &= seg == 0;
+    else if (seg || !last) {
+      from = seg ? p.trans + (pair * p.segs + seg - 1) * a.d_k * (int64_t)ld : p.start0 + pair * a.d_k * (int64_t)(strips_v * 16);
+      width = seg ? ld : strips_v * 16;
+      there = works;
     }
-    asm volatile("" : "+v"(S[b]));  // (waited for here, not in every turn of the loop)
+#pragma unroll
+    for (int b = 0; b < 2 * STEPS; ++b) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = place(b, 4 * g + i);
+        S[b][i] = there && row < a.d_k ? from[row * width + col] : unit_columns && row == col - strips_v * 16 ? 1.0f : 0.0f;
+        if (TRANS && seg == 0 && works && row < a.d_k) p.start0[pair * a.d_k * (int64_t)(strips_v * 16) + row * strips_v * 16 + col] = S[b][i];
+      }
+      asm volatile("" : "+v"(S[b]));  // (waited for here, not in every turn of the loop)
+    }
   }
   const int chunks = (span.len + C - 1) / C;
-  const size_t slot0 = first_slot(span, seq);
   // a chunk's operands in memory
   auto rows_at = [&](int chunk) { return p.frag_k + ((slot0 + chunk) * a.heads_k + hk) * (size_t)(3 * H::kRows); };
   auto tp_at = [&](int chunk) { return p.frag_t + ((slot0 + chunk) * a.heads_v + head) * (size_t)H::kTp; };
@@ -406,7 +432,7 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
   char* const s_scal = s_mem + 3 * H::kBuffer;
   // Stage `stage` of a chunk into buffer `buffer`
   auto request = [&](int chunk, int stage, int buffer) __attribute__((always_inline)) {
-    if (chunk >= chunks) return;
+    if (chunk >= chunks || (TRANS && stage >= HALVES && stage < 2 * HALVES)) return;
     // stages: K (halves), Q (halves), T and P, K' (halves)
     const bool tp = stage == 2 * HALVES;
     const char* const from = tp ? tp_at(chunk) : rows_at(chunk) + (size_t)(stage < 2 * HALVES ? stage : stage - 1) * (H::kRows / HALVES);
@@ -451,7 +477,8 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
       buffer = buffer == 2 ? 0 : buffer + 1;
       if (!works) return;
       auto frag = [&](int i) __attribute__((always_inline)) { return *(const b16x8*)(q + (size_t)i * kFrag); };
-      if constexpr (stage < 2 * HALVES) {  // K S, then Q S
+      if constexpr (TRANS && stage >= HALVES && stage < 2 * HALVES) {
+      } else if constexpr (stage < 2 * HALVES) {  // K S, then Q S
         constexpr bool keys = stage < HALVES;
         constexpr int b0 = stage % HALVES * BLOCKS;
         f32x4 acc[BLOCKS];
@@ -491,7 +518,7 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             R[b][i] = t0 + i < count ? beta[i] * v[b * 4 + i] - kf[i] * R[b][i] : 0.0f;
-            O[b][i] *= qf[i];
+            if (!TRANS) O[b][i] *= qf[i];
             if (!(fabsf(R[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
           }
         }
@@ -525,32 +552,34 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
           __builtin_amdgcn_sched_barrier(0);
         }
         if (__ballot(bad != 0 || first_bad < C)) cut_columns(D, bad, first_bad, g);
+        if constexpr (!TRANS) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          float x[8];
+          for (int s = 0; s < 2; ++s) {
+            float x[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[i] = D[2 * s][i];
-            x[4 + i] = D[2 * s + 1][i];
+            for (int i = 0; i < 4; ++i) {
+              x[i] = D[2 * s][i];
+              x[4 + i] = D[2 * s + 1][i];
+            }
+            b16x8 Dp[PO];
+            split8(x, Dp);
+#pragma unroll
+            for (int b = 2 * s; b < 4; ++b) {
+              b16x8 pp[PO];
+#pragma unroll
+              for (int part = 0; part < PO; ++part) pp[part] = frag(kTri * 3 + tri(b, s) * PO + part);
+              mfma_parts<ORD>(O[b], pp, Dp);
+            }
           }
-          b16x8 Dp[PO];
-          split8(x, Dp);
 #pragma unroll
-          for (int b = 2 * s; b < 4; ++b) {
-            b16x8 pp[PO];
+          for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int part = 0; part < PO; ++part) pp[part] = frag(kTri * 3 + tri(b, s) * PO + part);
-            mfma_parts<ORD>(O[b], pp, Dp);
-          }
+            for (int i = 0; i < 4; ++i) {
+              const int t = place(b, 4 * g) + i;
+              if (t < count && in)
+                store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, t < first_bad ? O[b][i] : NAN);
+            }
         }
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int t = place(b, 4 * g) + i;
-            if (t < count && in)
-              store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, t < first_bad ? O[b][i] : NAN);
-          }
         const float decay = scal[4 * C];
 #pragma unroll
         for (int b = 0; b < 2 * STEPS; ++b) S[b] *= decay;
@@ -595,13 +624,14 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
       run(std::integral_constant<int, 6>());
     }
   }
-  if (at >= 0 && a.state_out && in)
+  float* const out = TRANS ? p.trans + (pair * p.segs + seg) * a.d_k * (int64_t)ld : at >= 0 && a.state_out && last ? a.state_out + at : nullptr;
+  if (out && works && (TRANS || in))
 #pragma unroll
     for (int b = 0; b < 2 * STEPS; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = place(b, 4 * g + i);
-        if (row < a.d_k) a.state_out[at + (int64_t)row * a.d_v + col] = S[b][i];
+        if (row < a.d_k) out[row * (TRANS ? ld : a.d_v) + col] = S[b][i];
       }
 }
 
@@ -622,11 +652,21 @@ void steps_type(const DeltaParams& p, bool vec, unsigned grid, hipStream_t s) {
   else if (p.a.d_k <= 128) steps_rows<BF16, 16>(p, vec, grid, s);
   else steps_rows<BF16, 32>(p, vec, grid, s);
 }
+template <bool F32, int DKP, bool TRANS>
+void chain_pass(const DeltaParams& p, hipStream_t s) {
+  constexpr int waves = ChainShape<F32, DKP>::kWaves;
+  const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v * (TRANS ? p.segs - 1 : p.segs);
+  const int strips = (p.a.d_v + 15) / 16 + (TRANS ? (p.a.d_k + 15) / 16 : 0);
+  delta_chain<F32, DKP, TRANS><<<(unsigned)(pairs * ((strips + waves - 1) / waves)), waves * 64, ChainShape<F32, DKP>::kBytes, s>>>(p);
+}
 template <bool F32, int DKP>
 void chain(const DeltaParams& p, hipStream_t s) {
-  const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, strips = (p.a.d_v + 15) / 16;
-  constexpr int waves = ChainShape<F32, DKP>::kWaves;
-  delta_chain<F32, DKP><<<(unsigned)(pairs * ((strips + waves - 1) / waves)), waves * 64, ChainShape<F32, DKP>::kBytes, s>>>(p);
+  if constexpr (F32 && DKP <= 128)
+    if (p.segs > 1) {
+      chain_pass<F32, DKP, true>(p, s);
+      launch_delta_join(p, s);
+    }
+  chain_pass<F32, DKP, false>(p, s);
 }
 template <bool F32>
 void chunks_type(const DeltaParams& p, hipStream_t s) {

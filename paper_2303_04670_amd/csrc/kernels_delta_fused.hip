@@ -895,8 +895,7 @@ template <int DKP, int NC, bool VEC>
 void start(const DeltaParams& p, hipStream_t s) {
   if (p.segs > 1) {
     start_pass<DKP, NC, VEC, true>(p, s);
-    const int64_t grid = (int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 15) / 16);
-    delta_join<DKP><<<(unsigned)grid, 256, 0, s>>>(p);
+    launch_delta_join(p, s);
   }
   start_pass<DKP, NC, VEC, false>(p, s);
 }
@@ -915,20 +914,27 @@ bool delta_fused_supported(const DeltaParams& p) {
          near(p.a.v.token_stride) && near(p.a.o_token_stride) && near(p.a.gate.token_stride) && near(p.a.beta.token_stride);
 }
 
-// A workgroup of the unsplit launch per head and strips; where they leave most of the chip idle and sequences are long, segments,
-// as many as give every compute unit one, of 16 chunks at least.  Three segments cost what they save: every
-// chunk is worked on twice, the first time with twice the columns.  us, heads of 128 x 128 / 64 x 64, whole and in segments:
-//   1 sequence of 32 heads, 4096 tokens 502, 258 / 303, 159;  8192 1007, 399 / 599, 235;  32768 4040, 1399 / 2444, 818
-//   2 sequences of 8192 1025, 714 / 604, 421;  3 (three segments) 1031, 1287 / 622, 775;  4 (two) 1033, 1004 / 625, 571
-size_t plan_delta_segments(DeltaParams& p) {
-  const int waves = delta_fused_waves(p), strips_v = (p.a.d_v + 15) / 16, parts = (strips_v + waves - 1) / waves;
+// A workgroup of the unsplit launch per head and eight (four) strips; where they leave most of the chip idle and sequences are
+// long, segments, as many as give every compute unit one, of four chunks at least.  Three segments cost what they save: every
+// chunk is worked on twice, the first time with twice the columns.  us, whole and in segments, heads of 128 x 128 / 64 x 64:
+//                                    bf16                              fp32
+//   1 sequence of 4 heads,   800       107, 90 / 69, 56                  167, 136 / 98, 78
+//                           1024       130, 90 / 83, 56                  200, 138 / 117, 79
+//                           4096       483, 135 / 303, 70                684, 178 / 405, 97
+//   1 sequence of 32 heads, 2048       257, 155 / 158, 89                437, 282 / 247, 127
+//                          32768      4040, 1399 / 2444, 818            6696, 3087 / 4070, 1539
+//   2 sequences of 32 heads, 8192     1025, 714 / 604, 421              1971, 1573 / 1207, 803
+//   3 (three segments)                1031, 1287 / 622, 775             2213, 2652 / 1355, 1366
+//   4 (two)                           1033, 1004 / 625, 571             2477, 2507 / 1519, 1492
+size_t plan_delta_segments(DeltaParams& p, bool fused) {
+  const int waves = fused ? delta_fused_waves(p) : 8, strips_v = (p.a.d_v + 15) / 16, parts = (strips_v + waves - 1) / waves;
   const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, groups = pairs * parts;
   const int64_t most = p.len >= 0 ? (p.len + C - 1) / C : p.a.n_tokens / C + 1;                          // chunks of a sequence
   const int64_t sum = p.len >= 0 ? most * p.a.n_seq : p.a.n_tokens / C + p.a.n_seq;                      // of all
   p.segs = 1;
   p.seg_chunks = (int)most;
-  if (groups >= 128 || sum / p.a.n_seq < 64) return 0;
-  const int64_t chunks = std::max<int64_t>(16, (sum * p.a.heads_v * parts + 255) / 256), segs = (most + chunks - 1) / chunks;
+  if ((!fused && (p.a.dtype != EVCONV_F32 || p.a.d_k > 128)) || groups >= 128 || sum / p.a.n_seq < 12) return 0;
+  const int64_t chunks = std::max<int64_t>(4, (sum * p.a.heads_v * parts + 255) / 256), segs = (most + chunks - 1) / chunks;
   const int64_t state = (int64_t)p.a.d_k * (strips_v + (p.a.d_k + 15) / 16) * 16 * 4, start = (int64_t)p.a.d_k * strips_v * 16 * 4;
   const int64_t bytes = pairs * (segs * state + start);
   if (segs < 4 || bytes > 2ll << 30 || pairs * segs * parts * 8 >= 1ll << 31) return 0;
@@ -942,6 +948,11 @@ void place_delta_segments(DeltaParams& p, char* workspace) {
   p.start0 = p.trans + (int64_t)p.a.n_seq * p.a.heads_v * p.segs * p.a.d_k * (strips_v + (p.a.d_k + 15) / 16) * 16;
 }
 
+void launch_delta_join(const DeltaParams& p, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 15) / 16));
+  if (p.dkp == 64) delta_join<64><<<grid, 256, 0, s>>>(p);
+  else delta_join<128><<<grid, 256, 0, s>>>(p);
+}
 void launch_delta_fused(const DeltaParams& p, hipStream_t s) {
   if (p.dkp == 64) start_keys<64>(p, s);
   else start_keys<128>(p, s);

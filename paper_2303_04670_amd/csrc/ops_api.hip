@@ -39,7 +39,7 @@ constexpr int kShortFused = 6, kShort = 12;
 struct DeltaPlan {
   DeltaParams p;
   bool steps, chunks, fused;
-  size_t off_t, off_scal, bytes;
+  size_t off_k, off_t, off_scal, bytes;
 };
 
 evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
@@ -71,16 +71,17 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.short_len = one_launch ? kShortFused : kShort;
   d.steps = d.p.len < 0 || d.p.len <= d.p.short_len;
   d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
-  d.off_t = d.off_scal = d.bytes = 0;
+  d.off_k = d.off_t = d.off_scal = d.bytes = 0;
   d.fused = d.chunks && one_launch;
   if (d.chunks) {
     const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8 * ((a->d_v + 15) / 16);
     if (pairs >= 1ll << 31 || (int64_t)d.p.slots_total * a->heads_v >= 1ll << 31)
       return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens of %d sequences and %d heads are more than one launch takes", (long long)a->n_tokens, a->n_seq, a->heads_v);
   }
-  if (d.fused) d.bytes = plan_delta_segments(d.p);
+  if (d.chunks) d.bytes = plan_delta_segments(d.p, d.fused);
   if (d.chunks && !d.fused) {
-    d.off_t = (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);
+    d.off_k = (d.bytes + 255) / 256 * 256;
+    d.off_t = d.off_k + (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);
     d.off_scal = d.off_t + (size_t)d.p.slots_total * a->heads_v * delta_frag_t_bytes(a->dtype);
     d.bytes = d.off_scal + (size_t)d.p.slots_total * a->heads_v * kDeltaScalars * sizeof(float);
   }
@@ -145,9 +146,9 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
   if (st != EVCONV_OK) return st;
   if (d.bytes && (!workspace || workspace_bytes < d.bytes || !aligned(workspace, 256)))
     return refuse(EVCONV_ERR_WORKSPACE, "delta rule: needs %zu bytes of workspace at a multiple of 256, got %zu", d.bytes, workspace ? workspace_bytes : 0);
-  if (d.fused && d.p.segs > 1) place_delta_segments(d.p, (char*)workspace);
+  if (d.chunks && d.p.segs > 1) place_delta_segments(d.p, (char*)workspace);
   if (d.chunks && !d.fused) {
-    d.p.frag_k = (char*)workspace;
+    d.p.frag_k = (char*)workspace + d.off_k;
     d.p.frag_t = (char*)workspace + d.off_t;
     d.p.scal = (float*)((char*)workspace + d.off_scal);
   }

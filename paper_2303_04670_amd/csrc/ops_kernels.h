@@ -28,7 +28,7 @@ struct DeltaParams {
   char* frag_k;     // per chunk slot and key head: K, Q and K' as matrix-core operands
   char* frag_t;     // per chunk slot and value head: T and P
   float* scal;      // per chunk slot and value head: kDeltaScalars
-  int segs, seg_chunks;   // one launch for all chunks: segments of a sequence (1: whole), chunks of one
+  int segs, seg_chunks;   // segments of a sequence (1: whole), chunks of one
   float *trans, *start0;  // what segments do to the state, the first one's start
 };
 // Sizes in the workspace, per chunk slot and head.
@@ -37,10 +37,12 @@ size_t delta_frag_t_bytes(int dtype);
 constexpr int kDeltaScalars = 512;  // four factors of every token, the decay; up to whole 1 KB
 void launch_delta_steps(const DeltaParams& p, hipStream_t s);
 void launch_delta_chunks(const DeltaParams& p, hipStream_t s);
-// chunks in one launch; workspace for segments only
+// chunks in one launch
 bool delta_fused_supported(const DeltaParams& p);
-size_t plan_delta_segments(DeltaParams& p);  // sets segs and seg_chunks; bytes of workspace
+// segments of long sequences, of either way
+size_t plan_delta_segments(DeltaParams& p, bool fused);  // sets segs and seg_chunks; bytes of workspace
 void place_delta_segments(DeltaParams& p, char* workspace);
+void launch_delta_join(const DeltaParams& p, hipStream_t s);
 void launch_delta_fused(const DeltaParams& p, hipStream_t s);
 
 // ---- norms around a block, rows of 8-bit integers ------------------------------------------------

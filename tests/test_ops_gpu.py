@@ -107,23 +107,24 @@ def test_delta_rule_long_sequence():
     close(s, want_s)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 64), (2, 2, 128, 128), (1, 1, 40, 24), (1, 1, 37, 70), (1, 1, 128, 17)])
-def test_delta_rule_in_segments(hk, hv, dk, dv):
+def test_delta_rule_in_segments(hk, hv, dk, dv, dtype):
     """Sequences long enough, and heads few enough, to be worked on in segments side by side; states in place."""
     torch, ops = torch_ops()
     for lens in ([4500], [70, 9000, 0, 5, 3100]):
-        x = delta_inputs(16 + dk, sum(lens), len(lens), hk, hv, dk, dv, "bf16", True)
+        x = delta_inputs(16 + dk, sum(lens), len(lens), hk, hv, dk, dv, dtype, True)
         d = {n: a.cuda() for n, a in x.items()}
         o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], state_out=d["state"], seq_offsets=offsets(lens),
                               normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
         c = numbers(x)
         want_o, want_s = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], c["state"], spans_of(lens), dk ** -0.5, True,
                                             c["a_scale"], c["dt_bias"])
-        close(o, want_o, True)
+        close(o, want_o, dtype == "bf16")
         close(s, want_s)
     # no state to begin with, none to leave, and a value that is not finite in one column of one segment
     n = 4500
-    x = delta_inputs(17, n, 1, hk, hv, dk, dv, "bf16", True)
+    x = delta_inputs(17, n, 1, hk, hv, dk, dv, dtype, True)
     d = {name: a.cuda() for name, a in x.items()}
     kw = dict(normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
     o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], 0 * d["state"], n_seq=1, **kw)
