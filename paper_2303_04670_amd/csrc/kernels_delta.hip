@@ -351,8 +351,8 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
 // registers.  The waves share the operands: a chunk's are K, Q, (T, P) and K' in turn, each brought into one of three
 // buffers in LDS two stages before it is used (K, Q and K' in halves where they are larger than a buffer).
 // Bound by a sequence's longest chain: fp32 operands are three parts, so a product is six matrix instructions, and what comes
-// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 124 us, 11 a
-// chunk, beside 40 for delta_prepare (every wave with operands of its own from L2: 222).
+// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 106 us, 10 a
+// chunk, beside 36 for delta_prepare (keys as 128 channels instead of 96: 124; every wave with operands of its own from L2: 222).
 template <bool F32, int DKP>
 struct ChainShape {
   static constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32;
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
 #pragma unroll
         for (int b = 0; b < 4; ++b) D[b] *= *(const f32x4*)(scal + 3 * C + place(b, 4 * g));  // w D from here on
       } else {  // S = e^G S + K' (w D)
-        constexpr int b0 = (stage - 2 * HALVES - 1) * (2 * STEPS / HALVES);
+        constexpr int b0 = (stage - 2 * HALVES - 1) * (2 * STEPS / HALVES), KT = 2 * STEPS / HALVES % 4 ? 2 : 4;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           float x[8];
@@ -598,14 +598,14 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
           b16x8 Dw[3];
           split8(x, Dw);
 #pragma unroll
-          for (int b = 0; b < 2 * STEPS / HALVES; b += 4) {
-            b16x8 kt[4][PI];
+          for (int b = 0; b < 2 * STEPS / HALVES; b += KT) {
+            b16x8 kt[KT][PI];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < KT; ++i)
 #pragma unroll
               for (int part = 0; part < PI; ++part) kt[i][part] = frag(((b + i) * 2 + s) * PI + part);
             __builtin_amdgcn_sched_barrier(0);
-            mfma_parts<2, 4>(&S[b0 + b], kt, Dw);
+            mfma_parts<2, KT>(&S[b0 + b], kt, Dw);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -674,7 +674,9 @@ void chunks_type(const DeltaParams& p, hipStream_t s) {
   if (p.vec) delta_prepare<F32, true><<<grid, 256, 0, s>>>(p);
   else delta_prepare<F32, false><<<grid, 256, 0, s>>>(p);
   switch (p.dkp) {
+    case 32: if constexpr (F32) return chain<F32, 32>(p, s); else return;
     case 64: return chain<F32, 64>(p, s);
+    case 96: if constexpr (F32) return chain<F32, 96>(p, s); else return;
     case 128: return chain<F32, 128>(p, s);
     default: return chain<F32, 256>(p, s);
   }

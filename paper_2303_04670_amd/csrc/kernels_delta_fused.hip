@@ -950,7 +950,7 @@ void place_delta_segments(DeltaParams& p, char* workspace) {
 
 void launch_delta_join(const DeltaParams& p, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 15) / 16));
-  if (p.dkp == 64) delta_join<64><<<grid, 256, 0, s>>>(p);
+  if (p.dkp <= 64) delta_join<64><<<grid, 256, 0, s>>>(p);
   else delta_join<128><<<grid, 256, 0, s>>>(p);
 }
 void launch_delta_fused(const DeltaParams& p, hipStream_t s) {

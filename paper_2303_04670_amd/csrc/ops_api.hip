@@ -31,10 +31,12 @@ bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 bool wide(int dtype, const void* p, int64_t stride) { return aligned(p, 16) && stride * (int64_t)type_size(dtype) % 16 == 0; }
 bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token_stride) && wide(dtype, h.data, h.head_stride); }
 
-// Sequences of up to this many tokens go token by token (of calls that the one-launch kernel takes otherwise, of others).  us for
+// Sequences of up to this many tokens go token by token (of calls that the one-launch kernel takes otherwise, of others; of calls
+// with lengths of their own, whose chunks wait for the launch of the tokens: 24 ragged sequences of up to 700 tokens, 6 heads of
+// 80 x 112, fp32, wait for 24 us at 12 tokens, 12 at 4).  us for
 // 16 sequences of 4 heads of 64 x 64, 64 of 16 of 128 x 128, token by token / in chunks: bf16, 6 tokens 18 / 14, 59 / 76, 8
 // tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 137, 12 tokens 26 / 27, 80 / 136.
-constexpr int kShortFused = 6, kShort = 12;
+constexpr int kShortFused = 6, kShort = 12, kShortRagged = 4;
 
 struct DeltaPlan {
   DeltaParams p;
@@ -65,10 +67,11 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.len = a->seq_offsets ? -1 : (int)(a->n_tokens / a->n_seq);
   d.p.slots_total = (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
   d.p.dkp = a->d_k <= 64 ? 64 : a->d_k <= 128 ? 128 : 256;
+  if (a->dtype == EVCONV_F32 && a->d_k <= 128) d.p.dkp = (a->d_k + 31) / 32 * 32;  // (its products are six times as many)
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
   d.p.vec_v = a->d_v % 8 == 0 && wide(a->dtype, a->v) && aligned(a->o, 8) && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0;
   const bool one_launch = delta_fused_supported(d.p);
-  d.p.short_len = one_launch ? kShortFused : kShort;
+  d.p.short_len = d.p.len < 0 ? kShortRagged : one_launch ? kShortFused : kShort;
   d.steps = d.p.len < 0 || d.p.len <= d.p.short_len;
   d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
   d.off_k = d.off_t = d.off_scal = d.bytes = 0;
