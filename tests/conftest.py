@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -24,3 +25,13 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def _no_cycle_collection_inside_a_test():
+    """Tests compare how much device memory is allocated before and after a call.  What an earlier call left in a cycle
+    (pytest.raises keeps its frame, with the nets and tensors in it) would be freed by a collection in between, whose
+    moment depends on how many objects the tests before it made."""
+    gc.disable()
+    yield
+    gc.enable()
