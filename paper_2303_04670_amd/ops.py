@@ -40,6 +40,12 @@ class DeltaArgs(ctypes.Structure):
                 ("seq_offsets", _vp), ("slots", _vp), ("state_in", _vp), ("state_out", _vp)]
 
 
+class _FlatDeltaArgs(ctypes.Structure):
+    """DeltaArgs with the fields of its Heads in their place: filled in by position, without five more structures a call."""
+    _fields_ = [(name + part, kind) for name, of in DeltaArgs._fields_
+                for part, kind in ([("_" + p, t) for p, t in Heads._fields_] if of is Heads else [("", of)])]
+
+
 class NormArgs(ctypes.Structure):
     _fields_ = [("abi_version", _i32), ("dtype", _i32), ("norm", _i32), ("gate_act", _i32), ("pre_norm", _i32),
                 ("dim", _i32), ("group", _i32), ("eps", _f32), ("rows", _i64), ("x", _vp), ("branch", _vp), ("gate", _vp),
@@ -70,6 +76,9 @@ class NormResult(NamedTuple):
 
 
 _entry = None
+_byref, _empty, _empty_like = ctypes.byref, torch.empty, torch.empty_like
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (without the wrapper's own checks)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 
 
 def _calls():
@@ -123,6 +132,14 @@ def _packed(t, name, gpu, dtype, shape):
     return t.data_ptr()
 
 
+def _like(t, shape, dtype, gpu):
+    """A new contiguous tensor of this shape and type, those of `t` unless that is None.  (Making one like another takes less
+    time than making one from its shape.)"""
+    if t is not None and t.is_contiguous():
+        return _empty_like(t)
+    return _empty(*shape, dtype=dtype, device=gpu)
+
+
 def _dtype(t, name):
     code = _DTYPES.get(t.dtype)
     if code is None:
@@ -133,18 +150,22 @@ def _dtype(t, name):
 def _enqueue(call, args, gpu, workspace_of=None):
     """The call on the GPU's current stream, with a workspace of its own from the caching allocator (which
     keeps it for this stream until the call's kernels are done)."""
-    if torch.cuda.current_device() != gpu:
+    if _current_device() != gpu:
         with torch.cuda.device(gpu):
             return _enqueue(call, args, gpu, workspace_of)
-    stream, args = torch._C._cuda_getCurrentRawStream(gpu), ctypes.byref(args)
+    stream, args = _current_stream(gpu), _byref(args)
     if workspace_of is None:
-        return _check(call(args, stream))
-    n = ctypes.c_size_t(0)
-    _check(workspace_of(args, ctypes.byref(n)))
-    if n.value:
-        ws = torch.empty(n.value, dtype=torch.uint8, device=gpu)
-        return _check(call(args, ws.data_ptr(), n.value, stream))
-    _check(call(args, None, 0, stream))
+        status = call(args, stream)
+    else:
+        n = ctypes.c_size_t(0)
+        _check(workspace_of(args, _byref(n)))
+        if n.value:
+            ws = torch.empty(n.value, dtype=torch.uint8, device=gpu)
+            status = call(args, ws.data_ptr(), n.value, stream)
+        else:
+            status = call(args, None, 0, stream)
+    if status != OK:
+        _check(status)
 
 
 def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq_offsets=None, slots=None, n_seq=None,
@@ -165,35 +186,37 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
     if v_shape[0] != n:
         _explain(v, "v", gpu, dtype, (n, hv, dv))
     raw = a_scale is not None or dt_bias is not None
-    a = DeltaArgs()
-    a.abi_version, a.dtype, a.gate_dtype = ABI_VERSION, _dtype(v, "v"), _dtype(gate, "gate")
-    a.flags = (DELTA_NORMALIZE if normalize else 0) | (DELTA_RAW_GATES if raw else 0)
-    a.heads_k, a.heads_v, a.d_k, a.d_v, a.n_tokens, a.scale = hk, hv, dk, dv, n, dk ** -0.5 if scale is None else scale
-    for to, t, name, shape in ((a.q, q, "q", q_shape), (a.k, k, "k", q_shape), (a.v, v, "v", v_shape)):
-        to.data, (to.token_stride, to.head_stride, _) = _rows(t, name, gpu, dtype, shape)
-    for to, t, name in ((a.gate, gate, "gate"), (a.beta, beta, "beta")):  # (single values: any strides)
-        if t.get_device() != gpu or t.dtype is not gate_dtype or t.shape != (n, hv):
-            _explain(t, name, gpu, gate_dtype, (n, hv))
-        to.data, (to.token_stride, to.head_stride) = t.data_ptr(), t.stride()
+    flags, f32 = (DELTA_NORMALIZE if normalize else 0) | (DELTA_RAW_GATES if raw else 0), torch.float32
+    q_at, (q_token, q_head, _) = _rows(q, "q", gpu, dtype, q_shape)
+    k_at, (k_token, k_head, _) = _rows(k, "k", gpu, dtype, q_shape)
+    v_at, (v_token, v_head, _) = _rows(v, "v", gpu, dtype, v_shape)
+    gates = (n, hv)
+    if gate.get_device() != gpu or gate.shape != gates:  # (single values: any strides)
+        _explain(gate, "gate", gpu, gate_dtype, gates)
+    if beta.get_device() != gpu or beta.dtype is not gate_dtype or beta.shape != gates:
+        _explain(beta, "beta", gpu, gate_dtype, gates)
     if raw:
-        a.a_scale, a.dt_bias = _packed(a_scale, "a_scale", gpu, torch.float32, (hv,)), _packed(dt_bias, "dt_bias", gpu, torch.float32, (hv,))
+        a_scale, dt_bias = _packed(a_scale, "a_scale", gpu, f32, (hv,)), _packed(dt_bias, "dt_bias", gpu, f32, (hv,))
     if seq_offsets is not None:
         n_seq = seq_offsets.numel() - 1
-        a.seq_offsets = _packed(seq_offsets, "seq_offsets", gpu, torch.int32, (n_seq + 1,))
+        seq_offsets = _packed(seq_offsets, "seq_offsets", gpu, torch.int32, (n_seq + 1,))
     elif n_seq is None:
         n_seq = slots.numel() if slots is not None else state.shape[0] if state is not None and state.dim() else 1
-    a.slots = _packed(slots, "slots", gpu, torch.int32, (n_seq,))
+    slots_at = _packed(slots, "slots", gpu, torch.int32, (n_seq,))
     some = state if state is not None else state_out
     n_slots = some.shape[0] if some is not None and some.dim() else n_seq
     shape = (n_slots, hv, dk, dv)
-    a.state_in = _packed(state, "state", gpu, torch.float32, shape)
+    state_at = _packed(state, "state", gpu, f32, shape)
     if state_out is None:
-        state_out = state if state is not None and slots is not None else torch.empty(shape, dtype=torch.float32, device=gpu)
-    a.state_out = _packed(state_out, "state_out", gpu, torch.float32, shape)
+        state_out = state if state is not None and slots is not None else _like(state, shape, f32, gpu)
+    to_at = state_at if state_out is state else _packed(state_out, "state_out", gpu, f32, shape)
     if out is None:
-        out = torch.empty(v_shape, dtype=dtype, device=gpu)
-    a.o, (a.o_token_stride, a.o_head_stride, _) = _rows(out, "out", gpu, dtype, v_shape)
-    a.n_seq, a.n_slots = n_seq, n_slots
+        out = _like(v, v_shape, dtype, gpu)
+    o_at, (o_token, o_head, _) = _rows(out, "out", gpu, dtype, v_shape)
+    a = _FlatDeltaArgs(ABI_VERSION, _dtype(v, "v"), _dtype(gate, "gate"), flags, hk, hv, dk, dv, n_seq, n_slots, n,
+                  dk ** -0.5 if scale is None else scale, q_at, q_token, q_head, k_at, k_token, k_head, v_at, v_token, v_head,
+                  gate.data_ptr(), *gate.stride(), beta.data_ptr(), *beta.stride(), o_at, o_token, o_head, a_scale, dt_bias,
+                  seq_offsets, slots_at, state_at, to_at)  # (in the order of _fields_)
     L = _calls()
     _enqueue(L.evconv_delta_rule, a, gpu, L.evconv_delta_rule_workspace)
     return out, state_out
@@ -223,49 +246,65 @@ def block_norm(x=None, branch=None, gate=None, *, post_weight=None, post_bias=No
         want = "xh" if pre_norm else "x"
     if kind not in _NORMS or gate_act not in _GATES or not want or want.strip("xhq"):
         _refuse(ERR_INVALID_ARG, f"block norm: kind {kind!r}, gate_act {gate_act!r}, want {want!r}")
-    a, f32 = NormArgs(), torch.float32
-    a.abi_version, a.dtype, a.norm, a.gate_act, a.pre_norm = ABI_VERSION, _dtype(first, "x"), _NORMS[kind], _GATES[gate_act], bool(pre_norm)
-    a.dim, a.group, a.eps, a.rows = dim, group, eps, rows
+    f32 = torch.float32
+    x_at = branch_at = gate_at = x_to = h_to = q_to = scale_to = None
+    x_step = branch_step = gate_step = x_to_step = h_to_step = q_step = 0
     if x is not None:
-        a.x, (a.x_stride, _) = _rows(x, "x", gpu, dtype, shape)
+        x_at, (x_step, _) = _rows(x, "x", gpu, dtype, shape)
     if branch is not None:
-        a.branch, (a.branch_stride, _) = _rows(branch, "branch", gpu, dtype, shape)
+        branch_at, (branch_step, _) = _rows(branch, "branch", gpu, dtype, shape)
     if gate is not None:
-        a.gate, (a.gate_stride, _) = _rows(gate, "gate", gpu, dtype, shape)
+        gate_at, (gate_step, _) = _rows(gate, "gate", gpu, dtype, shape)
     if post_weight is not None:
-        a.post_weight = _packed(post_weight, "post_weight", gpu, f32, (group,))
+        post_weight = _packed(post_weight, "post_weight", gpu, f32, (group,))
     if post_bias is not None:
-        a.post_bias = _packed(post_bias, "post_bias", gpu, f32, (group,))
+        post_bias = _packed(post_bias, "post_bias", gpu, f32, (group,))
     if res_scale is not None:
-        a.res_scale = _packed(res_scale, "res_scale", gpu, f32, (dim,))
+        res_scale = _packed(res_scale, "res_scale", gpu, f32, (dim,))
     if pre_weight is not None:
-        a.pre_weight = _packed(pre_weight, "pre_weight", gpu, f32, (dim,))
+        pre_weight = _packed(pre_weight, "pre_weight", gpu, f32, (dim,))
     if pre_bias is not None:
-        a.pre_bias = _packed(pre_bias, "pre_bias", gpu, f32, (dim,))
+        pre_bias = _packed(pre_bias, "pre_bias", gpu, f32, (dim,))
     if "x" not in want:
         x_out = None
+    elif x_out is None:
+        x_out = _like(first, shape, dtype, gpu)
+        x_to, x_to_step = x_out.data_ptr(), dim
     else:
-        if x_out is None:
-            x_out = torch.empty(shape, dtype=dtype, device=gpu)
-        a.x_out, (a.x_out_stride, _) = _rows(x_out, "x_out", gpu, dtype, shape)
+        x_to, (x_to_step, _) = _rows(x_out, "x_out", gpu, dtype, shape)
     if "h" not in want:
         h_out = None
+    elif h_out is None:
+        h_out = _like(first, shape, dtype, gpu)
+        h_to, h_to_step = h_out.data_ptr(), dim
     else:
-        if h_out is None:
-            h_out = torch.empty(shape, dtype=dtype, device=gpu)
-        a.h_out, (a.h_out_stride, _) = _rows(h_out, "h_out", gpu, dtype, shape)
+        h_to, (h_to_step, _) = _rows(h_out, "h_out", gpu, dtype, shape)
     q = None
     if "q" in want:
-        a.q_stride = -(-dim // 128) * 128
-        q = QuantRows(torch.empty((rows, a.q_stride), dtype=torch.int8, device=gpu), torch.empty(rows, dtype=f32, device=gpu), dim)
-        a.q, a.q_scale = q.q.data_ptr(), q.scale.data_ptr()
+        q_step = -(-dim // 128) * 128
+        q = QuantRows(_empty(rows, q_step, dtype=torch.int8, device=gpu), _empty(rows, dtype=f32, device=gpu), dim)
+        q_to, scale_to = q.q.data_ptr(), q.scale.data_ptr()
+    a = NormArgs(ABI_VERSION, _dtype(first, "x"), _NORMS[kind], _GATES[gate_act], 1 if pre_norm else 0, dim, group, eps, rows,
+                 x_at, branch_at, gate_at, x_step, branch_step, gate_step, post_weight, post_bias, res_scale, pre_weight, pre_bias,
+                 x_to, h_to, x_to_step, h_to_step, q_to, q_step, scale_to)  # (in the order of _fields_)
     _enqueue(_calls().evconv_block_norm, a, gpu)
     return NormResult(x_out, h_out, q)
 
 
 def quantize_rows(x) -> QuantRows:
-    """Rows [rows, k] as 8-bit integers with a scale each (tokens of activations, output channels of a weight)."""
-    return block_norm(x, want="q").q
+    """Rows [rows, k] as 8-bit integers with a scale each (tokens of activations, output channels of a weight): block_norm's
+    "q" of x alone."""
+    if x.dim() != 2:
+        _refuse(ERR_SHAPE, "block norm: x or branch as [rows, dim]")
+    gpu, dtype, shape = x.get_device(), x.dtype, x.shape
+    rows, dim = shape
+    at, (step, _) = _rows(x, "x", gpu, dtype, shape)
+    q_step = -(-dim // 128) * 128
+    q, scale = _empty(rows, q_step, dtype=torch.int8, device=gpu), _empty(rows, dtype=torch.float32, device=gpu)
+    a = NormArgs(ABI_VERSION, _dtype(x, "x"), 0, 0, 0, dim, dim, 0.0, rows, at, None, None, step, 0, 0, None, None, None, None, None,
+                 None, None, 0, 0, q.data_ptr(), q_step, scale.data_ptr())
+    _enqueue(_calls().evconv_block_norm, a, gpu)
+    return QuantRows(q, scale, dim)
 
 
 def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype=torch.float32, out=None):
@@ -278,18 +317,16 @@ def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype
     if act not in _ACTS:
         _refuse(ERR_INVALID_ARG, f"quantised product: act {act!r}")
     gpu, m, n, f32 = aq.get_device(), aq.shape[0], bq.shape[0], torch.float32
-    args = QuantArgs()
-    args.abi_version, args.act, args.n, args.k, args.m = ABI_VERSION, _ACTS[act], n, k, m
-    args.a, (args.a_stride, _) = _rows(aq, "a.q", gpu, torch.int8, aq.shape)
-    args.b, (args.b_stride, _) = _rows(bq, "b.q", gpu, torch.int8, bq.shape)
+    a_at, (a_step, _) = _rows(aq, "a.q", gpu, torch.int8, aq.shape)
+    b_at, (b_step, _) = _rows(bq, "b.q", gpu, torch.int8, bq.shape)
     if aq.shape[1] < -(-k // 128) * 128 or bq.shape[1] < -(-k // 128) * 128:
         _refuse(ERR_SHAPE, f"quantised product: rows of {aq.shape[1]} and {bq.shape[1]} bytes for {k} values")
-    args.a_scale, args.b_scale = _packed(a_scale, "a.scale", gpu, f32, (m,)), _packed(b_scale, "b.scale", gpu, f32, (n,))
     if bias is not None:
-        args.bias = _packed(bias, "bias", gpu, f32, (n,))
+        bias = _packed(bias, "bias", gpu, f32, (n,))
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=gpu)
-    args.dtype = _dtype(out, "out")
-    args.y, (args.y_stride, _) = _rows(out, "out", gpu, out.dtype, (m, n))
+        out = _empty(m, n, dtype=out_dtype, device=gpu)
+    y_at, (y_step, _) = _rows(out, "out", gpu, out.dtype, (m, n))
+    args = QuantArgs(ABI_VERSION, _dtype(out, "out"), _ACTS[act], n, k, m, a_at, b_at, a_step, b_step,
+                     _packed(a_scale, "a.scale", gpu, f32, (m,)), _packed(b_scale, "b.scale", gpu, f32, (n,)), bias, y_at, y_step)
     _enqueue(_calls().evconv_quant_matmul, args, gpu)
     return out
