@@ -150,24 +150,23 @@ __device__ __forceinline__ void load_parts(const evconv_heads& h, int head, int 
 }
 
 template <bool F32, bool VEC>
-__global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
+__global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
   constexpr int PI = parts_in(F32), PO = parts_out(F32);
   const evconv_delta_args& a = p.a;
-  __shared__ float s_a[C][C + 1], s_t[C][C + 1], s_p[C][C + 1];
+  __shared__ float s_a[C][C + 1], s_t[C][C + 1];  // (P takes A's place)
   __shared__ double s_g[C];
   __shared__ float s_beta[C], s_rk[C], s_rq[C];
   __shared__ int s_bad;  // first token whose row of A is not finite
   const int slot = blockIdx.x / a.heads_v, head = blockIdx.x % a.heads_v, hk = head / p.share;
-  // the last sequence whose first slot is not behind this one
+  // the last sequence whose first slot is not behind this one, of 64 candidates at a time
   int seq = 0;
-  {
-    int lo = 0, hi = a.n_seq - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (first_slot(span_of(p, mid), mid) <= slot) lo = mid; else hi = mid - 1;
-    }
-    seq = lo;
+  for (int n = a.n_seq; n > 1;) {
+    const int step = (n + 63) / 64, i = (threadIdx.x & 63) * step;
+    const int before = __popcll(__ballot(i < n && first_slot(span_of(p, seq + min(i, n - 1)), seq + i) <= slot)) - 1;
+    seq += before * step;
+    n = min(step, n - before * step);
   }
+  seq = __builtin_amdgcn_readfirstlane(seq);
   const Span span = span_of(p, seq);
   const int chunk = slot - first_slot(span, seq);
   if (span.len <= p.short_len || chunk < 0 || chunk * C >= span.len) return;
@@ -198,15 +197,26 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
   {
     const int row = wave * 16 + m;
     for (int c = 0; c < p.dkp; c += 32) {
+      // (all rows of a step on their way before the first is used)
+      float k[4][8], q[8];
+      auto load = [&](const evconv_heads& h, int t, bool live, float (&v)[8]) __attribute__((always_inline)) {
+        load_run<!F32, 8, VEC>(h.data, (token0 + t) * h.token_stride + hk * h.head_stride + c + 8 * g, live && t < count ? a.d_k - c - 8 * g : 0, v);
+      };
+      load(a.q, row, true, q);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) load(a.k, b * 16 + m, b <= wave, k[b]);
+      __builtin_amdgcn_sched_barrier(0);
+      float own[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) own[j] = wave & 2 ? (wave & 1 ? k[3][j] : k[2][j]) : (wave & 1 ? k[1][j] : k[0][j]);
       b16x8 ka[PI], qa[PI], kb[PI];
-      load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + row, row < count, c + 8 * g, ka);
-      load_parts<F32, VEC>(a.q, hk, a.d_k, token0 + row, row < count, c + 8 * g, qa);
+      split8(own, ka);
+      split8(q, qa);
       mfma_parts<2>(qq, qa, qa);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         if (b > wave) break;
-        const int other = b * 16 + m;
-        load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + other, other < count, c + 8 * g, kb);
+        split8(k[b], kb);
         mfma_parts<2>(kk[b], ka, kb);
         mfma_parts<2>(qk[b], qa, kb);
       }
@@ -237,7 +247,7 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
         y = s_rq[row] * e * qk[b][i];
       }
       s_a[row][col] = x;
-      s_p[row][col] = y;
+      qk[b][i] = y;
       if (!(fabsf(x) < INFINITY)) atomicMin(&s_bad, row);
     }
   __syncthreads();
@@ -291,6 +301,12 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
     __syncthreads();
   }
 
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_a[wave * 16 + 4 * g + i][b * 16 + m] = qk[b][i];
+  __syncthreads();
+
   // ---- T and P as left operands, the factors of the rows
   char* const at_t = p.frag_t + (size_t)blockIdx.x * (kTri * kFrag * (3 + PO));
   for (int f = wave; f < 2 * kTri; f += 4) {
@@ -299,7 +315,7 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
     const int row = place(b, m), col = 32 * s + 8 * g;
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = is_p ? s_p[row][col + j] : col + j <= row ? s_t[row][col + j] : 0.0f;
+    for (int j = 0; j < 8; ++j) v[j] = is_p ? s_a[row][col + j] : col + j <= row ? s_t[row][col + j] : 0.0f;
     b16x8 out[3];
     split8(v, out);
     const int n = is_p ? PO : 3;
@@ -317,20 +333,23 @@ __global__ __launch_bounds__(256) void delta_prepare(DeltaParams p) {
     q[3 * C + tid] = s_rk[tid] * expf((float)(last - s_g[tid]));
     if (tid == 0) q[4 * C] = expf((float)last);
   }
-  // ---- K, Q and K' as left operands, once per key head
-  if (head % p.share == 0) {
+  // ---- K, Q and K' as left operands: once per key head, a part by each of its value heads
+  {
+    const int first = wave + 4 * (head % p.share), stride = 4 * p.share;
     const int steps = p.dkp / 32;
     const size_t one = (size_t)4 * steps * PI * kFrag;  // of K; the same of Q and K'
     char* const at_k = p.frag_k + ((size_t)slot * a.heads_k + hk) * 3 * one;
-    for (int f = wave; f < 8 * steps; f += 4) {
-      const bool is_q = f >= 4 * steps;
-      const int i = is_q ? f - 4 * steps : f, b = i / steps, s = i % steps, row = place(b, m);
-      b16x8 out[PI];
-      load_parts<F32, VEC>(is_q ? a.q : a.k, hk, a.d_k, token0 + row, row < count, 32 * s + 8 * g, out);
+    for (int i = first; i < 4 * steps; i += stride) {  // (of K and of Q)
+      const int b = i / steps, s = i % steps, row = place(b, m);
+      b16x8 out[2][PI];
+      load_parts<F32, VEC>(a.k, hk, a.d_k, token0 + row, row < count, 32 * s + 8 * g, out[0]);
+      load_parts<F32, VEC>(a.q, hk, a.d_k, token0 + row, row < count, 32 * s + 8 * g, out[1]);
 #pragma unroll
-      for (int part = 0; part < PI; ++part) *(b16x8*)(at_k + is_q * one + (size_t)(i * PI + part) * kFrag + lane * 16) = out[part];
+      for (int of = 0; of < 2; ++of)
+#pragma unroll
+        for (int part = 0; part < PI; ++part) *(b16x8*)(at_k + of * one + (size_t)(i * PI + part) * kFrag + lane * 16) = out[of][part];
     }
-    for (int f = wave; f < 4 * steps; f += 4) {
+    for (int f = first; f < 4 * steps; f += stride) {
       const int b = f / 2, s = f % 2, row = place(b, m);
       float v[8];
 #pragma unroll
