@@ -370,30 +370,15 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
 // registers.  The waves share the operands: a chunk's are K, Q, (T, P) and K' in turn, each brought into one of three
 // buffers in LDS two stages before it is used (K, Q and K' in halves where they are larger than a buffer).
 // Bound by a sequence's longest chain: fp32 operands are three parts, so a product is six matrix instructions, and what comes
-// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 106 us, 10 a
-// chunk, beside 36 for delta_prepare (keys as 128 channels instead of 96: 124; every wave with operands of its own from L2: 222).
-template <bool F32, int DKP>
-struct ChainShape {
-  static constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32;
-  static constexpr int kRows = 4 * STEPS * PI * kFrag;            // bytes of K; Q and K' alike
-  static constexpr int kHalves = kRows > 48 * 1024 ? 2 : 1;
-  static constexpr int kWaves = DKP == 256 ? 4 : 8;               // (256 rows of a strip do not fit half of a SIMD's registers)
-  static constexpr int kTp = kTri * kFrag * (3 + PO);
-  static constexpr int kBuffer = kRows / kHalves > kTp ? kRows / kHalves : kTp;
-  static constexpr int kStages = 3 * kHalves + 1;                 // of a chunk
-  static constexpr int kScalars = kDeltaScalars * 4;
-  static constexpr int kBytes = 3 * kBuffer + 2 * kScalars;
-  static_assert(kBytes <= 160 * 1024 && kScalars == 2 * kFrag, "LDS");
-  // pieces of 1 KB of a stage
-  static constexpr int pieces(int stage) { return (stage == 2 * kHalves ? kTp : kRows / kHalves) / kFrag; }
-};
-
+// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 92 us, 8.4 a
+// chunk (18 thousand cycles: K S, T and P, K' a quarter each beyond what Q S takes, for v's and o's single values), beside 29
+// for delta_prepare.  Before: keys as 128 channels instead of 96 124, every wave with operands of its own from L2 222.
 //
 // Segments and TRANS: kernels_delta_fused.hip, at delta_fused.
-template <bool F32, int DKP, bool TRANS>
-__global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParams p) {
+template <bool F32, int DKP, bool TRANS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
   typedef ChainShape<F32, DKP> H;
-  constexpr int PI = H::PI, PO = H::PO, STEPS = H::STEPS, ORD = F32 ? 2 : 1, HALVES = H::kHalves, BLOCKS = 4 / HALVES, WAVES = H::kWaves;
+  constexpr int kSize = F32 ? 4 : 2, PI = H::PI, PO = H::PO, STEPS = H::STEPS, ORD = F32 ? 2 : 1, HALVES = H::kHalves, BLOCKS = 4 / HALVES;
   extern __shared__ __align__(16) char s_mem[];
   const evconv_delta_args& a = p.a;
   const int strips_v = (a.d_v + 15) / 16, strips = strips_v + (TRANS ? (a.d_k + 15) / 16 : 0), groups = (strips + WAVES - 1) / WAVES;
@@ -466,20 +451,13 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
   request(0, 1, 1);
   f32x4 R[4], O[4], D[4];
   float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = 0.0f;
   int first_bad = C;
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const int64_t token0 = span.first + (int64_t)chunk * C;
     const int count = min(span.len - chunk * C, C);
     const float* const scal = (const float*)(s_scal + (chunk & 1) * H::kScalars);
-    if (works) {
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = place(b, 4 * g) + i;
-          v[b * 4 + i] = t < count && in ? load_one<!F32>(a.v.data, (token0 + t) * a.v.token_stride + head * a.v.head_stride + col) : 0.0f;
-        }
-    }
     auto run = [&](auto number) __attribute__((always_inline)) {
       constexpr int stage = decltype(number)::value;
       // everything that this stage reads has arrived; the stage before it is done with its buffer
@@ -495,6 +473,42 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
       const char* const q = s_mem + buffer * H::kBuffer + lane * 16;
       buffer = buffer == 2 ? 0 : buffer + 1;
       if (!works) return;
+      // What the next wait covers: the values a stage before they are needed, the outputs a stage after they are known.
+      // (Whole chunks: a lane's place and distances that are the same for all, without a mask for every token.)
+      if constexpr (stage == 0) {
+        if (count == C) {
+          if (in) {
+            const char* const from = (const char*)a.v.data + ((token0 + place(0, 4 * g)) * a.v.token_stride + head * a.v.head_stride + col) * kSize;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) v[t] = load_one<!F32>(from + place(t / 4, t % 4) * a.v.token_stride * kSize, 0);
+          }
+        } else {
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int t = place(b, 4 * g) + i;
+              v[b * 4 + i] = t < count && in ? load_one<!F32>(a.v.data, (token0 + t) * a.v.token_stride + head * a.v.head_stride + col) : 0.0f;
+            }
+        }
+      }
+      if constexpr (stage == 2 * HALVES + 1 && !TRANS) {
+        if (count == C) {
+          if (in) {
+            char* const to = (char*)a.o + ((token0 + place(0, 4 * g)) * a.o_token_stride + head * a.o_head_stride + col) * kSize;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) store_one<!F32>(to + place(t / 4, t % 4) * a.o_token_stride * kSize, 0, O[t / 4][t % 4]);
+          }
+        } else {
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int t = place(b, 4 * g) + i;
+              if (t < count && in) store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, O[b][i]);
+            }
+        }
+      }
       auto frag = [&](int i) __attribute__((always_inline)) { return *(const b16x8*)(q + (size_t)i * kFrag); };
       if constexpr (TRANS && stage >= HALVES && stage < 2 * HALVES) {
       } else if constexpr (stage < 2 * HALVES) {  // K S, then Q S
@@ -556,18 +570,20 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
         }
         bad = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          D[b] = f32x4{0, 0, 0, 0};
+        for (int b = 0; b < 4; b += 2) {
+          D[b] = D[b + 1] = f32x4{0, 0, 0, 0};
 #pragma unroll
           for (int s = 0; s < 1 + (b >> 1); ++s) {
-            b16x8 t[3];
+            b16x8 t[2][3];
 #pragma unroll
-            for (int part = 0; part < 3; ++part) t[part] = frag(tri(b, s) * 3 + part);
-            mfma_parts<2>(D[b], t, Rp[s]);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int part = 0; part < 3; ++part) t[i][part] = frag(tri(b + i, s) * 3 + part);
+            mfma_parts<2, 2>(&D[b], t, Rp[s]);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!(fabsf(D[b][i]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
+          for (int i = 0; i < 8; ++i)
+            if (!(fabsf(D[b + i / 4][i % 4]) < kBf16Overflow)) bad |= 1u << (b * 4 + i);
           __builtin_amdgcn_sched_barrier(0);
         }
         if (__ballot(bad != 0 || first_bad < C)) cut_columns(D, bad, first_bad, g);
@@ -583,21 +599,21 @@ __global__ __launch_bounds__(DKP == 256 ? 256 : 512) void delta_chain(DeltaParam
             b16x8 Dp[PO];
             split8(x, Dp);
 #pragma unroll
-            for (int b = 2 * s; b < 4; ++b) {
-              b16x8 pp[PO];
+            for (int b = 2 * s; b < 4; b += 2) {
+              b16x8 pp[2][PO];
 #pragma unroll
-              for (int part = 0; part < PO; ++part) pp[part] = frag(kTri * 3 + tri(b, s) * PO + part);
-              mfma_parts<ORD>(O[b], pp, Dp);
+              for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int part = 0; part < PO; ++part) pp[i][part] = frag(kTri * 3 + tri(b + i, s) * PO + part);
+              mfma_parts<ORD, 2>(&O[b], pp, Dp);
             }
           }
+          if (__ballot(first_bad < C))
 #pragma unroll
-          for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int t = place(b, 4 * g) + i;
-              if (t < count && in)
-                store_one<!F32>(a.o, (token0 + t) * a.o_token_stride + head * a.o_head_stride + col, t < first_bad ? O[b][i] : NAN);
-            }
+              for (int i = 0; i < 4; ++i)
+                if (place(b, 4 * g) + i >= first_bad) O[b][i] = NAN;
         }
         const float decay = scal[4 * C];
 #pragma unroll
@@ -671,21 +687,30 @@ void steps_type(const DeltaParams& p, bool vec, unsigned grid, hipStream_t s) {
   else if (p.a.d_k <= 128) steps_rows<BF16, 16>(p, vec, grid, s);
   else steps_rows<BF16, 32>(p, vec, grid, s);
 }
-template <bool F32, int DKP, bool TRANS>
+template <bool F32, int DKP, bool TRANS, int WAVES>
 void chain_pass(const DeltaParams& p, hipStream_t s) {
-  constexpr int waves = ChainShape<F32, DKP>::kWaves;
   const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v * (TRANS ? p.segs - 1 : p.segs);
   const int strips = (p.a.d_v + 15) / 16 + (TRANS ? (p.a.d_k + 15) / 16 : 0);
-  delta_chain<F32, DKP, TRANS><<<(unsigned)(pairs * ((strips + waves - 1) / waves)), waves * 64, ChainShape<F32, DKP>::kBytes, s>>>(p);
+  delta_chain<F32, DKP, TRANS, WAVES><<<(unsigned)(pairs * ((strips + WAVES - 1) / WAVES)), WAVES * 64, ChainShape<F32, DKP>::kBytes, s>>>(p);
 }
 template <bool F32, int DKP>
 void chain(const DeltaParams& p, hipStream_t s) {
-  if constexpr (F32 && DKP <= 128)
+  if constexpr (DKP == 256) {
+    chain_pass<F32, DKP, false, 4>(p, s);  // (256 rows of a strip do not fit half of a SIMD's registers)
+  } else if constexpr (F32) {
     if (p.segs > 1) {
-      chain_pass<F32, DKP, true>(p, s);
+      chain_pass<F32, DKP, true, 8>(p, s);
       launch_delta_join(p, s);
     }
-  chain_pass<F32, DKP, false>(p, s);
+    // Four strips to a workgroup where that gives every compute unit one at most (lengths of their own: two, which are seldom
+    // long both): a wave has its SIMD to itself.  us in eight / four: the call above 105 / 96; 8 chunks of 32 heads of
+    // 128 x 128 123 / 111, of 64 133 / 122.
+    const int64_t halves = (int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 63) / 64);
+    if (p.segs == 1 && p.a.d_v > 64 && halves <= (p.len < 0 ? 512 : 256)) chain_pass<F32, DKP, false, 4>(p, s);
+    else chain_pass<F32, DKP, false, 8>(p, s);
+  } else {
+    chain_pass<F32, DKP, false, 8>(p, s);
+  }
 }
 template <bool F32>
 void chunks_type(const DeltaParams& p, hipStream_t s) {
