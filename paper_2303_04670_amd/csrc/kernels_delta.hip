@@ -373,8 +373,22 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
 // out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 92 us, 8.4 a
 // chunk (18 thousand cycles: K S, T and P, K' a quarter each beyond what Q S takes, for v's and o's single values), beside 29
 // for delta_prepare.  Before: keys as 128 channels instead of 96 124, every wave with operands of its own from L2 222.
-//
-// Segments and TRANS: kernels_delta_fused.hip, at delta_fused.
+template <bool F32, int DKP>
+struct ChainShape {
+  static constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32;
+  static constexpr int kRows = 4 * STEPS * PI * kFrag;            // bytes of K; Q and K' alike
+  static constexpr int kHalves = kRows > 48 * 1024 ? 2 : 1;
+  static constexpr int kTp = kTri * kFrag * (3 + PO);
+  static constexpr int kBuffer = kRows / kHalves > kTp ? kRows / kHalves : kTp;
+  static constexpr int kStages = 3 * kHalves + 1;                 // of a chunk
+  static constexpr int kScalars = kDeltaScalars * 4;
+  static constexpr int kBytes = 3 * kBuffer + 2 * kScalars;
+  static_assert(kBytes <= 160 * 1024 && kScalars == 2 * kFrag, "LDS");
+  // pieces of 1 KB of a stage
+  static constexpr int pieces(int stage) { return (stage == 2 * kHalves ? kTp : kRows / kHalves) / kFrag; }
+};
+
+// Segments of a sequence side by side, TRANS: as delta_fused (kernels_delta_fused.hip).
 template <bool F32, int DKP, bool TRANS, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
   typedef ChainShape<F32, DKP> H;
