@@ -194,15 +194,18 @@ void start_tile(TileParams p, hipStream_t s) {
 //   16 x 4096 x 4096   16 x 32 by 8 groups 5.1, 32 x 32 by 4 6.2, 64 x 64 10.4  (3.3 TB/s of weights)
 //   64 x 4096 x 4096   9.7, 6.9, 10.9;   64 x 1024 x 1024   3.7, 4.0, 5.1
 //   1001 x 777 x 1000  64 x 64 5.4, 128 x 128 10.6;   2048 x 2048 x 2048  15.5, 17.5;   4096 x 2048 x 2048  27.9, 23.8
+//   3000 x 2048 x 2048  24.2, 22.1;   8000 x 1024 x 4096  54, 39
 //   4096 x 4096 x 4096  128 x 128 72, 256 x 256 64.5 (2.1 POP/s);   16384 x 8192 x 2048  323, 308 (1.8 POP/s)
+// The largest ones, of which a compute unit holds one at a time, only where more than three quarters of their rounds are full:
+//   5000 x 5000 x 3000 (0.78) 101, 94;   6000 x 4096 x 2048 (0.75) 65, 68;   4600 x 4096 x 2048 (0.56) 55, 67
 template <bool BF16>
 void start(const TileParams& p, hipStream_t s) {
   const evconv_quant_args& a = p.a;
   auto tiles = [&](int bm, int bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
   if (tiles(16, 32) <= 256) start_tile<BF16, 16, 32, 1, 1, 8>(p, s);
   else if (tiles(32, 32) <= 512) start_tile<BF16, 32, 32, 2, 1, 4>(p, s);
-  else if (tiles(256, 256) >= 256) start_tile<BF16, 256, 256, 2, 4, 1>(p, s);
-  else if (tiles(128, 128) >= 512) start_tile<BF16, 128, 128, 2, 2, 1>(p, s);
+  else if (tiles(256, 256) * 4 > (tiles(256, 256) + 255) / 256 * 256 * 3) start_tile<BF16, 256, 256, 2, 4, 1>(p, s);
+  else if (tiles(128, 128) >= 384) start_tile<BF16, 128, 128, 2, 2, 1>(p, s);
   else start_tile<BF16, 64, 64, 2, 2, 1>(p, s);
 }
 }  // namespace
