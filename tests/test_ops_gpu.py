@@ -108,7 +108,19 @@ def test_delta_rule_long_sequence():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 64), (2, 2, 128, 128), (1, 1, 40, 24), (1, 1, 37, 70), (1, 1, 128, 17)])
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 32, 16), (2, 2, 96, 128), (1, 2, 80, 112), (1, 1, 200, 30)])
+def test_delta_rule_every_short_length(hk, hv, dk, dv, dtype):
+    """Lengths on both sides of where tokens go one by one, alike and of their own."""
+    calls = [([n, n, n], False) for n in range(1, 15)] + [(list(range(16)), True)]
+    for lens, ragged in calls:
+        x = delta_inputs(60 + len(lens) + lens[0], sum(lens), len(lens), hk, hv, dk, dv, dtype, True)
+        o, s, want_o, want_s = run_delta(x, lens, ragged=ragged)
+        close(o, want_o, dtype == "bf16")
+        close(s, want_s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 64), (2, 2, 128, 128), (1, 1, 40, 24), (1, 1, 37, 70), (1, 1, 128, 17), (1, 1, 96, 128), (1, 2, 24, 72)])
 def test_delta_rule_in_segments(hk, hv, dk, dv, dtype):
     """Sequences long enough, and heads few enough, to be worked on in segments side by side; states in place."""
     torch, ops = torch_ops()
