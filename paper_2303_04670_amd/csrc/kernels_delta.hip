@@ -489,15 +489,23 @@ __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
       buffer = buffer == 2 ? 0 : buffer + 1;
       if (!works) return;
       // What the next wait covers: the values a stage before they are needed, the outputs a stage after they are known.
-      // (Whole chunks: a lane's place and distances that are the same for all, without a mask for every token.)
-      if constexpr (stage == 0) {
-        if (count == C) {
-          if (in) {
-            const char* const from = (const char*)a.v.data + ((token0 + place(0, 4 * g)) * a.v.token_stride + head * a.v.head_stride + col) * kSize;
+      // (Whole chunks: a lane's place and distances that are the same for all, without a mask for every token; a few at a time
+      // between the matrix instructions, which a row of such requests would hold up.)
+      const bool whole = count == C && in;
+      const int64_t lane_v = ((token0 + place(0, 4 * g)) * a.v.token_stride + head * a.v.head_stride + col) * kSize;
+      const int64_t lane_o = ((token0 + place(0, 4 * g)) * a.o_token_stride + head * a.o_head_stride + col) * kSize;
+      auto load_v = [&](int from, int to) __attribute__((always_inline)) {
+        if (whole)
 #pragma unroll
-            for (int t = 0; t < 16; ++t) v[t] = load_one<!F32>(from + place(t / 4, t % 4) * a.v.token_stride * kSize, 0);
-          }
-        } else {
+          for (int t = from; t < to; ++t) v[t] = load_one<!F32>((const char*)a.v.data + lane_v + place(t / 4, t % 4) * a.v.token_stride * kSize, 0);
+      };
+      auto store_o = [&](int from, int to) __attribute__((always_inline)) {
+        if (whole)
+#pragma unroll
+          for (int t = from; t < to; ++t) store_one<!F32>((char*)a.o + lane_o + place(t / 4, t % 4) * a.o_token_stride * kSize, 0, O[t / 4][t % 4]);
+      };
+      if constexpr (stage == 0) {
+        if (count < C) {
 #pragma unroll
           for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -508,13 +516,7 @@ __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
         }
       }
       if constexpr (stage == 2 * HALVES + 1 && !TRANS) {
-        if (count == C) {
-          if (in) {
-            char* const to = (char*)a.o + ((token0 + place(0, 4 * g)) * a.o_token_stride + head * a.o_head_stride + col) * kSize;
-#pragma unroll
-            for (int t = 0; t < 16; ++t) store_one<!F32>(to + place(t / 4, t % 4) * a.o_token_stride * kSize, 0, O[t / 4][t % 4]);
-          }
-        } else {
+        if (count < C) {
 #pragma unroll
           for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -539,6 +541,7 @@ __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
           for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int part = 0; part < PI; ++part) k[b][part] = frag((b * STEPS + s) * PI + part);
+          if constexpr (stage == 0) load_v(16 * s / STEPS, 16 * (s + 1) / STEPS);
           __builtin_amdgcn_sched_barrier(0);
           float x[8];
 #pragma unroll
@@ -654,6 +657,11 @@ __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
             for (int i = 0; i < KT; ++i)
 #pragma unroll
               for (int part = 0; part < PI; ++part) kt[i][part] = frag(((b + i) * 2 + s) * PI + part);
+            if constexpr (stage == 2 * HALVES + 1 && !TRANS) {
+              constexpr int kAll = 2 * (2 * STEPS / HALVES / KT);  // turns of these loops
+              const int turn = s * (kAll / 2) + b / KT;
+              store_o(16 * turn / kAll, 16 * (turn + 1) / kAll);
+            }
             __builtin_amdgcn_sched_barrier(0);
             mfma_parts<2, KT>(&S[b0 + b], kt, Dw);
             __builtin_amdgcn_sched_barrier(0);
