@@ -370,10 +370,10 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
 // registers.  The waves share the operands: a chunk's are K, Q, (T, P) and K' in turn, each brought into one of three
 // buffers in LDS two stages before it is used (K, Q and K' in halves where they are larger than a buffer).
 // Bound by a sequence's longest chain: fp32 operands are three parts, so a product is six matrix instructions, and what comes
-// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 92 us, 8.4 a
-// chunk, beside 28 for delta_prepare.  (Of 18.6 thousand cycles a chunk, with masks for every token, K S took 5.2, Q S 2.8, T and P
-// 5.3, K' 4.8; what K S and K' take beyond Q S are v's and o's single values.)  Before: keys as 128 channels
-// instead of 96 124, every wave with operands of its own from L2 222.
+// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 86 us, 7.8 a
+// chunk, beside 28 for delta_prepare.  (Of 18.6 thousand cycles a chunk with v's and o's single values in a row and masks for each, K S
+// took 5.2, Q S 2.8, T and P 5.3, K' 4.8: 96 us.)  Before: keys as 128 channels instead of 96 124, every wave with
+// operands of its own from L2 222.
 template <bool F32, int DKP>
 struct ChainShape {
   static constexpr int PI = parts_in(F32), PO = parts_out(F32), STEPS = DKP / 32;
