@@ -918,14 +918,14 @@ bool delta_fused_supported(const DeltaParams& p) {
 // long, segments, as many as give every compute unit one, of four chunks at least.  Three segments cost what they save: every
 // chunk is worked on twice, the first time with twice the columns.  us, whole and in segments, heads of 128 x 128 / 64 x 64:
 //                                    bf16                              fp32
-//   1 sequence of 4 heads,   800       107, 90 / 69, 56                  167, 136 / 98, 78
-//                           1024       130, 90 / 83, 56                  200, 138 / 117, 79
-//                           4096       483, 135 / 303, 70                684, 178 / 405, 97
-//   1 sequence of 32 heads, 2048       257, 155 / 158, 89                437, 282 / 247, 127
-//                          32768      4040, 1399 / 2444, 818            6696, 3087 / 4070, 1539
-//   2 sequences of 32 heads, 8192     1025, 714 / 604, 421              1971, 1573 / 1207, 803
-//   3 (three segments)                1031, 1287 / 622, 775             2213, 2652 / 1355, 1366
-//   4 (two)                           1033, 1004 / 625, 571             2477, 2507 / 1519, 1492
+//   1 sequence of 4 heads,   800       107, 90 / 69, 56                  137, 125 / 85, 72
+//                           1024       130, 90 / 83, 56                  161, 127 / 99, 74
+//                           4096       483, 135 / 303, 70                533, 169 / 331, 91
+//   1 sequence of 32 heads, 2048       257, 155 / 158, 89                364, 269 / 207, 118
+//                          32768      4040, 1399 / 2444, 818            5862, 2961 / 3611, 1457
+//   2 sequences of 32 heads, 8192     1025, 714 / 604, 421              1760, 1512 / 1081, 764
+//   3 (three segments)                1031, 1287 / 622, 775             2034, 2521 / 1225, 1271
+//   4 (two)                           1033, 1004 / 625, 571             2306, 2426 / 1375, 1388
 size_t plan_delta_segments(DeltaParams& p, bool fused) {
   const int waves = fused ? delta_fused_waves(p) : 8, strips_v = (p.a.d_v + 15) / 16, parts = (strips_v + waves - 1) / waves;
   const int64_t pairs = (int64_t)p.a.n_seq * p.a.heads_v, groups = pairs * parts;

@@ -31,11 +31,11 @@ bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
 bool wide(int dtype, const void* p, int64_t stride) { return aligned(p, 16) && stride * (int64_t)type_size(dtype) % 16 == 0; }
 bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token_stride) && wide(dtype, h.data, h.head_stride); }
 
-// Sequences of up to this many tokens go token by token (of calls that the one-launch kernel takes otherwise, of others; of calls
-// with lengths of their own, whose chunks wait for the launch of the tokens: 24 ragged sequences of up to 700 tokens, 6 heads of
-// 80 x 112, fp32, wait for 24 us at 12 tokens, 12 at 4).  us for
+// Sequences of up to this many tokens go token by token: of calls that the one-launch kernel takes otherwise, of others.  us for
 // 16 sequences of 4 heads of 64 x 64, 64 of 16 of 128 x 128, token by token / in chunks: bf16, 6 tokens 18 / 14, 59 / 76, 8
-// tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 137, 12 tokens 26 / 27, 80 / 136.
+// tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 128, 12 tokens 25 / 27, 77 / 128.
+// Of calls with lengths of their own, whose chunks wait for the launch of the tokens (24 sequences of up to 700 tokens, 6 heads of
+// 80 x 112, fp32: for 24 us at 12 tokens, 12 at 4), fewer.
 constexpr int kShortFused = 6, kShort = 12, kShortRagged = 4;
 
 struct DeltaPlan {
