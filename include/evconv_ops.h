@@ -77,8 +77,9 @@ typedef struct {
   const float *a_scale, *dt_bias; /* fp32 [heads_v] each; EVCONV_DELTA_RAW_GATES only */
   const int32_t* seq_offsets; /* [n_seq + 1] ascending token indices, from 0 to n_tokens; sequence i is tokens
                                * [offsets[i], offsets[i+1]).  NULL: n_seq sequences of n_tokens / n_seq
-                               * (a multiple) tokens.  Values out of order or range are read as empty sequences
-                               * or cut off at n_tokens; two sequences must not overlap */
+                               * (a multiple) tokens.  A pair that descends is an empty sequence, what is out of
+                               * range is cut off there, and tokens of no sequence have no output.  Sequences
+                               * that have tokens must not overlap and stand in the order of their tokens */
   const int32_t* slots;       /* [n_seq]: the state that sequence i continues and leaves; NULL: i.  Outside
                                * [0, n_slots): it starts from zero and leaves none.  No two alike */
   const float* state_in;      /* [n_slots][heads_v][d_k][d_v], or NULL: all start from zero */

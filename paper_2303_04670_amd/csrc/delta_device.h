@@ -23,8 +23,9 @@ __device__ __forceinline__ Span span_of(const DeltaParams& p, int seq) {
   const int a = min(max(p.a.seq_offsets[seq], 0), n), b = min(max(p.a.seq_offsets[seq + 1], 0), n);
   return {a, max(b - a, 0)};
 }
-// First chunk slot of a sequence: no two sequences' slots meet, and none is behind n_tokens / C + n_seq - 1.
-__device__ __forceinline__ int first_slot(const Span& s, int seq) { return s.first / C + seq; }
+// First chunk slot of a sequence: no two sequences' slots meet, and none is behind slots_total (n_tokens / C + n_seq; of equal lengths
+// their chunks).
+__device__ __forceinline__ int first_slot(const DeltaParams& p, const Span& s, int seq) { return p.len >= 0 ? seq * ((p.len + C - 1) / C) : s.first / C + seq; }
 
 // Offset of a sequence's state, or -1: it has none.
 __device__ __forceinline__ int64_t state_at(const DeltaParams& p, int seq, int head) {

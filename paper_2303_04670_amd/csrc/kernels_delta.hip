@@ -45,7 +45,11 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
   if (seq64 >= a.n_seq) return;
   const int seq = (int)seq64;
   const Span s = span_of(p, seq);
-  if (s.len > p.short_len) return;
+  if (s.len > p.short_len) {  // (delta_prepare's: its chunk slots are told whose they are)
+    if (p.slot_seq && head == 0 && block == 0)
+      for (int i = lane, slot0 = first_slot(p, s, seq); i < (s.len + C - 1) / C; i += 64) p.slot_seq[slot0 + i] = seq;
+    return;
+  }
   const int64_t at = state_at(p, seq, head);
   const int row0 = (lane >> 3) * ROWS, col = block * 32 + (lane & 7) * 4;
   f32x4 S[ROWS];
@@ -158,17 +162,12 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
   __shared__ float s_beta[C], s_rk[C], s_rq[C];
   __shared__ int s_bad;  // first token whose row of A is not finite
   const int slot = blockIdx.x / a.heads_v, head = blockIdx.x % a.heads_v, hk = head / p.share;
-  // the last sequence whose first slot is not behind this one, of 64 candidates at a time
-  int seq = 0;
-  for (int n = a.n_seq; n > 1;) {
-    const int step = (n + 63) / 64, i = (threadIdx.x & 63) * step;
-    const int before = __popcll(__ballot(i < n && first_slot(span_of(p, seq + min(i, n - 1)), seq + i) <= slot)) - 1;
-    seq += before * step;
-    n = min(step, n - before * step);
-  }
-  seq = __builtin_amdgcn_readfirstlane(seq);
+  // Whose slot it is: delta_step has written that down for every chunk of the long sequences.  What stands there of a slot that is
+  // nobody's may be anything, and is taken only where it is the truth.
+  const int seq = p.len >= 0 ? slot / ((p.len + C - 1) / C) : p.slot_seq[slot];
+  if ((unsigned)seq >= (unsigned)a.n_seq) return;
   const Span span = span_of(p, seq);
-  const int chunk = slot - first_slot(span, seq);
+  const int chunk = slot - first_slot(p, span, seq);
   if (span.len <= p.short_len || chunk < 0 || chunk * C >= span.len) return;
   const int64_t token0 = span.first + chunk * C;
   const int count = min(span.len - chunk * C, C);
@@ -404,7 +403,7 @@ __global__ __launch_bounds__(WAVES * 64) void delta_chain(DeltaParams p) {
   const int seq = (int)(pair / a.heads_v), head = (int)(pair % a.heads_v), hk = head / p.share;
   Span span = span_of(p, seq);
   if (span.len <= p.short_len) return;
-  const size_t slot0 = (size_t)first_slot(span, seq) + (size_t)seg * p.seg_chunks;
+  const size_t slot0 = (size_t)first_slot(p, span, seq) + (size_t)seg * p.seg_chunks;
   {
     const int64_t skip = (int64_t)seg * p.seg_chunks * C;
     if (span.len <= skip + (TRANS ? p.seg_chunks * C : 0)) return;  // (TRANS: nothing behind it)

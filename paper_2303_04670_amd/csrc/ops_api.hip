@@ -41,7 +41,7 @@ constexpr int kShortFused = 6, kShort = 12, kShortRagged = 4;
 struct DeltaPlan {
   DeltaParams p;
   bool steps, chunks, fused;
-  size_t off_k, off_t, off_scal, bytes;
+  size_t off_k, off_t, off_scal, off_seq, bytes;
 };
 
 evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
@@ -65,7 +65,7 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.a = *a;
   d.p.share = a->heads_v / a->heads_k;
   d.p.len = a->seq_offsets ? -1 : (int)(a->n_tokens / a->n_seq);
-  d.p.slots_total = (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
+  d.p.slots_total = d.p.len >= 0 ? a->n_seq * ((d.p.len + kDeltaChunk - 1) / kDeltaChunk) : (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
   d.p.dkp = a->d_k <= 64 ? 64 : a->d_k <= 128 ? 128 : 256;
   if (a->dtype == EVCONV_F32 && a->d_k <= 128) d.p.dkp = (a->d_k + 31) / 32 * 32;  // (its products are six times as many)
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
@@ -74,7 +74,7 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.short_len = d.p.len < 0 ? kShortRagged : one_launch ? kShortFused : kShort;
   d.steps = d.p.len < 0 || d.p.len <= d.p.short_len;
   d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
-  d.off_k = d.off_t = d.off_scal = d.bytes = 0;
+  d.off_k = d.off_t = d.off_scal = d.off_seq = d.bytes = 0;
   d.fused = d.chunks && one_launch;
   if (d.chunks) {
     const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8 * ((a->d_v + 15) / 16);
@@ -86,7 +86,8 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
     d.off_k = (d.bytes + 255) / 256 * 256;
     d.off_t = d.off_k + (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);
     d.off_scal = d.off_t + (size_t)d.p.slots_total * a->heads_v * delta_frag_t_bytes(a->dtype);
-    d.bytes = d.off_scal + (size_t)d.p.slots_total * a->heads_v * kDeltaScalars * sizeof(float);
+    d.off_seq = d.off_scal + (size_t)d.p.slots_total * a->heads_v * kDeltaScalars * sizeof(float);
+    d.bytes = d.off_seq + (d.p.len < 0 ? (size_t)d.p.slots_total * sizeof(int) : 0);
   }
   return EVCONV_OK;
 }
@@ -154,6 +155,7 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
     d.p.frag_k = (char*)workspace + d.off_k;
     d.p.frag_t = (char*)workspace + d.off_t;
     d.p.scal = (float*)((char*)workspace + d.off_scal);
+    if (d.p.len < 0) d.p.slot_seq = (int*)((char*)workspace + d.off_seq);
   }
   if (d.steps && (args->n_tokens || args->state_out)) launch_delta_steps(d.p, (hipStream_t)hip_stream);
   if (d.fused) launch_delta_fused(d.p, (hipStream_t)hip_stream);

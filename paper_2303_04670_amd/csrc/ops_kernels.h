@@ -20,7 +20,7 @@ struct DeltaParams {
   int share;        // value heads per key head
   int len;          // tokens of every sequence, or -1: seq_offsets
   int short_len;    // sequences of up to so many tokens go token by token
-  int slots_total;  // chunk slots: n_tokens / kDeltaChunk + n_seq
+  int slots_total;  // chunk slots that the sequences have together, at most
   int dkp;          // d_k, rounded up to whole 32
   int vec;          // q, k rows may be read in 16-byte loads
   int vec_v;        // v rows too, and o rows written in 8-byte stores
@@ -28,6 +28,7 @@ struct DeltaParams {
   char* frag_k;     // per chunk slot and key head: K, Q and K' as matrix-core operands
   char* frag_t;     // per chunk slot and value head: T and P
   float* scal;      // per chunk slot and value head: kDeltaScalars
+  int* slot_seq;    // per chunk slot: the sequence whose it is (seq_offsets only; anything where it is nobody's)
   int segs, seg_chunks;   // segments of a sequence (1: whole), chunks of one
   float *trans, *start0;  // what segments do to the state, the first one's start
 };

@@ -299,6 +299,32 @@ def test_delta_rule_offsets_out_of_order_stay_inside():
     assert torch.equal(s[1], d["state"][1]) and torch.equal(s[3], d["state"][3])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 32), (1, 1, 136, 20)])
+@pytest.mark.parametrize("at", [[100, 230, 300], [64, 70, 400], [200] + list(range(200, 1000, 11)), [900, 50, 200, 203, 1000], [0, 70, 2000000000, 2000000000],
+                                [-5, 70, 1000], [500, 500, 500, 100, 400, 900, 0]], ids=lambda at: f"{at[0]}-{at[1]}-{len(at) - 1}")
+def test_delta_rule_offsets_that_start_anywhere(at, hk, hv, dk, dv, dtype):
+    """Offsets of a part of the tokens (a slice of more offsets), a descending pair in front, values out of range: every sequence is
+    right, and tokens of none keep what stands in the output."""
+    torch, ops = torch_ops()
+    n = 1000
+    x = delta_inputs(18 + len(at), n, len(at) - 1, hk, hv, dk, dv, dtype, True)
+    d = {name: a.cuda() for name, a in x.items()}
+    out = torch.full((n, hv, dv), 5.0, dtype=d["v"].dtype, device="cuda")
+    o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], seq_offsets=torch.tensor(at, dtype=torch.int32).cuda(), out=out,
+                          normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
+    inside = np.clip(at, 0, n)
+    spans = [(int(a), max(int(b - a), 0)) for a, b in zip(inside, inside[1:])]
+    c = numbers(x)
+    want_o, want_s = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], c["state"], spans, dk ** -0.5, True, c["a_scale"], c["dt_bias"])
+    some = np.zeros(n, bool)
+    for first, length in spans:
+        some[first:first + length] = True
+    close(o[torch.from_numpy(some)], want_o[some], dtype == "bf16")
+    assert (o[torch.from_numpy(~some)] == 5.0).all()
+    close(s, want_s)
+
+
 @pytest.mark.parametrize("length", [1, 100])
 def test_delta_rule_on_another_stream_and_in_a_graph(length):
     torch, ops = torch_ops()
