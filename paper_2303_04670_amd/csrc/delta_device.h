@@ -23,9 +23,12 @@ __device__ __forceinline__ Span span_of(const DeltaParams& p, int seq) {
   const int a = min(max(p.a.seq_offsets[seq], 0), n), b = min(max(p.a.seq_offsets[seq + 1], 0), n);
   return {a, max(b - a, 0)};
 }
-// First chunk slot of a sequence: no two sequences' slots meet, and none is behind slots_total (n_tokens / C + n_seq; of equal lengths
-// their chunks).
-__device__ __forceinline__ int first_slot(const DeltaParams& p, const Span& s, int seq) { return p.len >= 0 ? seq * ((p.len + C - 1) / C) : s.first / C + seq; }
+// First chunk slot of a long sequence (one in chunks): no two sequences' slots meet, and none is behind slots_total (plan_delta).  Of
+// lengths of their own, behind s.first / C and one for every long sequence that can stand before this one: at most seq, and at most
+// s.first / (kDeltaShortRagged + 1).  (From one long sequence to the next the first grows by len / C and the second by one at least.)
+__device__ __forceinline__ int first_slot(const DeltaParams& p, const Span& s, int seq) {
+  return p.len >= 0 ? seq * ((p.len + C - 1) / C) : s.first / C + min(seq, s.first / (kDeltaShortRagged + 1));
+}
 
 // Offset of a sequence's state, or -1: it has none.
 __device__ __forceinline__ int64_t state_at(const DeltaParams& p, int seq, int head) {

@@ -2,6 +2,7 @@
 // kernels, launches on the caller's stream.
 #include "ops_kernels.h"
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -36,7 +37,7 @@ bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token
 // tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 128, 12 tokens 25 / 27, 77 / 128.
 // Of calls with lengths of their own, whose chunks wait for the launch of the tokens (24 sequences of up to 700 tokens, 6 heads of
 // 80 x 112, fp32: for 24 us at 12 tokens, 12 at 4), fewer.
-constexpr int kShortFused = 6, kShort = 12, kShortRagged = 4;
+constexpr int kShortFused = 6, kShort = 12;
 
 struct DeltaPlan {
   DeltaParams p;
@@ -65,13 +66,15 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.a = *a;
   d.p.share = a->heads_v / a->heads_k;
   d.p.len = a->seq_offsets ? -1 : (int)(a->n_tokens / a->n_seq);
-  d.p.slots_total = d.p.len >= 0 ? a->n_seq * ((d.p.len + kDeltaChunk - 1) / kDeltaChunk) : (int)(a->n_tokens / kDeltaChunk) + a->n_seq;
   d.p.dkp = a->d_k <= 64 ? 64 : a->d_k <= 128 ? 128 : 256;
   if (a->dtype == EVCONV_F32 && a->d_k <= 128) d.p.dkp = (a->d_k + 31) / 32 * 32;  // (its products are six times as many)
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
   d.p.vec_v = a->d_v % 8 == 0 && wide(a->dtype, a->v) && aligned(a->o, 8) && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0;
   const bool one_launch = delta_fused_supported(d.p);
-  d.p.short_len = d.p.len < 0 ? kShortRagged : one_launch ? kShortFused : kShort;
+  d.p.short_len = d.p.len < 0 ? kDeltaShortRagged : one_launch ? kShortFused : kShort;
+  // (room for the sequences that can be in chunks, not for all: a call of single tokens with offsets has few)
+  const int n = (int)a->n_tokens;
+  d.p.slots_total = d.p.len >= 0 ? a->n_seq * ((d.p.len + kDeltaChunk - 1) / kDeltaChunk) : n / kDeltaChunk + std::min(a->n_seq, n / (kDeltaShortRagged + 1));
   d.steps = d.p.len < 0 || d.p.len <= d.p.short_len;
   d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
   d.off_k = d.off_t = d.off_scal = d.off_seq = d.bytes = 0;

@@ -299,6 +299,19 @@ def test_delta_rule_offsets_out_of_order_stay_inside():
     assert torch.equal(s[1], d["state"][1]) and torch.equal(s[3], d["state"][3])
 
 
+@pytest.mark.parametrize("dtype,dk", [("f32", 64), ("bf16", 136)])
+@pytest.mark.parametrize("kind", ["fives", "mixed", "random", "few"])
+def test_delta_rule_chunks_of_many_sequences(kind, dtype, dk):
+    """Sequences just long enough for a chunk of their own, packed as closely as they can be."""
+    rng = np.random.default_rng(4)
+    lens = {"fives": [5] * 70, "mixed": [5, 4, 5, 1, 64, 0, 65, 5, 5, 63, 4, 4, 4, 128, 5] * 3, "random": rng.integers(0, 14, 120).tolist(),
+            "few": [5, 600, 5, 0, 700]}[kind]
+    x = delta_inputs(19, sum(lens), len(lens), 1, 2, dk, 24, dtype, True)
+    o, s, want_o, want_s = run_delta(x, lens)
+    close(o, want_o, dtype == "bf16")
+    close(s, want_s)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 32), (1, 1, 136, 20)])
 @pytest.mark.parametrize("at", [[100, 230, 300], [64, 70, 400], [200] + list(range(200, 1000, 11)), [900, 50, 200, 203, 1000], [0, 70, 2000000000, 2000000000],

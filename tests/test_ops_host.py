@@ -71,6 +71,20 @@ def test_delta_rule_workspace():
     assert L.evconv_delta_rule(None, None, 0, None) == ev.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("n", [256, 4096, 65535])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_delta_rule_workspace_of_single_tokens_with_offsets(n, dtype):
+    """Room for the chunks that so many tokens can have: sequences of up to four go token by token, so at most a fifth of the tokens begin one."""
+    kw = dict(dtype=dtype, heads_k=8, heads_v=16, d_k=192, d_v=128)  # (keys of which both types need a workspace)
+    one, some = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    L = ops._calls()
+    assert L.evconv_delta_rule_workspace(ctypes.byref(delta_args(n_tokens=64, n_seq=1, n_slots=1, **kw)), ctypes.byref(one)) == ev.OK
+    assert L.evconv_delta_rule_workspace(ctypes.byref(delta_args(n_tokens=n, n_seq=n, n_slots=n, seq_offsets=FAKE, **kw)), ctypes.byref(some)) == ev.OK
+    assert 0 < some.value <= (n // 64 + n // 5 + 1) * (one.value + 512)
+    assert L.evconv_delta_rule_workspace(ctypes.byref(delta_args(n_tokens=n * 64, n_seq=1, n_slots=1, seq_offsets=FAKE, **kw)), ctypes.byref(some)) == ev.OK
+    assert some.value <= (n + 1) * (one.value + 512)  # (one long sequence: its chunks)
+
+
 def norm_args(**kw):
     a = ops.NormArgs(abi_version=ops.ABI_VERSION, dim=512, group=512, rows=4, eps=1e-6, x=FAKE, branch=FAKE, x_out=FAKE,
                      x_stride=512, branch_stride=512, x_out_stride=512)
