@@ -74,7 +74,7 @@ typedef struct {
   evconv_heads q, k, v, gate, beta;
   void* o;                    /* [n_tokens][heads_v][d_v] */
   int64_t o_token_stride, o_head_stride;
-  const float *a_scale, *dt_bias; /* fp32 [heads_v] each; EVCONV_DELTA_RAW_GATES only */
+  const float *a_scale, *dt_bias; /* fp32 [heads_v] each; EVCONV_DELTA_RAW_GATES only (then without tokens too) */
   const int32_t* seq_offsets; /* [n_seq + 1] ascending token indices, from 0 to n_tokens; sequence i is tokens
                                * [offsets[i], offsets[i+1]).  NULL: n_seq sequences of n_tokens / n_seq
                                * (a multiple) tokens.  A pair that descends is an empty sequence, what is out of

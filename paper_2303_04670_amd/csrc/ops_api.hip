@@ -57,10 +57,8 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   if (a->n_tokens < 0 || (!a->seq_offsets && a->n_tokens % a->n_seq)) return refuse(EVCONV_ERR_SHAPE, "delta rule: %lld tokens for %d sequences", (long long)a->n_tokens, a->n_seq);
   if (a->n_tokens >= (1ll << 31) - 64) return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens", (long long)a->n_tokens);
   if ((a->state_in || a->state_out) && a->n_slots < (a->slots ? 0 : a->n_seq)) return refuse(EVCONV_ERR_SHAPE, "delta rule: %d state slots for %d sequences", a->n_slots, a->n_seq);
-  if (a->n_tokens) {
-    if (!a->q.data || !a->k.data || !a->v.data || !a->gate.data || !a->beta.data || !a->o) return refuse(EVCONV_ERR_INVALID_ARG, "delta rule: null tensor");
-    if ((a->flags & EVCONV_DELTA_RAW_GATES) && (!a->a_scale || !a->dt_bias)) return refuse(EVCONV_ERR_INVALID_ARG, "delta rule: raw gates without a_scale or dt_bias");
-  }
+  if ((a->flags & EVCONV_DELTA_RAW_GATES) && (!a->a_scale || !a->dt_bias)) return refuse(EVCONV_ERR_INVALID_ARG, "delta rule: raw gates without a_scale or dt_bias");
+  if (a->n_tokens && (!a->q.data || !a->k.data || !a->v.data || !a->gate.data || !a->beta.data || !a->o)) return refuse(EVCONV_ERR_INVALID_ARG, "delta rule: null tensor");
   DeltaPlan& d = *out;
   d.p = DeltaParams{};
   d.p.a = *a;

@@ -208,6 +208,21 @@ def test_delta_rule_without_states_and_without_tokens():
     assert o.shape == (0, 1, 32) and torch.equal(t, s) and t is not s
 
 
+@pytest.mark.parametrize("ragged", [False, True])
+def test_delta_rule_without_tokens_hands_the_states_on(ragged):
+    torch, ops = torch_ops()
+    x = delta_inputs(20, 4, 3, 1, 2, 32, 16, "f32", True)
+    d = {n: a.cuda() for n, a in x.items()}
+    tokens = [d[n][:0] for n in ("q", "k", "v", "gate", "beta")]
+    kw = dict(normalize=True, seq_offsets=offsets([0, 0, 0]) if ragged else None)
+    o, s = ops.delta_rule(*tokens, d["state"], a_scale=d["a_scale"], dt_bias=d["dt_bias"], **kw)
+    assert o.shape == (0, 2, 16) and s is not d["state"] and torch.equal(s, d["state"])
+    for given in (dict(a_scale=d["a_scale"]), dict(dt_bias=d["dt_bias"])):
+        with pytest.raises(ev.EvConvError) as e:
+            ops.delta_rule(*tokens, d["state"], **given, **kw)
+        assert e.value.status == ev.ERR_INVALID_ARG
+
+
 def test_delta_rule_state_behind_32_bits():
     """A slot whose first value is at index 2^31 and more of the cache."""
     torch, ops = torch_ops()

@@ -85,6 +85,18 @@ def test_delta_rule_workspace_of_single_tokens_with_offsets(n, dtype):
     assert some.value <= (n + 1) * (one.value + 512)  # (one long sequence: its chunks)
 
 
+@pytest.mark.parametrize("given", [dict(), dict(a_scale=FAKE), dict(dt_bias=FAKE)])
+@pytest.mark.parametrize("n", [0, 200])
+def test_delta_rule_raw_gates_need_their_parameters(n, given):
+    """Without tokens too: the states are handed on by the kernel that goes token by token, which reads them first."""
+    size = ctypes.c_size_t(77)
+    a = delta_args(n_tokens=n, flags=ops.DELTA_RAW_GATES, **given)
+    assert ops._calls().evconv_delta_rule_workspace(ctypes.byref(a), ctypes.byref(size)) == ev.ERR_INVALID_ARG and size.value == 77
+    assert ops._calls().evconv_delta_rule(ctypes.byref(a), FAKE, 1 << 40, None) == ev.ERR_INVALID_ARG
+    a.a_scale = a.dt_bias = FAKE
+    assert ops._calls().evconv_delta_rule_workspace(ctypes.byref(a), ctypes.byref(size)) == ev.OK
+
+
 def norm_args(**kw):
     a = ops.NormArgs(abi_version=ops.ABI_VERSION, dim=512, group=512, rows=4, eps=1e-6, x=FAKE, branch=FAKE, x_out=FAKE,
                      x_stride=512, branch_stride=512, x_out_stride=512)
