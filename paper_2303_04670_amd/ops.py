@@ -177,8 +177,8 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
     contiguous, the others may be strided (slices of one projection).  state: fp32 [slots, heads_v, d_k, d_v], None:
     zeros.  Sequences: seq_offsets (int32 [n_seq + 1]), or n_seq of equal length (by default as many as `slots`,
     else as states, else one).  slots: int32 [n_seq], which state a sequence continues, negative: none.
-    state_out: where the states go, may be `state`; by default a new tensor, with `slots` `state` itself.  scale: of o,
-    by default d_k ** -0.5.  normalize: q and k are divided by their norms first."""
+    state_out: where the states go, may be `state`; by default a new tensor (states of no sequence as in `state`), with
+    `slots` `state` itself.  Slots need one of the two.  scale: of o, by default d_k ** -0.5.  normalize: q and k are divided by their norms first."""
     if q.dim() != 3 or v.dim() != 3 or gate.dim() != 2:
         _refuse(ERR_SHAPE, f"q {tuple(q.shape)}, v {tuple(v.shape)}, gate {tuple(gate.shape)}: expected three, three and two dimensions")
     gpu, dtype, gate_dtype, q_shape, v_shape = v.get_device(), v.dtype, gate.dtype, q.shape, v.shape
@@ -204,11 +204,16 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
         n_seq = slots.numel() if slots is not None else state.shape[0] if state is not None and state.dim() else 1
     slots_at = _packed(slots, "slots", gpu, torch.int32, (n_seq,))
     some = state if state is not None else state_out
+    if some is None and slots is not None:
+        _refuse(ERR_INVALID_ARG, "slots without state and state_out: of how many states?")
     n_slots = some.shape[0] if some is not None and some.dim() else n_seq
     shape = (n_slots, hv, dk, dv)
     state_at = _packed(state, "state", gpu, f32, shape)
     if state_out is None:
-        state_out = state if state is not None and slots is not None else _like(state, shape, f32, gpu)
+        if slots is not None:
+            state_out = state
+        else:  # (the call writes the sequences' states; where there are more, the others are as they were)
+            state_out = state.clone() if n_slots > n_seq else _like(state, shape, f32, gpu)
     to_at = state_at if state_out is state else _packed(state_out, "state_out", gpu, f32, shape)
     if out is None:
         out = _like(v, v_shape, dtype, gpu)

@@ -208,6 +208,45 @@ def test_delta_rule_without_states_and_without_tokens():
     assert o.shape == (0, 1, 32) and torch.equal(t, s) and t is not s
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [1, 40])
+def test_delta_rule_new_states_of_more_slots_than_sequences(length, dtype):
+    """A new tensor of states has those of no sequence too: they stay as they were."""
+    torch, ops = torch_ops()
+    x = delta_inputs(21, 3 * length, 8, 1, 2, 64, 32, dtype, True)
+    d = {n: a.cuda() for n, a in x.items()}
+    before = d["state"].clone()
+    for kw in (dict(n_seq=3), dict(seq_offsets=offsets([length] * 3))):
+        junk = [torch.full_like(before, 7.0) for _ in range(4)]  # (what the new tensor may be made from)
+        del junk
+        o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], normalize=True, a_scale=d["a_scale"],
+                              dt_bias=d["dt_bias"], **kw)
+        c = numbers(x)
+        want_o, want_s = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], c["state"][:3], spans_of([length] * 3), 64 ** -0.5,
+                                            True, c["a_scale"], c["dt_bias"])
+        close(o, want_o, dtype == "bf16")
+        close(s[:3], want_s)
+        assert s is not d["state"] and torch.equal(s[3:], before[3:]) and torch.equal(d["state"], before)
+
+
+def test_delta_rule_slots_need_states():
+    """How many slots there are is known from `state` or `state_out` only."""
+    torch, ops = torch_ops()
+    x = delta_inputs(22, 2, 8, 1, 2, 64, 32, "f32", False)
+    d = {n: None if a is None else a.cuda() for n, a in x.items()}
+    slots = torch.tensor([5, 7], dtype=torch.int32).cuda()
+    tokens = (d["q"], d["k"], d["v"], d["gate"], d["beta"])
+    with pytest.raises(ev.EvConvError) as e:
+        ops.delta_rule(*tokens, slots=slots)
+    assert e.value.status == ev.ERR_INVALID_ARG
+    out = torch.full_like(d["state"], 5.0)
+    _, s = ops.delta_rule(*tokens, slots=slots, state_out=out)
+    c = numbers(x)
+    _, want = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], 0 * c["state"][:2], [(0, 1), (1, 1)], 64 ** -0.5)
+    close(s[[5, 7]], want)
+    assert s is out and (s[[0, 1, 2, 3, 4, 6]] == 5.0).all()
+
+
 @pytest.mark.parametrize("ragged", [False, True])
 def test_delta_rule_without_tokens_hands_the_states_on(ragged):
     torch, ops = torch_ops()
