@@ -3,6 +3,8 @@
 // chain of a launch, a read, one to five reductions and a write).  In fp32 it runs at 4.9 to 5.1 TB/s,
 // the rate of a large copy; in bf16 at 4.3 to 4.9: half the bytes to the same exponentials, roundings and
 // fp32 weights.  The sums go over a row twice (mean, then squares of differences), so no cancellation.
+#include <algorithm>
+
 #include "ops_device.h"
 #include "ops_kernels.h"
 
@@ -11,7 +13,8 @@ namespace {
 
 struct NormParams {
   evconv_norm_args a;
-  int lanes;  // threads to a group: a power of two that holds it in vectors of eight
+  int lanes;     // threads to a group: a power of two that holds it in vectors of eight
+  int64_t row0;  // first row of this launch
 };
 
 // Sum over `lanes` neighbouring lanes (a power of two up to 64), the same in all of them.
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
   __shared__ float s_part[T / 64];
   const evconv_norm_args& a = p.a;
   const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t row = T == 64 ? (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t row = p.row0 + (T == 64 ? (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6) : blockIdx.x);
   if (row >= a.rows) return;  // (T > 64: never, so every thread of a row meets its barriers)
   const int dim = a.dim, group = GROUPED ? a.group : dim;
   int at[NV], left[NV], in_group[NV];  // first value of a vector, how many are inside, its place in the group
@@ -249,13 +252,16 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void block_norm(NormParams p) {
 }
 
 template <bool BF16, bool VEC, int T, int NV>
-void start(const NormParams& p, hipStream_t s) {
+void start(NormParams p, hipStream_t s) {
   // waves of a workgroup: one where there are few rows, so that they spread over the chip
   const int per = T > 64 ? 1 : p.a.rows >= 2048 ? 4 : 1;
-  const unsigned grid = (unsigned)((p.a.rows + per - 1) / per);
   const int threads = T > 64 ? T : 64 * per;
-  if (p.a.group == p.a.dim) block_norm<BF16, VEC, T, NV, false><<<grid, threads, 0, s>>>(p);
-  else block_norm<BF16, VEC, T, NV, true><<<grid, threads, 0, s>>>(p);
+  const int64_t most = kMostThreads / threads * per;  // rows of a launch
+  for (; p.row0 < p.a.rows; p.row0 += most) {
+    const unsigned grid = (unsigned)((std::min(most, p.a.rows - p.row0) + per - 1) / per);
+    if (p.a.group == p.a.dim) block_norm<BF16, VEC, T, NV, false><<<grid, threads, 0, s>>>(p);
+    else block_norm<BF16, VEC, T, NV, true><<<grid, threads, 0, s>>>(p);
+  }
 }
 
 // How a row is laid over threads, by its vectors.  More values to a thread save barriers and shared reductions; fewer leave
@@ -285,7 +291,7 @@ static int group_lanes(const evconv_norm_args& a) {
 int block_norm_vectors(const evconv_norm_args& a) { return a.group == a.dim ? (a.dim + 7) / 8 : a.dim / a.group * group_lanes(a); }
 
 void launch_block_norm(const evconv_norm_args& a, bool vec, hipStream_t s) {
-  const NormParams p{a, group_lanes(a)};
+  const NormParams p{a, group_lanes(a), 0};
   if (a.dtype == EVCONV_BF16) vec ? start_size<true, true>(p, s) : start_size<true, false>(p, s);
   else vec ? start_size<false, true>(p, s) : start_size<false, false>(p, s);
 }

@@ -9,6 +9,9 @@
 
 namespace evk {
 
+// Threads of one launch, at most: HIP counts them in 32 bits.
+constexpr int64_t kMostThreads = 1ll << 31;
+
 // Text of evconv_last_error(NULL) (evconv_api.hip).
 void set_call_error(const char* text) noexcept;
 

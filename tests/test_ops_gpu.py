@@ -498,6 +498,20 @@ def test_block_norm_strides_and_in_place():
         assert torch.equal(wide[:, pad + 264:pad + 528], d["branch"])
 
 
+def test_block_norm_of_more_rows_than_one_launch_takes():
+    """2^26 rows and some: with 64 threads to a row more than the 2^32 threads that a launch can have."""
+    torch, ops = torch_ops()
+    n, dim = (1 << 26) + 37, 8
+    x = torch.randn(1 << 20, dim, device="cuda").bfloat16().repeat(65, 1)[:n]
+    x[-37:] *= 3
+    w = torch.rand(dim, device="cuda") + 0.5
+    got = ops.block_norm(x, pre_norm=True, pre_weight=w, want="h").h
+    part = ops.block_norm(x[:1 << 20].contiguous(), pre_norm=True, pre_weight=w, want="h").h
+    for i in range(64):
+        assert torch.equal(got[i << 20:(i + 1) << 20], part), i
+    close(got[-37:], ops_ref.block_norm(x[-37:].float().cpu().numpy(), pre_norm=True, pre_weight=w.cpu().numpy())[1], True)
+
+
 def test_block_norm_rows_of_zeros_and_bad_values():
     torch, ops = torch_ops()
     x = torch.randn(6, 300, generator=torch.Generator().manual_seed(1))
