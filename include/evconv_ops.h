@@ -86,7 +86,9 @@ typedef struct {
   float* state_out;           /* the same, may be state_in; or NULL.  Slots of no sequence stay as they are */
 } evconv_delta_args;
 
-/* Bytes of device workspace the call needs: 0 where nothing passes between launches (a few tokens to a
+/* A call whose largest launch would have 2^32 threads or more (some millions of sequences times heads: a launch has 64 to 1536 to
+ * each) is EVCONV_ERR_UNSUPPORTED.
+ * Bytes of device workspace the call needs: 0 where nothing passes between launches (a few tokens to a
  * sequence; bf16 keys of up to 128 channels, unless few sequences of some length are split over the chip). */
 evconv_status evconv_delta_rule_workspace(const evconv_delta_args* args, size_t* bytes);
 /* `workspace`: 256-byte aligned, free to be used again once the call's kernels are done. */

@@ -256,7 +256,7 @@ void start(NormParams p, hipStream_t s) {
   // waves of a workgroup: one where there are few rows, so that they spread over the chip
   const int per = T > 64 ? 1 : p.a.rows >= 2048 ? 4 : 1;
   const int threads = T > 64 ? T : 64 * per;
-  const int64_t most = kMostThreads / threads * per;  // rows of a launch
+  const int64_t most = kMostThreads / 2 / threads * per;  // rows of a launch
   for (; p.row0 < p.a.rows; p.row0 += most) {
     const unsigned grid = (unsigned)((std::min(most, p.a.rows - p.row0) + per - 1) / per);
     if (p.a.group == p.a.dim) block_norm<BF16, VEC, T, NV, false><<<grid, threads, 0, s>>>(p);

@@ -19,6 +19,7 @@
 // rows, applied to the sums), everything else that reaches the state as three bf16 parts, which hold
 // 24 bits; outputs of bf16 calls are summed from two parts.  G is summed in 64 bits: the difference of two
 // sums over a chunk would lose the bits that its exponential needs.
+#include <algorithm>
 #include <type_traits>
 
 #include "delta_device.h"
@@ -752,10 +753,16 @@ void chunks_type(const DeltaParams& p, hipStream_t s) {
 size_t delta_frag_k_bytes(int dtype, int dkp) { return (size_t)3 * 4 * (dkp / 32) * parts_in(dtype == EVCONV_F32) * kFrag; }
 size_t delta_frag_t_bytes(int dtype) { return (size_t)kTri * kFrag * (3 + parts_out(dtype == EVCONV_F32)); }
 
+int64_t delta_steps_threads(const DeltaParams& p) { return ((int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 31) / 32) + 3) / 4 * 256; }
+int64_t delta_chunks_threads(const DeltaParams& p) {
+  // delta_prepare; delta_chain, of eight strips to a workgroup (the first pass over segments has the keys' strips, too)
+  const int strips = (p.a.d_v + 15) / 16 + (p.segs > 1 ? (p.a.d_k + 15) / 16 : 0);
+  return std::max((int64_t)p.slots_total * p.a.heads_v * 256, (int64_t)p.a.n_seq * p.a.heads_v * p.segs * ((strips + 7) / 8) * 512);
+}
+
 void launch_delta_steps(const DeltaParams& p, hipStream_t s) {
   const bool vec = p.vec && p.a.d_v % 4 == 0 && ((uintptr_t)p.a.state_in | (uintptr_t)p.a.state_out) % 16 == 0;
-  const int64_t waves = (int64_t)p.a.n_seq * p.a.heads_v * ((p.a.d_v + 31) / 32);
-  const unsigned grid = (unsigned)((waves + 3) / 4);
+  const unsigned grid = (unsigned)(delta_steps_threads(p) / 256);
   if (p.a.dtype == EVCONV_BF16) steps_type<true>(p, vec, grid, s);
   else steps_type<false>(p, vec, grid, s);
 }

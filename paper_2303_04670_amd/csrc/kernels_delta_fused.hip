@@ -914,6 +914,11 @@ bool delta_fused_supported(const DeltaParams& p) {
          near(p.a.v.token_stride) && near(p.a.o_token_stride) && near(p.a.gate.token_stride) && near(p.a.beta.token_stride);
 }
 
+int64_t delta_fused_threads(const DeltaParams& p) {
+  const int waves = delta_fused_waves(p), strips = (p.a.d_v + 15) / 16 + (p.segs > 1 ? (p.a.d_k + 15) / 16 : 0);  // (with the first pass' strips of keys)
+  return (int64_t)p.a.n_seq * p.a.heads_v * p.segs * ((strips + waves - 1) / waves) * (waves + 4) * 64;
+}
+
 // A workgroup of the unsplit launch per head and eight (four) strips; where they leave most of the chip idle and sequences are
 // long, segments, as many as give every compute unit one, of four chunks at least.  Three segments cost what they save: every
 // chunk is worked on twice, the first time with twice the columns.  us, whole and in segments, heads of 128 x 128 / 64 x 64:

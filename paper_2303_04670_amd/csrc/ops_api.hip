@@ -77,12 +77,9 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.chunks = d.p.len < 0 ? a->n_tokens > d.p.short_len : !d.steps;
   d.off_k = d.off_t = d.off_scal = d.off_seq = d.bytes = 0;
   d.fused = d.chunks && one_launch;
-  if (d.chunks) {
-    const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8 * ((a->d_v + 15) / 16);
-    if (pairs >= 1ll << 31 || (int64_t)d.p.slots_total * a->heads_v >= 1ll << 31)
-      return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens of %d sequences and %d heads are more than one launch takes", (long long)a->n_tokens, a->n_seq, a->heads_v);
-  }
   if (d.chunks) d.bytes = plan_delta_segments(d.p, d.fused);
+  if ((d.steps && delta_steps_threads(d.p) > kMostThreads) || (d.chunks && (d.fused ? delta_fused_threads(d.p) : delta_chunks_threads(d.p)) > kMostThreads))
+    return refuse(EVCONV_ERR_UNSUPPORTED, "delta rule: %lld tokens of %d sequences and %d heads are more than one launch takes", (long long)a->n_tokens, a->n_seq, a->heads_v);
   if (d.chunks && !d.fused) {
     d.off_k = (d.bytes + 255) / 256 * 256;
     d.off_t = d.off_k + (size_t)d.p.slots_total * a->heads_k * delta_frag_k_bytes(a->dtype, d.p.dkp);

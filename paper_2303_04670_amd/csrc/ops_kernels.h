@@ -10,7 +10,7 @@
 namespace evk {
 
 // Threads of one launch, at most: HIP counts them in 32 bits.
-constexpr int64_t kMostThreads = 1ll << 31;
+constexpr int64_t kMostThreads = (1ll << 32) - 1;
 
 // Text of evconv_last_error(NULL) (evconv_api.hip).
 void set_call_error(const char* text) noexcept;
@@ -40,6 +40,10 @@ struct DeltaParams {
 size_t delta_frag_k_bytes(int dtype, int dkp);
 size_t delta_frag_t_bytes(int dtype);
 constexpr int kDeltaScalars = 512;  // four factors of every token, the decay; up to whole 1 KB
+// Threads of the largest launch of each way.
+int64_t delta_steps_threads(const DeltaParams& p);
+int64_t delta_chunks_threads(const DeltaParams& p);
+int64_t delta_fused_threads(const DeltaParams& p);
 void launch_delta_steps(const DeltaParams& p, hipStream_t s);
 void launch_delta_chunks(const DeltaParams& p, hipStream_t s);
 // chunks in one launch

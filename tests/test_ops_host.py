@@ -97,6 +97,25 @@ def test_delta_rule_raw_gates_need_their_parameters(n, given):
     assert ops._calls().evconv_delta_rule_workspace(ctypes.byref(a), ctypes.byref(size)) == ev.OK
 
 
+@pytest.mark.parametrize("kw,few,many", [
+    # single tokens: 64 threads to a sequence, head and 32 columns
+    (dict(n_tokens=65535, d_v=64), 512, 1024),
+    # with offsets the chunks' launch stands behind it: eight waves to each, which end at once
+    (dict(n_tokens=65535, d_v=64, seq_offsets=FAKE), 64, 1024),
+    # chunks: eight (twelve) waves to a sequence and head of one launch
+    (dict(n_tokens=7 * 65535, dtype=1), 128, 256), (dict(n_tokens=7 * 65535, dtype=1, seq_offsets=FAKE), 128, 256), (dict(n_tokens=7 * 65535, dtype=1, d_v=65), 64, 128),
+    (dict(n_tokens=13 * 65535), 128, 256), (dict(n_tokens=13 * 65535, d_k=200, d_v=200), 64, 128)])
+def test_delta_rule_refuses_more_than_a_launch_takes(kw, few, many):
+    """HIP counts a launch's threads in 32 bits; nothing has been enqueued when a call is refused for it."""
+    n, kw = ctypes.c_size_t(77), dict(n_seq=65535, n_slots=65535, **kw)
+    L = ops._calls()
+    assert L.evconv_delta_rule_workspace(ctypes.byref(delta_args(heads_k=few, heads_v=few, **kw)), ctypes.byref(n)) == ev.OK
+    for heads in (many, 1024):
+        a = delta_args(heads_k=heads, heads_v=heads, **kw)
+        assert L.evconv_delta_rule_workspace(ctypes.byref(a), ctypes.byref(n)) == ev.ERR_UNSUPPORTED
+        assert L.evconv_delta_rule(ctypes.byref(a), FAKE, 1 << 50, None) == ev.ERR_UNSUPPORTED
+
+
 def norm_args(**kw):
     a = ops.NormArgs(abi_version=ops.ABI_VERSION, dim=512, group=512, rows=4, eps=1e-6, x=FAKE, branch=FAKE, x_out=FAKE,
                      x_stride=512, branch_stride=512, x_out_stride=512)
