@@ -144,8 +144,8 @@ typedef struct {
   int32_t abi_version;  /* EVCONV_OPS_ABI_VERSION */
   int32_t dtype;        /* of y: EVCONV_F32 or EVCONV_BF16 */
   int32_t act;          /* evconv_act */
-  int32_t n, k;         /* k at most 131072: a sum of more products may not fit 32 bits */
-  int64_t m;            /* below 2^31 */
+  int32_t n, k;         /* n at most 2^24; k at most 131072: a sum of more products may not fit 32 bits */
+  int64_t m;            /* below 2^31, and fewer than 2^23 tiles of 256 x 256 in y */
   const int8_t *a, *b;
   int64_t a_stride, b_stride; /* bytes */
   const float *a_scale, *b_scale, *bias; /* fp32 [m], [n], [n] or NULL */

@@ -120,7 +120,7 @@ evconv_status check_quant(const evconv_quant_args* a) {
   if (!float_type(a->dtype)) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: dtype %d", a->dtype);
   if (a->act < EVCONV_ACT_NONE || a->act > EVCONV_ACT_TANH) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: act %d", a->act);
   if (a->m < 0 || a->n < 1 || a->k < 1) return refuse(EVCONV_ERR_SHAPE, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
-  if (a->m >= 1ll << 31 || a->k > 131072 || a->n > 1 << 24 || ((a->m + 255) / 256) * ((a->n + 255) / 256) >= 1ll << 31) return refuse(EVCONV_ERR_UNSUPPORTED, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
+  if (a->m >= 1ll << 31 || a->k > 131072 || a->n > 1 << 24 || ((a->m + 255) / 256) * ((a->n + 255) / 256) * 512 > kMostThreads) return refuse(EVCONV_ERR_UNSUPPORTED, "quantised product: %lld x %d x %d", (long long)a->m, a->n, a->k);
   if (!a->m) return EVCONV_OK;
   if (!a->a || !a->b || !a->a_scale || !a->b_scale || !a->y) return refuse(EVCONV_ERR_INVALID_ARG, "quantised product: null tensor");
   const int64_t row = (a->k + 127) / 128 * 128;

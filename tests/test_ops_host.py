@@ -158,6 +158,13 @@ def test_quant_matmul_refusals(change, status):
     assert ev.lib().evconv_last_error(None).decode().startswith("quantised product")
 
 
+@pytest.mark.parametrize("m,n", [((1 << 31) - 1, 1), (1 << 23, 1 << 16), (1, (1 << 24) + 1)])
+def test_quant_matmul_refuses_more_than_a_launch_takes(m, n):
+    """Tiles of 256 x 256 with 512 threads each, fewer than 2^32 together; at most 2^24 columns."""
+    a = quant_args(m=m, n=n, y_stride=n)
+    assert ops._calls().evconv_quant_matmul(ctypes.byref(a), None) == ev.ERR_UNSUPPORTED
+
+
 def test_nothing_to_do_is_ok():
     assert ops._calls().evconv_block_norm(ctypes.byref(norm_args(rows=0, x=None, branch=None)), None) == ev.OK
     assert ops._calls().evconv_quant_matmul(ctypes.byref(quant_args(m=0, a=None, y=None)), None) == ev.OK
