@@ -49,8 +49,8 @@ extern "C" {
  *
  * A value that is not finite makes what depends on it NaN (or infinite): outputs of its sequence and
  * head from its token on, and the state; never an earlier token's output or another sequence's.
- * A finite value of 3.39e38 and more counts as infinite, and so may a query or a key whose sum of squares
- * is beyond fp32. */
+ * A finite value of 3.39e38 and more counts as infinite, and so does a query or a key whose sum of squares is beyond
+ * fp32 (without EVCONV_DELTA_NORMALIZE: may). */
 #define EVCONV_DELTA_NORMALIZE 1u
 #define EVCONV_DELTA_RAW_GATES 2u
 

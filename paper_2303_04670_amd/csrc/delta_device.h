@@ -56,6 +56,9 @@ __device__ __forceinline__ Gates gates_of(const DeltaParams& p, int64_t token, i
                     raw ? p.a.a_scale[head] : 0.0f, raw ? p.a.dt_bias[head] : 0.0f);
 }
 
+// What a row is divided by, from its sum of squares; NaN beyond fp32: the division would make it zeros.
+__device__ __forceinline__ float norm_of(float squares) { return squares < INFINITY ? sqrtf(squares + 1e-6f) : NAN; }
+
 // Operands of the 16 x 16 x 32 matrix instruction: a lane (m = lane % 16, g = lane / 16) holds row m of the left
 // operand (column m of the right one) at the contraction's places 8 g .. 8 g + 7, and column m, rows
 // 4 g .. 4 g + 3 of the result.  Let block b of a result's rows hold, at its row 4 g + i, the row

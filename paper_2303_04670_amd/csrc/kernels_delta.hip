@@ -111,8 +111,8 @@ __global__ __launch_bounds__(256) void delta_step(DeltaParams p) {
       for (int j = 0; j < 11; ++j) sum[j] += __shfl_xor(sum[j], d);
     float rk = 1.0f, rq = a.scale;
     if (a.flags & EVCONV_DELTA_NORMALIZE) {
-      rk = 1.0f / sqrtf(sum[9] + 1e-6f);
-      rq = a.scale / sqrtf(sum[10] + 1e-6f);
+      rk = 1.0f / norm_of(sum[9]);
+      rq = a.scale / norm_of(sum[10]);
     }
     float out[4];
 #pragma unroll
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
     const float v = m & 2 ? (m & 1 ? qq[3] : qq[2]) : (m & 1 ? qq[1] : qq[0]);
     if (m >> 2 == g) {
       const bool normalize = a.flags & EVCONV_DELTA_NORMALIZE;
-      s_rk[row] = normalize ? 1.0f / sqrtf(u + 1e-6f) : 1.0f;
-      s_rq[row] = normalize ? a.scale / sqrtf(v + 1e-6f) : a.scale;
+      s_rk[row] = normalize ? 1.0f / norm_of(u) : 1.0f;
+      s_rq[row] = normalize ? a.scale / norm_of(v) : a.scale;
     }
   }
   __syncthreads();

@@ -198,7 +198,7 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
   const float square = s_rk[lane];
   const uint64_t wrong = __ballot(!(fabsf(square) < INFINITY) || !(fabsf(gate.beta) < INFINITY) || !(fabsf(hi) < INFINITY));
   const int bad = wrong ? (int)__builtin_ctzll(wrong) : C;
-  const float rk = normalize ? 1.0f / sqrtf(square + 1e-6f) : 1.0f;
+  const float rk = normalize ? 1.0f / norm_of(square) : 1.0f;
   s_rk[lane] = rk;
   const float beta_rk = lane < bad ? gate.beta * rk : 0.0f;
   __builtin_amdgcn_sched_barrier(0);
@@ -212,7 +212,7 @@ __device__ __forceinline__ void prepare_products(const DeltaParams& p, char* slo
     const bool good = i < bad;
     float rq = a.scale;
     if (!TRANS) {
-      if (normalize) rq = a.scale / sqrtf(__shfl(diagonal(q), (m >> 2) << 4 | m) + 1e-6f);
+      if (normalize) rq = a.scale / norm_of(__shfl(diagonal(q), (m >> 2) << 4 | m));
       if (g == 0) scal[2 * C + i] = rq * __builtin_amdgcn_exp2f(hi_i);
     }
     // a lane holds of block j the row i = place(bi, m) of A and P, columns j0 .. j0 + 3

@@ -340,6 +340,27 @@ def test_delta_rule_bad_values_reach_nothing_before_them(length, token, value, w
         assert not torch.isfinite(t[0, 1, :, 5]).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", ["q", "k"])
+@pytest.mark.parametrize("length,token", [(1, 0), (5, 3), (200, 0), (200, 70), (200, 199)])
+def test_delta_rule_norms_beyond_fp32(length, token, what, dtype):
+    """A query or a key whose sum of squares is beyond fp32 counts as infinite: NaN, not a vector of zeros."""
+    torch, ops = torch_ops()
+    x = delta_inputs(23, 2 * length, 2, 2, 2, 64, 32, dtype, True)
+    d = {n: a.cuda() for n, a in x.items()}
+    call = lambda: ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])
+    o, s = call()
+    d[what][token, 1, 5] = 3e19
+    p, t = call()
+    assert torch.equal(p[:, 0], o[:, 0]) and torch.equal(p[:token], o[:token]) and torch.equal(p[length:], o[length:])
+    assert torch.equal(t[:, 0], s[:, 0]) and torch.equal(t[1], s[1])
+    assert p[token, 1].isnan().all()
+    if what == "q":
+        assert torch.equal(t, s) and torch.equal(p[token + 1:], o[token + 1:])
+    else:
+        assert p[token:length, 1].isnan().all() and t[0, 1].isnan().all()
+
+
 def test_delta_rule_offsets_out_of_order_stay_inside():
     """Offsets that are not ascending or not in range are empty sequences or cut off: nothing outside is read or
     written, and the sequences that are well formed keep their values."""
