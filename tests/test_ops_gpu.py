@@ -340,6 +340,57 @@ def test_delta_rule_bad_values_reach_nothing_before_them(length, token, value, w
         assert not torch.isfinite(t[0, 1, :, 5]).all()
 
 
+@pytest.mark.parametrize("what", ["q", "k", "v", "gate", "beta", "state"])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("dtype,dk,dv", [("bf16", 64, 32), ("bf16", 128, 72), ("bf16", 37, 51), ("bf16", 200, 20), ("f32", 96, 40), ("f32", 200, 20)])
+def test_delta_rule_bad_values_in_chunks(dtype, dk, dv, value, what):
+    """As above for every kernel of the chunks: vectors and single values, keys in halves; tokens in both halves of a chunk, on its
+    ends, in a last chunk that is not whole, in a sequence that is one chunk; segments of a long sequence."""
+    torch, ops = torch_ops()
+    for length, tokens in ((200, [0, 31, 32, 63, 64, 150, 198]), (20, [13]), (3000, [1300])):
+        x = delta_inputs(24, 2 * length, 2, 2, 2, dk, dv, dtype, False)
+        d = {n: None if a is None else a.cuda() for n, a in x.items()}
+        call = lambda: ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"])
+        o, s = call()
+        for token in tokens:
+            at = {"q": (token, 1, 5), "k": (token, 1, 5), "v": (token, 1, 5), "gate": (token, 1), "beta": (token, 1), "state": (0, 1, 7, 5)}[what]
+            keep = d[what][at].clone()
+            d[what][at] = value
+            p, t = call()
+            d[what][at] = keep
+            where = (length, token)
+            assert torch.equal(p[:, 0], o[:, 0]) and torch.equal(t[:, 0], s[:, 0]), where
+            assert torch.equal(p[length:], o[length:]) and torch.equal(t[1], s[1]), where
+            if what in ("v", "state"):  # one column
+                rest = [c for c in range(dv) if c != 5]
+                assert torch.equal(p[:, :, rest], o[:, :, rest]) and torch.equal(t[..., rest], s[..., rest]), where
+            if what != "state":
+                assert torch.equal(p[:token], o[:token]), where
+            if what == "q":
+                assert torch.equal(t, s) and torch.equal(p[token + 1:], o[token + 1:]) and not torch.isfinite(p[token, 1]).any(), where
+            elif what != "gate" or np.isnan(value):
+                assert not torch.isfinite(t[0, 1, :, 5]).any() and not torch.isfinite(p[token if what != "state" else 0:length, 1, 5]).any(), where
+            if what == "gate" and value == -np.inf:  # forgets what was
+                assert torch.isfinite(p).all() and torch.isfinite(t).all(), where
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [("bf16", 64, 16), ("bf16", 128, 40), ("bf16", 37, 51), ("bf16", 144, 16), ("f32", 128, 72), ("f32", 37, 51)])
+@pytest.mark.parametrize("length", [9, 200, 3000])
+def test_delta_rule_decays_in_chunks(length, dtype, dk, dv):
+    """No decay, strong decay, a decay that forgets everything and tokens that do nothing, in both halves of a chunk."""
+    x = delta_inputs(25, 2 * length, 2, 1, 2, dk, dv, dtype, False)
+    x["gate"][::3] = 0.0
+    for first in range(4, 2 * length, 37):
+        x["gate"][first] = -np.inf
+        x["gate"][first + 1:first + 2, 1] = -3e38
+        x["gate"][first + 3:first + 4] = -90.0
+    x["beta"][::4] = 0.0
+    x["beta"][1::4] = 1.0
+    o, s, want_o, want_s = run_delta(x, [length] * 2, ragged=False)
+    close(o, want_o, dtype == "bf16")
+    close(s, want_s)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("what", ["q", "k"])
 @pytest.mark.parametrize("length,token", [(1, 0), (5, 3), (200, 0), (200, 70), (200, 199)])
