@@ -175,6 +175,30 @@ def test_delta_rule_reads_slices_of_a_projection(dtype):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("dk,dv", [(64, 32), (128, 40), (37, 51)])
+@pytest.mark.parametrize("which", ["q", "k", "v", "gate", "out"])
+def test_delta_rule_tokens_far_apart(which, dk, dv):
+    """More than 2^23 elements from token to token in one of the tensors: bf16 chunks in two launches."""
+    torch, ops = torch_ops()
+    lens, step = [70, 0, 20], (1 << 23) + 64
+    n = sum(lens)
+    x = delta_inputs(26, n, 3, 1, 2, dk, dv, "bf16", True)
+    d = {name: a.cuda() for name, a in x.items()}
+    d["out"] = torch.empty_like(d["v"])
+    room = torch.empty(n * step, dtype=torch.bfloat16, device="cuda")
+    far = room.as_strided(d[which].shape, (step,) + d[which].stride()[1:])
+    far.copy_(d[which])
+    d[which] = far
+    o, s = ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], seq_offsets=offsets(lens), out=d["out"], normalize=True,
+                          a_scale=d["a_scale"], dt_bias=d["dt_bias"])
+    c = numbers(x)
+    want_o, want_s = ops_ref.delta_rule(c["q"], c["k"], c["v"], c["gate"], c["beta"], c["state"], spans_of(lens), dk ** -0.5, True, c["a_scale"],
+                                        c["dt_bias"])
+    assert o is d["out"]
+    close(o, want_o, True)
+    close(s, want_s)
+
+
 def test_delta_rule_slots_and_states_in_place():
     torch, ops = torch_ops()
     lens = [3, 0, 70, 1, 20]
@@ -624,6 +648,24 @@ def test_quant_matmul(m, n, k, act, bias, dtype):
     assert np.array_equal(qa.scale.cpu().numpy(), want_a[1]) and np.array_equal(qb.scale.cpu().numpy(), want_b[1])
     y = ops.quant_matmul(qa, qb, bias=None if b is None else b.cuda(), act=act, out_dtype=torch.float32 if dtype == "f32" else torch.bfloat16)
     close(y, ops_ref.quant_matmul(*want_a, *want_b, None if b is None else b.numpy(), act), dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k,act,bias", [
+    (2500, 2600, 200, "tanh", True), (2433, 2569, 129, "none", False), (2500, 2600, 1, "relu", True),  # 128 x 128
+    (3500, 3600, 300, "none", True), (3329, 3585, 1153, "sigmoid", False), (50000, 33, 256, "relu", True), (40, 50000, 256, "none", True)])  # 256 x 256
+def test_quant_matmul_in_large_tiles(m, n, k, act, bias, dtype):
+    """From 384 tiles of 128 x 128 and 193 of 256 x 256 on; tiles that the ends cut, one row and column beyond a tile."""
+    torch, ops = torch_ops()
+    g = torch.Generator().manual_seed(m + n + k)
+    x, w = torch.randn(m, k, generator=g), torch.randn(n, k, generator=g) / k ** 0.5
+    b = torch.randn(n, generator=g) if bias else None
+    want_a, want_b = ops_ref.quantize_rows(x.numpy()), ops_ref.quantize_rows(w.numpy())
+    qa, qb = ops.quantize_rows(x.cuda()), ops.quantize_rows(w.cuda())
+    out = torch.full((m, n + 8), 9.0, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
+    y = ops.quant_matmul(qa, qb, bias=None if b is None else b.cuda(), act=act, out=out[:, :n])
+    close(y, ops_ref.quant_matmul(*want_a, *want_b, None if b is None else b.numpy(), act), dtype == "bf16")
+    assert (out[:, n:] == 9.0).all()
 
 
 @pytest.mark.parametrize("m", [2, 40, 300])
