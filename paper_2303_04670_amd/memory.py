@@ -21,6 +21,7 @@ import numpy as np
 import torch
 
 from . import ops
+from .evconv import ERR_INVALID_ARG, EvConvError
 
 
 class Layer(NamedTuple):
@@ -76,6 +77,8 @@ class Memory:
         """Features [windows, dim] -> [windows, n_out].  By default one window of every stream, in their order; with
         slots (int32 [n], a stream at most once; negative: nothing is remembered) one window of each of those; with
         seq_offsets (int32 [n + 1]) windows seq_offsets[i] .. seq_offsets[i + 1] are the next ones of stream slots[i]."""
+        if x.dtype != self.dtype:  # (found by the last call of a layer only, behind the one that rewrites its states)
+            raise EvConvError(ERR_INVALID_ARG, f"features are {x.dtype}, the memory's {self.dtype}")
         to = self.columns
         n_seq = None if slots is not None or seq_offsets is not None else self.n_streams
         rows = ops.block_norm(x, pre_norm=True, pre_weight=self.layers[0].pre_norm, want="q").q

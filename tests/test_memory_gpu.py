@@ -99,6 +99,21 @@ def test_streams_are_independent():
     assert not memory.states[0][3].any() and memory.states[0][4].any()
 
 
+@pytest.mark.parametrize("how", ["type", "width", "dimensions", "slots"])
+def test_a_refused_window_leaves_the_states(how):
+    torch, memory = make()
+    from paper_2303_04670_amd import evconv as ev
+    x = torch.randn(5, 96, device="cuda")
+    memory(x)
+    before = [s.clone() for s in memory.states]
+    bad, slots = {"type": (x.bfloat16(), None), "width": (x[:, :95], None), "dimensions": (x[0], None),
+                  "slots": (x, torch.arange(4, dtype=torch.int32, device="cuda"))}[how]
+    with pytest.raises(ev.EvConvError):
+        memory(bad, slots=slots)
+    for s, b in zip(memory.states, before):
+        assert torch.equal(s, b)
+
+
 def test_a_window_in_a_graph():
     torch, memory = make()
     _, other = make()
