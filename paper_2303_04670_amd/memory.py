@@ -69,9 +69,18 @@ class Memory:
         return ops.quantize_rows(self._of(a))
 
     def forget(self, slots=None):
-        """Streams (all of them) begin anew."""
+        """Streams (all of them) begin anew.  slots: as in a window's call, or whatever else indexes the streams."""
+        if slots is None or isinstance(slots, slice) or torch.is_tensor(slots) and slots.dtype == torch.bool:
+            for state in self.states:
+                state[slots if slots is not None else slice(None)] = 0
+            return
+        # (on the GPU alone: which streams are meant is not waited for, and a slot that is none is not an index from the end)
+        slots, n = torch.as_tensor(slots, device=self.device).reshape(-1).long(), self.n_streams
+        meant = torch.zeros(n + 1, dtype=torch.bool, device=self.device)
+        meant.index_fill_(0, torch.where((slots >= 0) & (slots < n), slots, n), True)
+        rows = slots.clamp(0, n - 1)
         for state in self.states:
-            state[slots if slots is not None else slice(None)] = 0
+            state[rows] = torch.where(meant[rows][:, None, None, None], torch.zeros((), device=self.device), state[rows])
 
     def __call__(self, x, slots=None, seq_offsets=None):
         """Features [windows, dim] -> [windows, n_out].  By default one window of every stream, in their order; with

@@ -114,6 +114,20 @@ def test_a_refused_window_leaves_the_states(how):
         assert torch.equal(s, b)
 
 
+@pytest.mark.parametrize("on", ["cuda", "cpu", "list"])
+def test_forgetting_takes_slots_as_a_window_does(on):
+    """Negative ones are no stream's."""
+    torch, memory = make()
+    memory(torch.randn(5, 96, device="cuda"))
+    before = [s.clone() for s in memory.states]
+    slots = [3, -1, 0]
+    memory.forget(slots if on == "list" else torch.tensor(slots, dtype=torch.int32, device=on))
+    for s, b in zip(memory.states, before):
+        assert not s[[0, 3]].any() and torch.equal(s[[1, 2, 4]], b[[1, 2, 4]]) and b.flatten(1).any(dim=1).all()
+    memory.forget()
+    assert not any(s.any() for s in memory.states)
+
+
 def test_a_window_in_a_graph():
     torch, memory = make()
     _, other = make()
