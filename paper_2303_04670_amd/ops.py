@@ -2,7 +2,8 @@
 
 Argument marshalling only: PyTorch owns the memory and names the stream (the current one of the
 tensors' device); every value is computed by the library's kernels.  A refused call raises
-`EvConvError` with the library's status, as the net's calls do.
+`EvConvError` with the library's status, as the net's calls do.  No operator has a gradient: a tensor that
+wants one is refused where gradients are recorded.
 
     o, state = delta_rule(q, k, v, gate, beta, state)            the gated delta rule
     r = block_norm(x, branch, z, ...)                            norms around a block: r.x, r.h, r.q
@@ -76,7 +77,7 @@ class NormResult(NamedTuple):
 
 
 _entry = None
-_byref, _empty, _empty_like = ctypes.byref, torch.empty, torch.empty_like
+_byref, _empty, _empty_like, _grad_enabled = ctypes.byref, torch.empty, torch.empty_like, torch.is_grad_enabled
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (without the wrapper's own checks)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 
@@ -112,13 +113,16 @@ def _explain(t, name, gpu, dtype, shape):
         _refuse(ERR_INVALID_ARG, f"{name} is {t.dtype}, expected {dtype}")
     if t.shape != shape:
         _refuse(ERR_SHAPE, f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.requires_grad and _grad_enabled():
+        _refuse(ERR_INVALID_ARG, f"{name} wants a gradient, which these operators do not have: call them under torch.no_grad()")
     _refuse(ERR_SHAPE, f"{name}: strides {t.stride()}: rows (parameters and states: the whole tensor) must be contiguous")
 
 
 def _rows(t, name, gpu, dtype, shape):
     """(address, strides) of a tensor of this GPU, type and shape whose last dimension is contiguous."""
     stride = t.stride()
-    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
+    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1) \
+            or (t.requires_grad and _grad_enabled()):
         _explain(t, name, gpu, dtype, shape)
     return t.data_ptr(), stride
 
@@ -127,7 +131,8 @@ def _packed(t, name, gpu, dtype, shape):
     """Address of a contiguous tensor; None of None."""
     if t is None:
         return None
-    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or not t.is_contiguous() \
+            or (t.requires_grad and _grad_enabled()):
         _explain(t, name, gpu, dtype, shape)
     return t.data_ptr()
 
@@ -191,9 +196,9 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
     k_at, (k_token, k_head, _) = _rows(k, "k", gpu, dtype, q_shape)
     v_at, (v_token, v_head, _) = _rows(v, "v", gpu, dtype, v_shape)
     gates = (n, hv)
-    if gate.get_device() != gpu or gate.shape != gates:  # (single values: any strides)
+    if gate.get_device() != gpu or gate.shape != gates or (gate.requires_grad and _grad_enabled()):  # (single values: any strides)
         _explain(gate, "gate", gpu, gate_dtype, gates)
-    if beta.get_device() != gpu or beta.dtype is not gate_dtype or beta.shape != gates:
+    if beta.get_device() != gpu or beta.dtype is not gate_dtype or beta.shape != gates or (beta.requires_grad and _grad_enabled()):
         _explain(beta, "beta", gpu, gate_dtype, gates)
     if raw:
         a_scale, dt_bias = _packed(a_scale, "a_scale", gpu, f32, (hv,)), _packed(dt_bias, "dt_bias", gpu, f32, (hv,))

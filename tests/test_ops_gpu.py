@@ -745,3 +745,26 @@ def test_refusals_leave_the_device_usable():
                          ops.QuantRows(torch.zeros(2, 128, dtype=torch.int8, device="cuda"), torch.ones(2, device="cuda"), 100))
     o, _ = ops.delta_rule(*good)
     assert torch.isfinite(o).all()
+
+
+def test_tensors_that_want_a_gradient_are_refused():
+    """These operators have none, and their outputs would be detached without a word; under no_grad nothing is lost."""
+    torch, ops = torch_ops()
+    x = delta_inputs(27, 8, 1, 1, 1, 16, 16, "f32", True)
+    d = {n: a.cuda() for n, a in x.items()}
+    delta = lambda d: ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], normalize=True, a_scale=d["a_scale"], dt_bias=d["dt_bias"])[0]
+    n = {i: a.cuda() for i, a in norm_case(6, 4, 32, 32, "f32", "silu").items()}
+    norm = lambda n: ops.block_norm(**n).x
+    w = ops.quantize_rows(torch.randn(8, 32, device="cuda"))
+    product = lambda b: ops.quant_matmul(w, w, bias=b["bias"])
+    rows = lambda x: ops.quantize_rows(x["x"]).scale
+    for call, given in ((delta, d), (norm, n), (product, {"bias": torch.randn(8, device="cuda")}), (rows, {"x": n["x"]})):
+        want = call(given)
+        for name in given:
+            some = {**given, name: given[name].clone().requires_grad_()}
+            with pytest.raises(ev.EvConvError) as e:
+                call(some)
+            assert e.value.status == ev.ERR_INVALID_ARG and "gradient" in str(e.value), name
+            with torch.no_grad():
+                got = call(some)
+            assert torch.equal(got, want) and not got.requires_grad
