@@ -203,6 +203,8 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
     if raw:
         a_scale, dt_bias = _packed(a_scale, "a_scale", gpu, f32, (hv,)), _packed(dt_bias, "dt_bias", gpu, f32, (hv,))
     if seq_offsets is not None:
+        if n_seq is not None and n_seq != seq_offsets.numel() - 1:
+            _refuse(ERR_SHAPE, f"{seq_offsets.numel()} offsets for {n_seq} sequences")
         n_seq = seq_offsets.numel() - 1
         seq_offsets = _packed(seq_offsets, "seq_offsets", gpu, torch.int32, (n_seq + 1,))
     elif n_seq is None:

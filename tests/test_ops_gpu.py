@@ -253,6 +253,20 @@ def test_delta_rule_new_states_of_more_slots_than_sequences(length, dtype):
         assert s is not d["state"] and torch.equal(s[3:], before[3:]) and torch.equal(d["state"], before)
 
 
+def test_delta_rule_n_seq_beside_offsets():
+    torch, ops = torch_ops()
+    x = delta_inputs(28, 6, 3, 1, 1, 16, 16, "f32", False)
+    d = {n: None if a is None else a.cuda() for n, a in x.items()}
+    call = lambda n_seq: ops.delta_rule(d["q"], d["k"], d["v"], d["gate"], d["beta"], d["state"], seq_offsets=offsets([1, 2, 3]), n_seq=n_seq)
+    want = call(None)
+    got = call(3)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for n_seq in (2, 6):
+        with pytest.raises(ev.EvConvError) as e:
+            call(n_seq)
+        assert e.value.status == ev.ERR_SHAPE
+
+
 def test_delta_rule_slots_need_states():
     """How many slots there are is known from `state` or `state_out` only."""
     torch, ops = torch_ops()
