@@ -121,7 +121,7 @@ def _explain(t, name, gpu, dtype, shape):
 def _rows(t, name, gpu, dtype, shape):
     """(address, strides) of a tensor of this GPU, type and shape whose last dimension is contiguous."""
     stride = t.stride()
-    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1) \
+    if t.get_device() != gpu or t.dtype is not dtype or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1) \
             or (t.requires_grad and _grad_enabled()):
         _explain(t, name, gpu, dtype, shape)
     return t.data_ptr(), stride
@@ -131,7 +131,7 @@ def _packed(t, name, gpu, dtype, shape):
     """Address of a contiguous tensor; None of None."""
     if t is None:
         return None
-    if t.get_device() != gpu or gpu < 0 or t.dtype is not dtype or t.shape != shape or not t.is_contiguous() \
+    if t.get_device() != gpu or t.dtype is not dtype or t.shape != shape or not t.is_contiguous() \
             or (t.requires_grad and _grad_enabled()):
         _explain(t, name, gpu, dtype, shape)
     return t.data_ptr()
@@ -188,7 +188,7 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
         _refuse(ERR_SHAPE, f"q {tuple(q.shape)}, v {tuple(v.shape)}, gate {tuple(gate.shape)}: expected three, three and two dimensions")
     gpu, dtype, gate_dtype, q_shape, v_shape = v.get_device(), v.dtype, gate.dtype, q.shape, v.shape
     (n, hk, dk), (hv, dv) = q_shape, v_shape[1:]
-    if v_shape[0] != n:
+    if gpu < 0 or v_shape[0] != n:
         _explain(v, "v", gpu, dtype, (n, hv, dv))
     raw = a_scale is not None or dt_bias is not None
     flags, f32 = (DELTA_NORMALIZE if normalize else 0) | (DELTA_RAW_GATES if raw else 0), torch.float32
@@ -221,10 +221,14 @@ def delta_rule(q, k, v, gate, beta, state=None, *, state_out=None, out=None, seq
             state_out = state
         else:  # (the call writes the sequences' states; where there are more, the others are as they were)
             state_out = state.clone() if n_slots > n_seq else _like(state, shape, f32, gpu)
-    to_at = state_at if state_out is state else _packed(state_out, "state_out", gpu, f32, shape)
+        to_at = state_out.data_ptr()
+    else:
+        to_at = state_at if state_out is state else _packed(state_out, "state_out", gpu, f32, shape)
     if out is None:
         out = _like(v, v_shape, dtype, gpu)
-    o_at, (o_token, o_head, _) = _rows(out, "out", gpu, dtype, v_shape)
+        o_at, (o_token, o_head, _) = out.data_ptr(), out.stride()
+    else:
+        o_at, (o_token, o_head, _) = _rows(out, "out", gpu, dtype, v_shape)
     a = _FlatDeltaArgs(ABI_VERSION, _dtype(v, "v"), _dtype(gate, "gate"), flags, hk, hv, dk, dv, n_seq, n_slots, n,
                   dk ** -0.5 if scale is None else scale, q_at, q_token, q_head, k_at, k_token, k_head, v_at, v_token, v_head,
                   gate.data_ptr(), *gate.stride(), beta.data_ptr(), *beta.stride(), o_at, o_token, o_head, a_scale, dt_bias,
@@ -247,6 +251,8 @@ def block_norm(x=None, branch=None, gate=None, *, post_weight=None, post_bias=No
     if first is None or first.dim() != 2:
         _refuse(ERR_SHAPE, "block norm: x or branch as [rows, dim]")
     gpu, dtype, shape = first.get_device(), first.dtype, first.shape
+    if gpu < 0:
+        _explain(first, "x" if x is not None else "branch", gpu, dtype, shape)
     rows, dim = shape
     if group is None:
         group = dim
@@ -309,6 +315,8 @@ def quantize_rows(x) -> QuantRows:
     if x.dim() != 2:
         _refuse(ERR_SHAPE, "block norm: x or branch as [rows, dim]")
     gpu, dtype, shape = x.get_device(), x.dtype, x.shape
+    if gpu < 0:
+        _explain(x, "x", gpu, dtype, shape)
     rows, dim = shape
     at, (step, _) = _rows(x, "x", gpu, dtype, shape)
     q_step = -(-dim // 128) * 128
@@ -329,6 +337,8 @@ def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype
     if act not in _ACTS:
         _refuse(ERR_INVALID_ARG, f"quantised product: act {act!r}")
     gpu, m, n, f32 = aq.get_device(), aq.shape[0], bq.shape[0], torch.float32
+    if gpu < 0:
+        _explain(aq, "a.q", gpu, torch.int8, aq.shape)
     a_at, (a_step, _) = _rows(aq, "a.q", gpu, torch.int8, aq.shape)
     b_at, (b_step, _) = _rows(bq, "b.q", gpu, torch.int8, bq.shape)
     if aq.shape[1] < -(-k // 128) * 128 or bq.shape[1] < -(-k // 128) * 128:
@@ -337,7 +347,9 @@ def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype
         bias = _packed(bias, "bias", gpu, f32, (n,))
     if out is None:
         out = _empty(m, n, dtype=out_dtype, device=gpu)
-    y_at, (y_step, _) = _rows(out, "out", gpu, out.dtype, (m, n))
+        y_at, y_step = out.data_ptr(), n
+    else:
+        y_at, (y_step, _) = _rows(out, "out", gpu, out.dtype, (m, n))
     args = QuantArgs(ABI_VERSION, _dtype(out, "out"), _ACTS[act], n, k, m, a_at, b_at, a_step, b_step,
                      _packed(a_scale, "a.scale", gpu, f32, (m,)), _packed(b_scale, "b.scale", gpu, f32, (n,)), bias, y_at, y_step)
     _enqueue(_calls().evconv_quant_matmul, args, gpu)
