@@ -198,14 +198,19 @@ void start_tile(TileParams p, hipStream_t s) {
 //   4096 x 4096 x 4096  128 x 128 72, 256 x 256 64.5 (2.1 POP/s);   16384 x 8192 x 2048  323, 308 (1.8 POP/s)
 // The largest ones, of which a compute unit holds one at a time, only where more than three quarters of their rounds are full:
 //   5000 x 5000 x 3000 (0.78) 101, 94;   6000 x 4096 x 2048 (0.75) 65, 68;   4600 x 4096 x 2048 (0.56) 55, 67
+// and both only where not too much of their tiles is outside (inside, of 256 x 256 and of 128 x 128; 64 x 64, 128 x 128, 256 x 256):
+//   65536 x 400 x 1024 (0.78, 0.78) 53, 51, 48;   65536 x 200 x 1024 (0.78, 0.78) 31, 29, 27;   65536 x 520 x 1024 (0.68, 0.81) 64, 66, 69
+//   65536 x 300 x 1024 (0.59, 0.78) 62, 64, 72;   65536 x 160 x 1024 (0.63, 0.63) 25, 28, 26;   65536 x 257 x 1024 (0.50, 0.67) 54, 56, 67
+//   260 x 50000 x 1024 (0.51, 0.68) 31, 34, 43;   65536 x 40 x 1024 (0.16, 0.31) 14, 17, 24
 template <bool BF16>
 void start(const TileParams& p, hipStream_t s) {
   const evconv_quant_args& a = p.a;
   auto tiles = [&](int bm, int bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
+  auto inside = [&](int side, double share) { return (double)a.m * a.n > share * side * side * tiles(side, side); };
   if (tiles(16, 32) <= 256) start_tile<BF16, 16, 32, 1, 1, 8>(p, s);
   else if (tiles(32, 32) <= 512) start_tile<BF16, 32, 32, 2, 1, 4>(p, s);
-  else if (tiles(256, 256) * 4 > (tiles(256, 256) + 255) / 256 * 256 * 3) start_tile<BF16, 256, 256, 2, 4, 1>(p, s);
-  else if (tiles(128, 128) >= 384) start_tile<BF16, 128, 128, 2, 2, 1>(p, s);
+  else if (tiles(256, 256) * 4 > (tiles(256, 256) + 255) / 256 * 256 * 3 && inside(256, 0.7)) start_tile<BF16, 256, 256, 2, 4, 1>(p, s);
+  else if (tiles(128, 128) >= 384 && inside(128, 0.75)) start_tile<BF16, 128, 128, 2, 2, 1>(p, s);
   else start_tile<BF16, 64, 64, 2, 2, 1>(p, s);
 }
 }  // namespace

@@ -667,7 +667,8 @@ def test_quant_matmul(m, n, k, act, bias, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,k,act,bias", [
     (2500, 2600, 200, "tanh", True), (2433, 2569, 129, "none", False), (2500, 2600, 1, "relu", True),  # 128 x 128
-    (3500, 3600, 300, "none", True), (3329, 3585, 1153, "sigmoid", False), (50000, 33, 256, "relu", True), (40, 50000, 256, "none", True)])  # 256 x 256
+    (3500, 3600, 300, "none", True), (3329, 3585, 1153, "sigmoid", False),  # 256 x 256
+    (50000, 33, 256, "relu", True), (40, 50000, 256, "none", True), (30000, 200, 128, "none", True)])  # narrow: 64 x 64, 128 x 128
 def test_quant_matmul_in_large_tiles(m, n, k, act, bias, dtype):
     """From 384 tiles of 128 x 128 and 193 of 256 x 256 on; tiles that the ends cut, one row and column beyond a tile."""
     torch, ops = torch_ops()
