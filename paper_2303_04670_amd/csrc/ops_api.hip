@@ -35,8 +35,10 @@ bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token
 // Sequences of up to this many tokens go token by token: of calls that the one-launch kernel takes otherwise, of others.  us for
 // 16 sequences of 4 heads of 64 x 64, 64 of 16 of 128 x 128, token by token / in chunks: bf16, 6 tokens 18 / 14, 59 / 76, 8
 // tokens 22 / 14, 70 / 76; fp32, 8 tokens 19 / 27, 61 / 128, 12 tokens 25 / 27, 77 / 128.
-// Of calls with lengths of their own, whose chunks wait for the launch of the tokens (24 sequences of up to 700 tokens, 6 heads of
-// 80 x 112, fp32: for 24 us at 12 tokens, 12 at 4), fewer.
+// Of calls with lengths of their own the chunks wait for the launch of the tokens (24 sequences of up to 700 tokens, 6 heads of
+// 80 x 112, fp32: for 24 us at 12 tokens, 12 at 4): fewer there, where sequences are longer than that on average.  Where they are not, as
+// many (256 sequences of 16 heads of 128 x 128 / of 4 of 64 x 64: 5 tokens each in bf16 207 / 35 us, in chunks 304 / 53; 12 in fp32 297 / 55,
+// 521 / 82).
 constexpr int kShortFused = 6, kShort = 12;
 
 struct DeltaPlan {
@@ -69,7 +71,8 @@ evconv_status plan_delta(const evconv_delta_args* a, DeltaPlan* out) {
   d.p.vec = a->d_k % 8 == 0 && wide(a->dtype, a->q) && wide(a->dtype, a->k);
   d.p.vec_v = a->d_v % 8 == 0 && wide(a->dtype, a->v) && aligned(a->o, 8) && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0;
   const bool one_launch = delta_fused_supported(d.p);
-  d.p.short_len = d.p.len < 0 ? kDeltaShortRagged : one_launch ? kShortFused : kShort;
+  d.p.short_len = one_launch ? kShortFused : kShort;
+  if (d.p.len < 0 && a->n_tokens > (int64_t)d.p.short_len * a->n_seq) d.p.short_len = kDeltaShortRagged;
   // (room for the sequences that can be in chunks, not for all: a call of single tokens with offsets has few)
   const int n = (int)a->n_tokens;
   d.p.slots_total = d.p.len >= 0 ? a->n_seq * ((d.p.len + kDeltaChunk - 1) / kDeltaChunk) : n / kDeltaChunk + std::min(a->n_seq, n / (kDeltaShortRagged + 1));

@@ -17,7 +17,7 @@ void set_call_error(const char* text) noexcept;
 
 // ---- gated delta rule ---------------------------------------------------------------------------
 constexpr int kDeltaChunk = 64;       // tokens of a chunk
-constexpr int kDeltaShortRagged = 4;  // sequences of up to so many tokens go token by token where lengths are their own (ops_api.hip)
+constexpr int kDeltaShortRagged = 4;  // sequences of up to so many tokens go token by token, at least, where lengths are their own (ops_api.hip)
 
 struct DeltaParams {
   evconv_delta_args a;

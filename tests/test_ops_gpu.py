@@ -464,12 +464,12 @@ def test_delta_rule_offsets_out_of_order_stay_inside():
 
 
 @pytest.mark.parametrize("dtype,dk", [("f32", 64), ("bf16", 136)])
-@pytest.mark.parametrize("kind", ["fives", "mixed", "random", "few"])
+@pytest.mark.parametrize("kind", ["fives", "mixed", "random", "few", "fives and a long one"])
 def test_delta_rule_chunks_of_many_sequences(kind, dtype, dk):
     """Sequences just long enough for a chunk of their own, packed as closely as they can be."""
     rng = np.random.default_rng(4)
     lens = {"fives": [5] * 70, "mixed": [5, 4, 5, 1, 64, 0, 65, 5, 5, 63, 4, 4, 4, 128, 5] * 3, "random": rng.integers(0, 14, 120).tolist(),
-            "few": [5, 600, 5, 0, 700]}[kind]
+            "few": [5, 600, 5, 0, 700], "fives and a long one": [5] * 70 + [1200] + [5] * 20}[kind]
     x = delta_inputs(19, sum(lens), len(lens), 1, 2, dk, 24, dtype, True)
     o, s, want_o, want_s = run_delta(x, lens)
     close(o, want_o, dtype == "bf16")
