@@ -40,7 +40,8 @@ extern "C" {
  *   o_t = scale * S' q_t
  * Value head h uses key (query) head h / (heads_v / heads_k).  q, k, v and o are of `dtype`; the state is
  * fp32, and everything that reaches it is computed in fp32 or as sums of bf16 parts that hold an fp32
- * value's 24 bits; o of a bf16 call is computed to 16 bits and rounded once.
+ * value's 24 bits.  o of a bf16 call is rounded once, token by token from fp32, in chunks from a sum of terms of 16 bits each: where
+ * terms cancel, it is off by up to some 2^-16 of the largest instead of itself.
  *
  * EVCONV_DELTA_NORMALIZE: q_t and k_t are first divided by sqrt(sum of squares + 1e-6).
  * EVCONV_DELTA_RAW_GATES: `gate` and `beta` hold what a projection gave, a_t and b_t:
@@ -96,7 +97,8 @@ evconv_status evconv_delta_rule(const evconv_delta_args* args, void* workspace, 
                                 void* hip_stream);
 
 /* ---- norms around a block ---------------------------------------------------------------------------
- * Per row of `dim` values, all in fp32, each output rounded once:
+ * Per row of `dim` values, all in fp32, each output rounded once (the sigmoid of bf16 rows by the hardware's exponential and
+ * reciprocal, good to about 2^-20 of itself, also where only the 8-bit rows are wanted):
  *   t = norm(branch) * post_weight + post_bias     in groups of `group` values (heads), each with a norm of its own
  *   t = t * act(gate)                              act: 1, sigmoid(z) or z * sigmoid(z)
  *   x' = x + res_scale * t                         (x NULL: x' = res_scale * t;  branch NULL: x' = x)

@@ -370,8 +370,8 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(DeltaParams p) {
 // registers.  The waves share the operands: a chunk's are K, Q, (T, P) and K' in turn, each brought into one of three
 // buffers in LDS two stages before it is used (K, Q and K' in halves where they are larger than a buffer).
 // Bound by a sequence's longest chain: fp32 operands are three parts, so a product is six matrix instructions, and what comes
-// out of one has to be split again for the next.  24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 86 us, 7.8 a
-// chunk, beside 28 for delta_prepare.  (Of 18.6 thousand cycles a chunk with v's and o's single values in a row and masks for each, K S
+// out of one has to be split again for the next; a wave alone on its SIMD reads operands, waits, splits and multiplies in a row.
+// 24 sequences of up to 700 tokens, 6 heads of 80 x 112, fp32: 83 us, 7.6 a chunk, beside 28 for delta_prepare.  (Of 18.6 thousand cycles a chunk with v's and o's single values in a row and masks for each, K S
 // took 5.2, Q S 2.8, T and P 5.3, K' 4.8: 96 us.)  Before: keys as 128 channels instead of 96 124, every wave with
 // operands of its own from L2 222.
 template <bool F32, int DKP>

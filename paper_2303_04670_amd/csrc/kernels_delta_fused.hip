@@ -6,10 +6,11 @@
 // (the transposed operand K' comes from the same rows by transposing LDS reads), T and P go from producer to
 // consumer through a ring of three slots, S, R and D stay in their lanes (kernels_delta.hip: place).
 //
-// Bound by the vector units: a step of the chip full of workgroups (heads of 128 x 128) takes 9 us, 18 thousand cycles, of which
-// a SIMD spends 9 to 11 thousand on vector instructions (parts of S, R and D, exponentials, T's substitution), 7 thousand on matrix
-// instructions and waits in LDS reads and the step's meeting for the rest.  8 sequences of 4096 tokens and 32 heads: 0.58 ms,
-// where the rows and states alone would take 0.16; prepared by a launch of its own they took 3.6.
+// A step of the chip full of workgroups (heads of 128 x 128) takes 9 us, 18 thousand cycles, of which a SIMD spends 9 to 11 thousand on
+// vector instructions (parts of S, R and D, exponentials, T's substitution) and 7 thousand on matrix instructions: together the step.
+// They hardly run beside each other, for all waves meet once a step, so that the two consumers of a SIMD split at the same time and
+// multiply at the same time; beside each other the same instructions would fit into 11 thousand.  8 sequences of 4096 tokens and
+// 32 heads: 0.55 ms, where the rows and states alone would take 0.16; prepared by a launch of its own they took 3.6.
 // Measured without gain: a pair of producers instead of two in workgroups of four strips; more priority to half of the consumers (slower).
 //
 // In step c (all waves meet once per step) the consumers apply chunk c and bring in the rows of chunk c + 1; a pair of producers
