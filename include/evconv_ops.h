@@ -8,6 +8,11 @@
  *                         and residual sum between them, and the 8-bit rows of the result
  *   evconv_quant_matmul   product of 8-bit integers with one scale per row (token) and per column
  *                         (channel)
+ *   evconv_cache_append   keys and values of new tokens into a paged cache (bf16 or 4 bits), with the norm
+ *                         and the rotation of their heads and their queries' on the way
+ *   evconv_cache_read     cached keys and values back as rows
+ *   evconv_cache_attend   attention of queries over the cache, whole or over chosen pages
+ *   evconv_cache_select   the pages that a bound on their scores makes worth a query's look
  *
  * Plain C, in libevconv.so beside the net's calls, with their statuses (evconv.h).  The text of the
  * last failed call of a host thread is evconv_last_error(NULL).  All pointers are DEVICE memory owned by
@@ -15,7 +20,8 @@
  * stream) and returns: it neither allocates nor synchronises nor keeps anything, so it may be captured
  * into a HIP graph, and calls on different streams do not meet as long as their workspaces and
  * outputs are different.  A count of zero tokens (rows) is a valid call that does nothing, except that the
- * delta rule hands the states on.
+ * delta rule hands the states on.  Arguments that are device memory (tables, positions, offsets) cannot be refused: what of
+ * them is out of range is left out, as said at each call, and nothing outside the given buffers is read or written.
  *
  * Strides are in elements.  Rows (the last dimension) are contiguous.  Alignment beyond that of an
  * element is not required, but rows of 16-byte multiples at 16-byte addresses are read in wide loads.
@@ -156,6 +162,134 @@ typedef struct {
 } evconv_quant_args;
 
 evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* hip_stream);
+
+/* ---- a paged cache of keys and values ----------------------------------------------------------------
+ * Tokens of n_seq sequences ("streams") in pages of `page` tokens: table[s * table_stride + i] is the page that holds
+ * sequence s's tokens i * page and on.  A sequence has past[s] tokens there; the call's tokens continue it (or look back):
+ * token i of sequence s has position past[s] + i.  past is only read: who appends moves it on, once for all layers.
+ * A table entry outside [0, n_pages), a negative position and one of width * page and more hold nothing: what is appended
+ * there is dropped, what looks there sees nothing.  Pages may be read by several sequences; a page that a call appends to must be
+ * one sequence's alone.
+ *
+ * Channels are padded to dp = 32, 64, 96, 128, 192 or 256 with zeros.  All tensors are contiguous, at 16-byte addresses:
+ *   EVCONV_CACHE_BF16   k [n_pages][heads][page][dp], v [n_pages][heads][dp][page]  (channels of v in rows: both are
+ *                       operands of the matrix instructions as they stand)
+ *   EVCONV_CACHE_FP4    the same of 4-bit floating-point values (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), two to a byte,
+ *                       the first in the low bits: neighbouring channels of k, neighbouring tokens of v; times
+ *                       k_scale, v_scale fp32 [n_pages][heads][page].  Of a row x with m = max |x|: scale = m / 6, codes
+ *                       the nearest of 6 x / m (each operation rounded to fp32), ties to the even code
+ *   bounds              bf16 [n_pages][heads][2][dp]: least and largest of bf16(k) per channel over what was appended
+ *                       since the page's first token; or NULL (no evconv_cache_select then)
+ * A key row with a value that is not finite (in bf16) makes what looks at its token NaN; so does a value row, whose
+ * token's key is stored as NaN for it (v itself holds finite values only: one that is not would reach queries that do not see
+ * it).  Other tokens and queries are as without it. */
+typedef enum { EVCONV_CACHE_BF16 = 0, EVCONV_CACHE_FP4 = 1 } evconv_cache_kind;
+
+typedef struct {
+  int32_t kind;    /* evconv_cache_kind */
+  int32_t n_pages; /* at least 1 */
+  int32_t heads;   /* of keys and values, 1..1024 */
+  int32_t page;    /* 32, 64, 128 or 256 */
+  int32_t d;       /* channels of a head, 1..256 */
+  void *k, *v;
+  float *k_scale, *v_scale; /* EVCONV_CACHE_FP4 only */
+  void* bounds;
+} evconv_cache;
+
+typedef struct {
+  int32_t n_seq;               /* sequences, 1..65535 */
+  int32_t width;               /* entries of a table row, at least 1; width * page below 2^30 */
+  int64_t n_tokens;            /* of all sequences together, below 2^31 - 64 */
+  const int32_t* table;        /* [n_seq][width] */
+  int64_t table_stride;
+  const int32_t* past;         /* [n_seq] */
+  const int32_t* seq_offsets;  /* [n_seq + 1] ascending, from 0 to n_tokens: sequence s is tokens [offsets[s], offsets[s+1]).
+                                * NULL: n_tokens / n_seq (a multiple) tokens each.  Tokens of no sequence have no output.  Offsets
+                                * that do not ascend: which tokens are dealt with is not said */
+} evconv_tokens;
+
+/* Per head: norm (q_norm, k_norm: weights, NULL: none): x / sqrt(mean(x^2) + eps) * weight, the sum in 64 bits; then the
+ * rotation (freqs): pairs (a, b) of the first `rot` channels become (a cos - b sin, b cos + a sin) of the angle position *
+ * freqs[i], taken in 64 bits; all else in fp32.  k and v then go to the cache, q to q_out (rounded once; may be q). */
+typedef enum { EVCONV_PAIRS_HALVES = 0, EVCONV_PAIRS_NEIGHBOURS = 1 } evconv_pairs; /* (i, i + rot / 2) or (2 i, 2 i + 1) */
+
+typedef struct {
+  int32_t abi_version; /* EVCONV_OPS_ABI_VERSION */
+  int32_t dtype;       /* of q, k, v, q_out: EVCONV_F32 or EVCONV_BF16 */
+  evconv_cache cache;
+  evconv_tokens tokens;
+  int32_t heads_q;     /* 0: no queries; else 1..1024 */
+  int32_t rot;         /* channels that are rotated, even, at most d; 0: none */
+  int32_t pairs;       /* evconv_pairs */
+  float eps;
+  evconv_heads q, k, v; /* [n_tokens][heads][d] */
+  void* q_out;
+  int64_t q_out_token_stride, q_out_head_stride;
+  const float *q_norm, *k_norm; /* fp32 [d] or NULL */
+  const float* freqs;           /* fp32 [rot / 2] */
+  const int64_t* positions;     /* [n_tokens]: of the angles; NULL: past[s] + i */
+} evconv_append_args;
+
+evconv_status evconv_cache_append(const evconv_append_args* args, void* hip_stream);
+
+/* Keys and values of the tokens past[s] + i as rows [n_tokens][heads][d] of `dtype`; tokens that the cache does not hold are zero. */
+typedef struct {
+  int32_t abi_version;
+  int32_t dtype; /* of k and v: EVCONV_F32 or EVCONV_BF16 */
+  evconv_cache cache;
+  evconv_tokens tokens;
+  void *k, *v;   /* contiguous */
+} evconv_read_args;
+
+evconv_status evconv_cache_read(const evconv_read_args* args, void* hip_stream);
+
+/* o = sum over the tokens t that a query sees of softmax_t(scale * q . k_t) v_t, statistics and sums in fp32; a query that
+ * sees none gets zeros.  Query head h uses key head h / (heads_q / cache.heads).  Seen are, of the query's sequence, tokens 0 .. its own
+ * position (causal: of the last `window` ones of them), or all past[s] (else); of those the ones in chosen pages, if `selected`
+ * is given.  Products with bf16 queries are exact; fp32 queries and the weights of fp32 calls enter them as three bf16 parts
+ * (24 bits), the weights of bf16 calls rounded to bf16, relative to the row's largest. */
+typedef struct {
+  int32_t abi_version;
+  int32_t dtype;    /* of q and o: EVCONV_F32 or EVCONV_BF16 */
+  evconv_cache cache;
+  evconv_tokens tokens;
+  int32_t heads_q;  /* a multiple of cache.heads, up to 1024 */
+  int32_t causal;   /* 0 or 1 */
+  int32_t window;   /* 0: no limit; only with causal */
+  int32_t count;    /* pages of a query in `selected`, 1..65536 */
+  int64_t max_len;  /* no sequence has more tokens than that with the call's; what is behind is not seen.  0: width * page */
+  float scale;
+  evconv_heads q;   /* [n_tokens][heads_q][d] */
+  void* o;
+  int64_t o_token_stride, o_head_stride;
+  const int32_t* selected; /* [n_tokens][cache.heads][count]: table entries of the query's sequence, what is outside
+                            * [0, width) for none; one that is there twice counts twice.  NULL: all.  Not with window */
+} evconv_attend_args;
+
+evconv_status evconv_cache_attend_workspace(const evconv_attend_args* args, size_t* bytes);
+evconv_status evconv_cache_attend(const evconv_attend_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Which `count` pages of its sequence each query (and key head) looks at, ascending, then -1.  With c the page of the query's
+ * own position: the first `first` pages and the last `last` ones up to c; then, of the others below c, those of the highest
+ *   score = max over the query heads of the key head of  sum over channels of max(q lo, q hi)
+ * (no query . key product of the page is larger), taken in 64 bits and rounded to fp32; ties: the lower page.  A score that is
+ * NaN is the highest.  A page that is not there is not chosen. */
+typedef struct {
+  int32_t abi_version;
+  int32_t dtype;   /* of q */
+  evconv_cache cache;
+  evconv_tokens tokens;
+  int32_t heads_q;
+  int32_t count;   /* 1..65536 */
+  int32_t first;   /* at least 0 */
+  int32_t last;    /* at least 1, first + last at most count: the own page's bounds hold tokens that the query does not see */
+  int64_t max_len; /* as of evconv_cache_attend */
+  evconv_heads q;
+  int32_t* selected; /* [n_tokens][cache.heads][count] */
+} evconv_select_args;
+
+evconv_status evconv_cache_select_workspace(const evconv_select_args* args, size_t* bytes);
+evconv_status evconv_cache_select(const evconv_select_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,114 @@
+// Attention over a paged cache (evconv_cache_attend): how a call is cut into launches, and the join of what several workgroups
+// found of a row.  The kernels: cache_attend_rows.h.
+#include <algorithm>
+
+#include "cache_attend_rows.h"
+
+namespace evk {
+namespace {
+
+// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row, its waves to every fourth
+// stretch.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
+template <bool BF16>
+__global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0) {
+  __shared__ float s_sum[4][256], s_total[4];
+  const evconv_attend_args& a = p.a;
+  const evconv_tokens& tk = a.tokens;
+  const int64_t row = row0 + blockIdx.x;
+  const int64_t token = row / a.heads_q;
+  const int head = (int)(row - token * a.heads_q);
+  const Piece piece = find_piece(tk, token, tk.seq_offsets ? -1 : (int)(tk.n_tokens / tk.n_seq), 1, 1, 0);
+  const int within = (int)(token - piece.first);
+  if (within < 0 || within >= piece.count) return;
+  int s0 = 0, s1 = p.splits - 1;
+  if (!a.selected) {
+    int lo, hi;
+    seen_by(p, tk.past[piece.seq], within, lo, hi);
+    if (hi <= lo) return;
+    s0 = lo / p.chunk;
+    s1 = (hi - 1) / p.chunk;
+    if (s0 == s1) return;
+  }
+  const int64_t rows = tk.n_tokens * a.heads_q;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float big = -INFINITY;
+  for (int s = s0 + lane; s <= s1; s += 64) big = fmaxf(big, p.stat[2 * (s * rows + row)]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d));
+  float sum[4] = {0, 0, 0, 0}, total = 0.0f;
+  for (int s = s0 + wave; s <= s1; s += 4) {
+    const int64_t at = s * rows + row;
+    const float m = p.stat[2 * at], factor = m == big ? 1.0f : __builtin_amdgcn_exp2f(m - big);
+    total += factor * p.stat[2 * at + 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (64 * i + lane < p.dp) sum[i] += factor * p.part[at * p.dp + 64 * i + lane];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s_sum[wave][64 * i + lane] = sum[i];
+  if (lane == 0) s_total[wave] = total;
+  __syncthreads();
+  const int ch = threadIdx.x;
+  if (ch >= a.cache.d) return;
+  const float all = (s_total[0] + s_total[1]) + (s_total[2] + s_total[3]);
+  const float o = (s_sum[0][ch] + s_sum[1][ch]) + (s_sum[2][ch] + s_sum[3][ch]);
+  store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + ch, all == 0.0f ? 0.0f : o / all);
+}
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t plan_attend(AttendParams& p) {
+  const evconv_attend_args& a = p.a;
+  const evconv_tokens& t = a.tokens;
+  p.dp = cache_channels(a.cache.d);
+  p.log = __builtin_ctz(a.cache.page);
+  p.share = a.heads_q / a.cache.heads;
+  p.most = (int64_t)t.width * a.cache.page;
+  if (a.max_len) p.most = std::min(p.most, a.max_len);
+  p.scale2 = a.scale * 1.44269504f;
+  int64_t extent;
+  if (a.selected) {
+    p.row_tiles = (p.share + 15) / 16;
+    p.row_units = t.n_tokens * p.row_tiles;
+    extent = (int64_t)a.count * a.cache.page;
+  } else {
+    const int64_t len = t.n_tokens / t.n_seq;
+    p.row_tiles = t.seq_offsets ? -1 : (int)((len * p.share + 15) / 16);
+    p.row_units = t.seq_offsets ? t.n_tokens * p.share / 16 + t.n_seq : (int64_t)t.n_seq * p.row_tiles;
+    extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
+  }
+  extent = std::max<int64_t>(extent, 1);
+  // Tokens to a workgroup: so many that there are workgroups for the chip a few times over, at least as many as make its start worth while.
+  const int64_t units = std::max<int64_t>(p.row_units * a.cache.heads, 1);
+  const int64_t least = a.cache.kind == EVCONV_CACHE_FP4 ? 1024 : 512;
+  const int64_t chunk = std::max(least, (int64_t)((units * (double)extent) / 4096));
+  p.chunk = (int)std::min<int64_t>((chunk + 127) / 128 * 128, 1 << 30);
+  p.splits = (int)std::min<int64_t>((p.most + p.chunk - 1) / p.chunk, 65535);
+  if (a.selected) p.splits = (int)std::min<int64_t>((extent + p.chunk - 1) / p.chunk, 65535);
+  if (p.splits < 1) p.splits = 1;
+  if ((int64_t)p.splits * p.chunk < (a.selected ? extent : p.most)) p.chunk = (int)(((a.selected ? extent : p.most) / p.splits + 128) / 128 * 128);
+  if (p.splits == 1) return 0;
+  const size_t rows = (size_t)t.n_tokens * a.heads_q * p.splits;
+  return up(rows * 2 * sizeof(float)) + rows * p.dp * sizeof(float);
+}
+
+void place_attend(AttendParams& p, char* workspace) {
+  p.stat = (float*)workspace;
+  p.part = (float*)(workspace + up((size_t)p.a.tokens.n_tokens * p.a.heads_q * p.splits * 2 * sizeof(float)));
+}
+
+void launch_attend(const AttendParams& p, hipStream_t s) {
+  if (p.a.cache.kind == EVCONV_CACHE_FP4) launch_attend_rows_fp4(p, s);
+  else launch_attend_rows_bf16(p, s);
+  if (p.splits == 1) return;
+  const int64_t rows = p.a.tokens.n_tokens * p.a.heads_q, most = kMostThreads / 256;
+  for (int64_t at = 0; at < rows; at += most) {
+    const unsigned grid = (unsigned)std::min(most, rows - at);
+    if (p.a.dtype == EVCONV_BF16) attend_join<true><<<grid, 256, 0, s>>>(p, at);
+    else attend_join<false><<<grid, 256, 0, s>>>(p, at);
+  }
+}
+
+}  // namespace evk

@@ -1,0 +1,248 @@
+// Choosing pages of a paged cache (evconv_cache_select) on gfx950, in two launches: the scores of all pages, and of each query and
+// key head the highest ones.
+//
+// Scores are taken in 64 bits: which of two pages is chosen is then the formula's answer and not that of an order of additions.  A wave
+// holds the bounds of a few pages per lane as 64-bit values, eight channels to a lane, and goes over the query heads that share
+// them, whose values come from LDS; so the conversions are made once for all heads.
+#include <algorithm>
+
+#include "cache_device.h"
+
+namespace evk {
+namespace {
+
+constexpr unsigned kForced = 0xffffffffu, kNotANumber = 0xfffffffeu;
+constexpr int kHeads = 16;  // query heads whose values are in LDS at once
+constexpr int kHeld = 4;    // pages that a lane holds
+
+// Unsigned numbers in the order of the floats, all above 0: that is the mark of a page that cannot be chosen.
+__device__ __forceinline__ unsigned key_of(float score) {
+  if (score != score) return kNotANumber;
+  const unsigned u = __float_as_uint(score + 0.0f);  // (no negative zero)
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct Query {
+  int seq, token;
+  int64_t last;  // page of the query's own position, -1: it sees none
+};
+__device__ __forceinline__ Query find_query(const SelectParams& p, int64_t token) {
+  const evconv_tokens& tk = p.a.tokens;
+  const Piece piece = find_piece(tk, token, p.len, 1, 1, 0);
+  const int64_t within = token - piece.first;
+  if (within < 0 || within >= piece.count) return {-1, 0, -1};
+  const int64_t position = min((int64_t)tk.past[piece.seq] + within, p.most - 1);
+  return {piece.seq, (int)token, position < 0 ? -1 : position >> p.log};
+}
+
+__device__ __forceinline__ double pages_sum(double v, int lanes) {
+  for (int d = 1; d < lanes; d *= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+template <bool BF16, int DP>
+__global__ __launch_bounds__(256) void score_pages(SelectParams p, int blocks, int64_t block0) {
+  constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32, GROUPS = 64 / LANES;
+  __shared__ double s_q[kHeads][2][DP];  // min(q, 0), max(q, 0)
+  const evconv_select_args& a = p.a;
+  const evconv_cache& c = a.cache;
+  const int64_t unit = (block0 + blockIdx.x) / blocks, token = unit / c.heads;
+  const int head = (int)(unit - token * c.heads);
+  const Query query = find_query(p, token);
+  const int first_page = (int)(block0 + blockIdx.x - unit * blocks) * (4 * kHeld * GROUPS);
+  if (query.seq < 0 || first_page > query.last) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane / LANES, ch = lane % LANES * 8;
+  // ---- the bounds
+  int at[kHeld];
+  bool there[kHeld];
+  double lo[kHeld][8], hi[kHeld][8];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    at[i] = first_page + (wave * kHeld + i) * GROUPS + group;
+    const int page = at[i] <= query.last ? page_of(c, a.tokens, query.seq, at[i]) : -1;
+    there[i] = page >= 0;
+    float l[8], h[8];
+    const int64_t row = ((int64_t)max(page, 0) * c.heads + head) * 2 * DP;
+    load_run<true, 8, true>(c.bounds, row + ch, DP - ch, l);
+    load_run<true, 8, true>(c.bounds, row + DP + ch, DP - ch, h);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lo[i][j] = (double)l[j], hi[i][j] = (double)h[j];
+  }
+  double best[kHeld];
+  bool bad[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) best[i] = -INFINITY, bad[i] = false;
+  for (int h0 = 0; h0 < p.share; h0 += kHeads) {
+    const int heads = min(p.share - h0, kHeads);
+    __syncthreads();
+    for (int i = threadIdx.x; i < heads * DP; i += 256) {
+      const int h = i / DP, x = i % DP;
+      const int64_t from = token * a.q.token_stride + (int64_t)(head * p.share + h0 + h) * a.q.head_stride + x;
+      const double v = x < c.d ? (double)load_one<BF16>(a.q.data, from) : 0.0;
+      s_q[h][0][x] = v > 0.0 ? 0.0 : v;  // (a NaN is in both)
+      s_q[h][1][x] = v < 0.0 ? 0.0 : v;
+    }
+    __syncthreads();
+    for (int h = 0; h < heads; ++h) {
+      double sum[kHeld];
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) sum[i] = 0.0;
+      if (ch < DP)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const double neg = s_q[h][0][ch + j], pos = s_q[h][1][ch + j];
+#pragma unroll
+          for (int i = 0; i < kHeld; ++i) sum[i] = fma(neg, lo[i][j], fma(pos, hi[i][j], sum[i]));
+        }
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        sum[i] = pages_sum(sum[i], LANES);
+        bad[i] = bad[i] || sum[i] != sum[i];
+        best[i] = fmax(best[i], sum[i]);
+      }
+    }
+  }
+  if (lane % LANES == 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (at[i] <= query.last) {
+        const bool forced = at[i] < a.first || at[i] > query.last - a.last;
+        p.score[unit * p.pages + at[i]] = !there[i] ? 0u : forced ? kForced : bad[i] ? kNotANumber : key_of((float)best[i]);
+      }
+  }
+}
+
+// Sum over the threads of a workgroup of what stands before each of them; `all`: of all.
+__device__ __forceinline__ int sum_before(int v, int* s_wave, int* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  int before = v;
+  for (int d = 1; d < 64; d *= 2) {
+    const int u = __shfl_up(before, d);
+    if (lane >= d) before += u;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = before;
+  __syncthreads();
+  int others = 0, total = 0;
+  for (int w = 0; w < waves; ++w) {
+    if (w < wave) others += s_wave[w];
+    total += s_wave[w];
+  }
+  *all = total;
+  return others + before - v;
+}
+
+// The `count` highest keys of a row, the lower index first among equals: the key of the last one by its bytes from the top, then all
+// above it and the first of those that equal it, in the order of their pages.  A workgroup to a row, a thread to neighbouring pages.
+__global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t unit0) {
+  __shared__ int s_bins[256], s_wave[16], s_found[2];
+  const evconv_select_args& a = p.a;
+  const int64_t unit = unit0 + blockIdx.x, token = unit / a.cache.heads;
+  const Query query = find_query(p, token);
+  if (query.seq < 0) return;
+  const int n = (int)query.last + 1, threads = blockDim.x, t = threadIdx.x;
+  const unsigned* const key = p.score + unit * p.pages;
+  int* const out = a.selected + unit * a.count;
+  const int per = ((n + threads - 1) / threads + 3) / 4 * 4, from = min(t * per, n), to = min(from + per, n);
+  int mine = 0, some;
+  for (int i = from; i < to; ++i) mine += key[i] != 0;
+  sum_before(mine, s_wave, &some);
+  unsigned edge = 0;  // key of the last one that is chosen
+  int equal = 0;      // how many with it
+  if (some > a.count) {
+    int need = a.count;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int i = t; i < 256; i += threads) s_bins[i] = 0;
+      __syncthreads();
+      for (int i = from; i < to; ++i) {
+        const unsigned k = key[i];
+        if (k != 0 && (shift == 24 || k >> (shift + 8) == edge >> (shift + 8))) atomicAdd(&s_bins[k >> shift & 255], 1);
+      }
+      __syncthreads();
+      if (t < 64) {  // bins 255 - 4 t and down: the one where the sum from the top reaches `need`
+        int sum = 0, bin[4];
+        for (int i = 0; i < 4; ++i) sum += bin[i] = s_bins[255 - 4 * t - i];
+        int before = sum;
+        for (int d = 1; d < 64; d *= 2) {
+          const int u = __shfl_up(before, d);
+          if (t >= d) before += u;
+        }
+        before -= sum;
+        if (before < need && before + sum >= need)
+          for (int i = 0; i < 4; ++i) {
+            if (before + bin[i] >= need) {
+              s_found[0] = 255 - 4 * t - i;
+              s_found[1] = need - before;
+              break;
+            }
+            before += bin[i];
+          }
+      }
+      __syncthreads();
+      edge |= (unsigned)s_found[0] << shift;
+      need = s_found[1];
+      __syncthreads();
+    }
+    equal = need;
+  }
+  // ---- written in the order of the pages
+  int above = 0, same = 0;
+  for (int i = from; i < to; ++i) {
+    above += key[i] > edge;
+    same += key[i] == edge && edge != 0;
+  }
+  int all_above, all_same;
+  int above_before = sum_before(above, s_wave, &all_above), same_before = sum_before(same, s_wave, &all_same);
+  for (int i = from; i < to; ++i) {
+    const bool is_above = key[i] > edge, is_same = key[i] == edge && edge != 0;
+    if (is_above || (is_same && same_before < equal)) out[above_before + min(same_before, equal)] = i;
+    above_before += is_above;
+    same_before += is_same;
+  }
+  for (int i = all_above + min(all_same, equal) + t; i < a.count; i += threads) out[i] = -1;
+}
+
+template <bool BF16>
+void start_scores(const SelectParams& p, unsigned grid, int blocks, int64_t at, hipStream_t s) {
+  switch (p.dp) {
+    case 32: score_pages<BF16, 32><<<grid, 256, 0, s>>>(p, blocks, at); break;
+    case 64: score_pages<BF16, 64><<<grid, 256, 0, s>>>(p, blocks, at); break;
+    case 96: score_pages<BF16, 96><<<grid, 256, 0, s>>>(p, blocks, at); break;
+    case 128: score_pages<BF16, 128><<<grid, 256, 0, s>>>(p, blocks, at); break;
+    case 192: score_pages<BF16, 192><<<grid, 256, 0, s>>>(p, blocks, at); break;
+    default: score_pages<BF16, 256><<<grid, 256, 0, s>>>(p, blocks, at); break;
+  }
+}
+
+int pages_of_a_workgroup(int dp) { return 4 * kHeld * (dp <= 32 ? 16 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2); }
+
+}  // namespace
+
+size_t plan_select(SelectParams& p) {
+  const evconv_select_args& a = p.a;
+  const evconv_tokens& t = a.tokens;
+  p.dp = cache_channels(a.cache.d);
+  p.log = __builtin_ctz(a.cache.page);
+  p.share = a.heads_q / a.cache.heads;
+  p.most = (int64_t)t.width * a.cache.page;
+  if (a.max_len) p.most = std::min(p.most, a.max_len);
+  p.len = t.seq_offsets ? -1 : (int)(t.n_tokens / t.n_seq);
+  p.pages = (int)((((p.most + a.cache.page - 1) >> p.log) + 3) / 4 * 4);
+  return (size_t)t.n_tokens * a.cache.heads * p.pages * sizeof(unsigned);
+}
+
+void launch_select(const SelectParams& p, hipStream_t s) {
+  const int64_t units = p.a.tokens.n_tokens * p.a.cache.heads;
+  const int per = pages_of_a_workgroup(p.dp), blocks = (p.pages + per - 1) / per;
+  const int64_t total = units * blocks, most = kMostThreads / 256;
+  for (int64_t at = 0; at < total; at += most) {
+    const unsigned grid = (unsigned)std::min(most, total - at);
+    if (p.a.dtype == EVCONV_BF16) start_scores<true>(p, grid, blocks, at, s);
+    else start_scores<false>(p, grid, blocks, at, s);
+  }
+  const int threads = p.pages <= 1024 ? 256 : 1024;
+  const int64_t rows = kMostThreads / threads;
+  for (int64_t at = 0; at < units; at += rows) choose_pages<<<(unsigned)std::min(rows, units - at), threads, 0, s>>>(p, at);
+}
+
+}  // namespace evk

@@ -1,36 +1,12 @@
 // Host side of the C ABI declared in include/evconv_ops.h: checks of the arguments, the choice of
 // kernels, launches on the caller's stream.
-#include "ops_kernels.h"
+#include "ops_host.h"
 
 #include <algorithm>
-#include <cstdarg>
-#include <cstdio>
 
 using namespace evk;
 
 namespace {
-
-evconv_status refuse(evconv_status st, const char* format, ...) {
-  char text[256];
-  va_list args;
-  va_start(args, format);
-  vsnprintf(text, sizeof text, format, args);
-  va_end(args);
-  set_call_error(text);
-  return st;
-}
-
-evconv_status launched(const char* what) {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? EVCONV_OK : refuse(EVCONV_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool float_type(int dtype) { return dtype == EVCONV_F32 || dtype == EVCONV_BF16; }
-size_t type_size(int dtype) { return dtype == EVCONV_F32 ? 4 : 2; }
-bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
-// Whether rows of `dtype` at this address and these distances may be read 16 bytes at a time.
-bool wide(int dtype, const void* p, int64_t stride) { return aligned(p, 16) && stride * (int64_t)type_size(dtype) % 16 == 0; }
-bool wide(int dtype, const evconv_heads& h) { return wide(dtype, h.data, h.token_stride) && wide(dtype, h.data, h.head_stride); }
 
 // Sequences of up to this many tokens go token by token: of calls that the one-launch kernel takes otherwise, of others.  us for
 // 16 sequences of 4 heads of 64 x 64, 64 of 16 of 128 x 128, token by token / in chunks: bf16, 6 tokens 18 / 14, 59 / 76, 8

@@ -63,4 +63,43 @@ void launch_block_norm(const evconv_norm_args& a, bool vec, hipStream_t s);
 // ---- product in 8-bit integers -------------------------------------------------------------------
 void launch_quant_matmul(const evconv_quant_args& a, hipStream_t s);
 
+// ---- paged cache ---------------------------------------------------------------------------------
+// Channels of a head in the cache.
+constexpr int cache_channels(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+void launch_cache_append(const evconv_append_args& a, bool vec, hipStream_t s);
+void launch_cache_read(const evconv_read_args& a, hipStream_t s);
+
+struct AttendParams {
+  evconv_attend_args a;
+  int dp, log;         // padded channels, log2 of the page
+  int share;           // query heads to a key head
+  bool vec;            // rows of q may be read in 16-byte loads
+  int64_t most;        // tokens of a sequence that are looked at, at most
+  float scale2;        // scale * log2(e)
+  // few rows: 16 of them to a workgroup
+  int row_tiles;       // of a sequence of equal lengths (of a token with chosen pages), or -1
+  int64_t row_units;   // row tiles of all sequences, as find_piece numbers them
+  int chunk, splits;   // tokens that one workgroup looks at (with chosen pages: of their list), pieces
+  // workspace
+  float* part;         // [splits][n_tokens * heads_q][dp] sums
+  float* stat;         // [splits][n_tokens * heads_q][2] largest exponent, sum of weights
+};
+size_t plan_attend(AttendParams& p);                     // bytes of workspace
+void place_attend(AttendParams& p, char* workspace);
+void launch_attend(const AttendParams& p, hipStream_t s);
+void launch_attend_rows_bf16(const AttendParams& p, hipStream_t s);
+void launch_attend_rows_fp4(const AttendParams& p, hipStream_t s);
+
+struct SelectParams {
+  evconv_select_args a;
+  int dp, log, share;
+  bool vec;
+  int64_t most;   // as above
+  int pages;      // pages of a sequence at most, the row length of `score`
+  int len;        // tokens of every sequence, or -1
+  unsigned* score;  // workspace: [n_tokens][heads][pages], in the order of the scores
+};
+size_t plan_select(SelectParams& p);
+void launch_select(const SelectParams& p, hipStream_t s);
+
 }  // namespace evk

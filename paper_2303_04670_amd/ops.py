@@ -8,6 +8,11 @@ wants one is refused where gradients are recorded.
     o, state = delta_rule(q, k, v, gate, beta, state)            the gated delta rule
     r = block_norm(x, branch, z, ...)                            norms around a block: r.x, r.h, r.q
     y = quant_matmul(quantize_rows(x), quantize_rows(weight))    product in 8-bit integers
+
+    cache = cache_new(n_pages, heads, d, kind="fp4")             a paged cache of keys and values
+    q = cache_append(cache, k, v, table, past, q, ...)           new tokens into it, heads normed and rotated
+    pages = cache_select(q, cache, table, past, count)           pages worth a look
+    o = cache_attend(q, cache, table, past, selected=pages)      attention over it
 """
 from __future__ import annotations
 
@@ -16,15 +21,19 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .evconv import (ERR_INVALID_ARG, ERR_SHAPE, OK, EvConvError, lib)
+from .evconv import (ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, OK, EvConvError, lib)
 
 ABI_VERSION = 1
-EXPORTS = ["evconv_delta_rule_workspace", "evconv_delta_rule", "evconv_block_norm", "evconv_quant_matmul"]
+EXPORTS = ["evconv_delta_rule_workspace", "evconv_delta_rule", "evconv_block_norm", "evconv_quant_matmul", "evconv_cache_append",
+           "evconv_cache_read", "evconv_cache_attend_workspace", "evconv_cache_attend", "evconv_cache_select_workspace",
+           "evconv_cache_select"]
 DELTA_NORMALIZE, DELTA_RAW_GATES = 1, 2
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 _NORMS = {"rms": 0, "layer": 1}
 _GATES = {"none": 0, "sigmoid": 1, "silu": 2}
 _ACTS = {"none": 0, "relu": 1, "sigmoid": 2, "tanh": 3}
+_PAIRS = {"halves": 0, "neighbours": 1}
+CACHE_BF16, CACHE_FP4 = 0, 1
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
 
@@ -41,10 +50,22 @@ class DeltaArgs(ctypes.Structure):
                 ("seq_offsets", _vp), ("slots", _vp), ("state_in", _vp), ("state_out", _vp)]
 
 
-class _FlatDeltaArgs(ctypes.Structure):
-    """DeltaArgs with the fields of its Heads in their place: filled in by position, without five more structures a call."""
-    _fields_ = [(name + part, kind) for name, of in DeltaArgs._fields_
-                for part, kind in ([("_" + p, t) for p, t in Heads._fields_] if of is Heads else [("", of)])]
+def _flat(args):
+    """The structure with the fields of the structures in it in their place: filled in by position, without as many more structures
+    a call."""
+    def fields(of):
+        for name, kind in of._fields_:
+            if issubclass(kind, ctypes.Structure):
+                assert ctypes.sizeof(kind) % 8 == 0 and getattr(of, name).offset % 8 == 0, name  # (no padding but their own)
+                yield from ((f"{name}_{part}", t) for part, t in fields(kind))
+            else:
+                yield name, kind
+    flat = type("_Flat" + args.__name__, (ctypes.Structure,), {"_fields_": list(fields(args))})
+    assert ctypes.sizeof(flat) == ctypes.sizeof(args)
+    return flat
+
+
+_FlatDeltaArgs = _flat(DeltaArgs)
 
 
 class NormArgs(ctypes.Structure):
@@ -60,6 +81,49 @@ class QuantArgs(ctypes.Structure):
     _fields_ = [("abi_version", _i32), ("dtype", _i32), ("act", _i32), ("n", _i32), ("k", _i32), ("m", _i64),
                 ("a", _vp), ("b", _vp), ("a_stride", _i64), ("b_stride", _i64), ("a_scale", _vp), ("b_scale", _vp),
                 ("bias", _vp), ("y", _vp), ("y_stride", _i64)]
+
+
+class CacheArgs(ctypes.Structure):
+    _fields_ = [("kind", _i32), ("n_pages", _i32), ("heads", _i32), ("page", _i32), ("d", _i32), ("k", _vp), ("v", _vp),
+                ("k_scale", _vp), ("v_scale", _vp), ("bounds", _vp)]
+
+
+class TokenArgs(ctypes.Structure):
+    _fields_ = [("n_seq", _i32), ("width", _i32), ("n_tokens", _i64), ("table", _vp), ("table_stride", _i64), ("past", _vp),
+                ("seq_offsets", _vp)]
+
+
+class AppendArgs(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("dtype", _i32), ("cache", CacheArgs), ("tokens", TokenArgs), ("heads_q", _i32), ("rot", _i32),
+                ("pairs", _i32), ("eps", _f32), ("q", Heads), ("k", Heads), ("v", Heads), ("q_out", _vp), ("q_out_token_stride", _i64),
+                ("q_out_head_stride", _i64), ("q_norm", _vp), ("k_norm", _vp), ("freqs", _vp), ("positions", _vp)]
+
+
+class ReadArgs(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("dtype", _i32), ("cache", CacheArgs), ("tokens", TokenArgs), ("k", _vp), ("v", _vp)]
+
+
+class AttendArgs(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("dtype", _i32), ("cache", CacheArgs), ("tokens", TokenArgs), ("heads_q", _i32), ("causal", _i32),
+                ("window", _i32), ("count", _i32), ("max_len", _i64), ("scale", _f32), ("q", Heads), ("o", _vp), ("o_token_stride", _i64),
+                ("o_head_stride", _i64), ("selected", _vp)]
+
+
+class SelectArgs(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("dtype", _i32), ("cache", CacheArgs), ("tokens", TokenArgs), ("heads_q", _i32), ("count", _i32),
+                ("first", _i32), ("last", _i32), ("max_len", _i64), ("q", Heads), ("selected", _vp)]
+
+
+class Cache(NamedTuple):
+    """A paged cache of keys and values (evconv_cache): k [pages, heads, page, dp] and v [pages, heads, dp, page] in bfloat16, or
+    with two 4-bit values to a byte (uint8, last dimensions halved) and fp32 scales [pages, heads, page].  bounds: bfloat16
+    [pages, heads, 2, dp], or None (cache_select needs them).  d: channels that count of the dp."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor]
+    v_scale: Optional[torch.Tensor]
+    bounds: Optional[torch.Tensor]
+    d: int
 
 
 class QuantRows(NamedTuple):
@@ -90,6 +154,9 @@ def _calls():
         L.evconv_delta_rule.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
         L.evconv_block_norm.argtypes = [_vp, _vp]
         L.evconv_quant_matmul.argtypes = [_vp, _vp]
+        L.evconv_cache_append.argtypes = L.evconv_cache_read.argtypes = [_vp, _vp]
+        L.evconv_cache_attend_workspace.argtypes = L.evconv_cache_select_workspace.argtypes = [_vp, _vp]
+        L.evconv_cache_attend.argtypes = L.evconv_cache_select.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
         _entry = L
     return _entry
 
@@ -353,4 +420,197 @@ def quant_matmul(a: QuantRows, b: QuantRows, *, bias=None, act="none", out_dtype
     args = QuantArgs(ABI_VERSION, _dtype(out, "out"), _ACTS[act], n, k, m, a_at, b_at, a_step, b_step,
                      _packed(a_scale, "a.scale", gpu, f32, (m,)), _packed(b_scale, "b.scale", gpu, f32, (n,)), bias, y_at, y_step)
     _enqueue(_calls().evconv_quant_matmul, args, gpu)
+    return out
+
+
+# ------------------------------------------------------------------- a paged cache
+
+def cache_channels(d):
+    """Channels that a head of `d` has in the cache (dp)."""
+    for dp in (32, 64, 96, 128, 192, 256):
+        if d <= dp:
+            return dp
+    _refuse(ERR_UNSUPPORTED, f"cache: heads of {d}: at most 256")
+
+
+def cache_new(n_pages, heads, d, *, page=64, kind="bf16", bounds=True, device="cuda") -> Cache:
+    """A cache of `n_pages` pages of `page` tokens (32, 64, 128 or 256), in "bf16" or "fp4" (4.5 bits a value at d = 64, 4.25 at 128).
+    What is in it is not set: no operator looks at tokens that were not appended.  bounds: keep what cache_select needs."""
+    if kind not in ("bf16", "fp4"):
+        _refuse(ERR_INVALID_ARG, f"cache: kind {kind!r}")
+    dp, new = cache_channels(d), lambda t, *shape: torch.empty(n_pages, heads, *shape, dtype=t, device=device)
+    low = new(torch.bfloat16, 2, dp) if bounds else None
+    if kind == "bf16":
+        return Cache(new(torch.bfloat16, page, dp), new(torch.bfloat16, dp, page), None, None, low, d)
+    return Cache(new(torch.uint8, page, dp // 2), new(torch.uint8, dp, page // 2), new(torch.float32, page), new(torch.float32, page), low, d)
+
+
+_FlatAppendArgs, _FlatReadArgs, _FlatAttendArgs, _FlatSelectArgs = (_flat(a) for a in (AppendArgs, ReadArgs, AttendArgs, SelectArgs))
+
+
+def _cache(cache, gpu):
+    """The fields of CacheArgs."""
+    k, v, k_scale, v_scale, bounds, d = cache
+    dtype = k.dtype
+    if v.dim() != 4 or (dtype is not torch.bfloat16 and dtype is not torch.uint8):
+        _refuse(ERR_INVALID_ARG, f"cache: k {tuple(k.shape)} {dtype}, v {tuple(v.shape)}")
+    pages, heads, dp, page = v.shape
+    if dp != cache_channels(d):
+        _refuse(ERR_SHAPE, f"cache: {dp} channels for heads of {d}, expected {cache_channels(d)}")
+    if bounds is not None:
+        bounds = _packed(bounds, "bounds", gpu, torch.bfloat16, (pages, heads, 2, dp))
+    if dtype is torch.bfloat16:
+        return (CACHE_BF16, pages, heads, page, d, _packed(k, "k cache", gpu, dtype, (pages, heads, page, dp)),
+                _packed(v, "v cache", gpu, dtype, (pages, heads, dp, page)), None, None, bounds)
+    page *= 2
+    scales = (pages, heads, page)
+    if k_scale is None or v_scale is None:
+        _refuse(ERR_INVALID_ARG, "cache: 4 bits without scales")
+    return (CACHE_FP4, pages, heads, page, d, _packed(k, "k cache", gpu, dtype, (pages, heads, page, dp // 2)),
+            _packed(v, "v cache", gpu, dtype, (pages, heads, dp, page // 2)), _packed(k_scale, "k_scale", gpu, torch.float32, scales),
+            _packed(v_scale, "v_scale", gpu, torch.float32, scales), bounds)
+
+
+def _tokens(n, table, past, seq_offsets, gpu):
+    """The fields of TokenArgs."""
+    if table.dim() != 2:
+        _refuse(ERR_SHAPE, f"table {tuple(table.shape)}: expected [sequences, pages]")
+    n_seq, width = table.shape
+    table, (step, _) = _rows(table, "table", gpu, torch.int32, (n_seq, width))
+    past = _packed(past, "past", gpu, torch.int32, (n_seq,))
+    if seq_offsets is not None:
+        seq_offsets = _packed(seq_offsets, "seq_offsets", gpu, torch.int32, (n_seq + 1,))
+    return n_seq, width, n, table, step, past, seq_offsets
+
+
+def _head_rows(t, name, gpu, dtype, shape):
+    """The fields of Heads."""
+    at, (token, head, _) = _rows(t, name, gpu, dtype, shape)
+    return at, token, head
+
+
+def cache_append(cache, k, v, table, past, q=None, *, seq_offsets=None, q_norm=None, k_norm=None, eps=1e-6, freqs=None, pairs="halves",
+                 positions=None, q_out=None):
+    """New tokens into a paged cache (evconv_cache_append).  Returns the queries as the attention wants them (None without q).
+
+    k, v: [tokens, heads, d], q: [tokens, heads_q, d], the last dimension contiguous (slices of one projection).
+    table: int32 [sequences, width], pages of each sequence; past: int32 [sequences], tokens that each has in the cache before the call
+    (not changed: `past += new` once all layers have appended).  Sequences have equally many new tokens, or those that seq_offsets (int32
+    [sequences + 1]) give.  q_norm, k_norm: fp32 [d], weights of the heads' norms; freqs: fp32 [rot / 2], the rotation of the first rot
+    channels, of pairs "halves" (i, i + rot / 2) or "neighbours" (2 i, 2 i + 1), by position * freqs.  positions: int64 [tokens], instead of
+    the places in the sequence.  q_out: where the queries go, may be q."""
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        _refuse(ERR_SHAPE, f"k {tuple(k.shape)}: expected [tokens, heads, d], q alike")
+    gpu, dtype, shape = k.get_device(), k.dtype, k.shape
+    if gpu < 0:
+        _explain(k, "k", gpu, dtype, shape)
+    if pairs not in _PAIRS:
+        _refuse(ERR_INVALID_ARG, f"cache append: pairs {pairs!r}")
+    fields = _cache(cache, gpu)
+    n, d, f32 = shape[0], fields[4], torch.float32
+    expected = (n, fields[2], d)
+    k_at = _head_rows(k, "k", gpu, dtype, expected)
+    v_at = _head_rows(v, "v", gpu, dtype, expected)
+    q_at = q_to = (None, 0, 0)
+    heads_q = rot = 0
+    if q is not None:
+        heads_q = q.shape[1]
+        q_at = _head_rows(q, "q", gpu, dtype, (n, heads_q, d))
+        if q_out is None:
+            q_out = _empty(n, heads_q, d, dtype=dtype, device=gpu)
+            q_to = (q_out.data_ptr(), heads_q * d, d)
+        else:
+            q_to = q_at if q_out is q else _head_rows(q_out, "q_out", gpu, dtype, (n, heads_q, d))
+    if freqs is not None:
+        rot = 2 * freqs.numel()
+        freqs = _packed(freqs, "freqs", gpu, f32, (rot // 2,))
+    a = _FlatAppendArgs(ABI_VERSION, _dtype(k, "k"), *fields, *_tokens(n, table, past, seq_offsets, gpu), heads_q, rot, _PAIRS[pairs], eps,
+                        *q_at, *k_at, *v_at, *q_to, _packed(q_norm, "q_norm", gpu, f32, (d,)), _packed(k_norm, "k_norm", gpu, f32, (d,)),
+                        freqs, _packed(positions, "positions", gpu, torch.int64, (n,)))  # (in the order of _fields_)
+    _enqueue(_calls().evconv_cache_append, a, gpu)
+    return q_out
+
+
+def cache_read(cache, table, past, n, *, seq_offsets=None, dtype=torch.float32):
+    """Keys and values of `n` tokens from position past[s] on of the sequences, as rows [n, heads, d] (evconv_cache_read)."""
+    gpu = table.get_device()
+    if gpu < 0:
+        _explain(table, "table", gpu, torch.int32, table.shape)
+    fields = _cache(cache, gpu)
+    if dtype not in _DTYPES:
+        _refuse(ERR_INVALID_ARG, f"cache read: {dtype}, expected float32 or bfloat16")
+    k = _empty(n, fields[2], fields[4], dtype=dtype, device=gpu)
+    v = _empty_like(k)
+    a = _FlatReadArgs(ABI_VERSION, _DTYPES[dtype], *fields, *_tokens(n, table, past, seq_offsets, gpu), k.data_ptr(), v.data_ptr())
+    _enqueue(_calls().evconv_cache_read, a, gpu)
+    return k, v
+
+
+def _bound(value, name):
+    """A limit that may be None, as the calls have it: 0 for none."""
+    if value is None:
+        return 0
+    if value < 1:
+        _refuse(ERR_INVALID_ARG, f"{name} {value}: at least 1, None for no limit")
+    return value
+
+
+def cache_attend(q, cache, table, past, *, seq_offsets=None, causal=True, window=None, scale=None, selected=None, max_len=None, out=None):
+    """Attention over a paged cache (evconv_cache_attend): [tokens, heads_q, d] like q.
+
+    q: [tokens, heads_q, d]; table, past, seq_offsets as of cache_append, with the same past: token i of a sequence sees the past + i + 1
+    first tokens (causal), of them the last `window`; or, without causal, the `past` ones.  selected: int32 [tokens, heads, count], the table
+    entries that each token and key head looks at (cache_select).  scale: of the scores, by default d ** -0.5.  max_len: no sequence has more tokens,
+    the call's among them; by default what a table row holds.  The closer it is, the better a call spreads over the GPU."""
+    if q.dim() != 3:
+        _refuse(ERR_SHAPE, f"q {tuple(q.shape)}: expected [tokens, heads, d]")
+    gpu, dtype, shape = q.get_device(), q.dtype, q.shape
+    if gpu < 0:
+        _explain(q, "q", gpu, dtype, shape)
+    fields = _cache(cache, gpu)
+    n, heads_q, d = shape[0], shape[1], fields[4]
+    q_at = _head_rows(q, "q", gpu, dtype, (n, heads_q, d))
+    count = 0
+    if selected is not None:
+        if selected.dim() != 3:
+            _refuse(ERR_SHAPE, f"selected {tuple(selected.shape)}: expected [tokens, heads, pages]")
+        count = selected.shape[2]
+        if count < 1:
+            _refuse(ERR_SHAPE, f"selected {tuple(selected.shape)}: no pages")
+        selected = _packed(selected, "selected", gpu, torch.int32, (n, fields[2], count))
+    if out is None:
+        out = _empty(n, heads_q, d, dtype=dtype, device=gpu)
+        o_at = (out.data_ptr(), heads_q * d, d)
+    else:
+        o_at = _head_rows(out, "out", gpu, dtype, (n, heads_q, d))
+    a = _FlatAttendArgs(ABI_VERSION, _dtype(q, "q"), *fields, *_tokens(n, table, past, seq_offsets, gpu), heads_q, 1 if causal else 0,
+                        _bound(window, "window"), count, _bound(max_len, "max_len"), d ** -0.5 if scale is None else scale,
+                        *q_at, *o_at, selected)  # (in the order of _fields_)
+    L = _calls()
+    _enqueue(L.evconv_cache_attend, a, gpu, L.evconv_cache_attend_workspace)
+    return out
+
+
+def cache_select(q, cache, table, past, count, *, seq_offsets=None, first=1, last=1, max_len=None, out=None):
+    """The pages that each token and key head should look at (evconv_cache_select): int32 [tokens, heads, count], ascending, then -1.
+
+    The `first` pages of the sequence and the `last` ones up to the token's own, then those whose keys' bounds allow the highest scores.
+    q as it goes to cache_attend; the rest as of cache_attend."""
+    if q.dim() != 3:
+        _refuse(ERR_SHAPE, f"q {tuple(q.shape)}: expected [tokens, heads, d]")
+    gpu, dtype, shape = q.get_device(), q.dtype, q.shape
+    if gpu < 0:
+        _explain(q, "q", gpu, dtype, shape)
+    fields = _cache(cache, gpu)
+    n, heads_q, heads = shape[0], shape[1], fields[2]
+    q_at = _head_rows(q, "q", gpu, dtype, (n, heads_q, fields[4]))
+    if out is None:
+        out = _empty(n, heads, count, dtype=torch.int32, device=gpu)
+        out_at = out.data_ptr()
+    else:
+        out_at = _packed(out, "out", gpu, torch.int32, (n, heads, count))
+    a = _FlatSelectArgs(ABI_VERSION, _dtype(q, "q"), *fields, *_tokens(n, table, past, seq_offsets, gpu), heads_q, count, first, last,
+                        _bound(max_len, "max_len"), *q_at, out_at)  # (in the order of _fields_)
+    L = _calls()
+    _enqueue(L.evconv_cache_select, a, gpu, L.evconv_cache_select_workspace)
     return out

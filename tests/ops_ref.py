@@ -86,3 +86,60 @@ def quant_matmul(qa, sa, qb, sb, bias=None, act="none"):
     if bias is not None:
         y = y + np.asarray(bias, np.float64)
     return {"none": lambda v: v, "relu": lambda v: np.where(v < 0, 0.0, v), "sigmoid": sigmoid, "tanh": np.tanh}[act](y)
+
+
+# ---- the paged cache
+
+LEVELS = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+def head_rows(x, weight, eps, freqs, pairs, positions):
+    """Norm and rotation of heads [n, heads, d]."""
+    x = np.array(x, np.float64)
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
+    if freqs is not None and len(freqs):
+        half = len(freqs)
+        a, b = (slice(0, half), slice(half, 2 * half)) if pairs == "halves" else (slice(0, 2 * half, 2), slice(1, 2 * half, 2))
+        turn = np.exp(1j * np.asarray(positions, np.float64)[:, None] * np.asarray(freqs, np.float64))[:, None]
+        z = (x[..., a] + 1j * x[..., b]) * turn
+        x[..., a], x[..., b] = z.real, z.imag
+    return x
+
+
+def fp4_rows(x):
+    """Codes and scales of rows of fp32, in fp32 as the header has it."""
+    x = np.asarray(x, np.float32)
+    m = np.abs(x).max(-1)
+    with np.errstate(all="ignore"):
+        y = (np.float32(6) * x / np.where(m > 0, m, np.float32(1))[..., None]).astype(np.float64)
+        scale = m / np.float32(6)
+    middle = (LEVELS[1:] + LEVELS[:-1]) / 2
+    up = np.where(np.arange(7) % 2 == 1, np.abs(y)[..., None] >= middle, np.abs(y)[..., None] > middle)
+    code = up.sum(-1) + 8 * (y < 0)
+    fine = np.isfinite(m)
+    return np.where(fine[..., None], code, 0).astype(np.uint8), np.where(fine, scale, np.float32(np.nan))
+
+
+def fp4_values(code, scale):
+    return np.where(code & 8, -1.0, 1.0) * LEVELS[code & 7] * np.asarray(scale, np.float64)[..., None]
+
+
+def attend(q, k, v, scale, seen):
+    """One head's rows: q [n, d], k, v [t, d], seen [n, t].  (o, the weights' sum over |v|)."""
+    with np.errstate(all="ignore"):
+        x = np.where(seen, q @ k.T * scale, -np.inf)
+        top = x.max(-1, keepdims=True, initial=-np.inf)
+        p = np.where(seen, np.exp(x - np.where(np.isfinite(top), top, 0)), 0)
+        p = p / np.maximum(p.sum(-1, keepdims=True), 1e-300)
+        hidden = ~seen.any(0)
+        v = np.where(hidden[:, None], 0, v)
+        return p @ v, p @ np.abs(v)
+
+
+def choose(score, count, first, last):
+    """Pages 0 .. len(score) - 1, the last one the query's own: the first and last ones, then by score."""
+    n = len(score)
+    rank = [(0, 0, i) if i < first or i >= n - last else (1, -np.inf if np.isnan(score[i]) else -float(score[i]), i) for i in range(n)]
+    chosen = sorted(i for _, _, i in sorted(rank)[:count])
+    return chosen + [-1] * (count - len(chosen))
