@@ -2,8 +2,8 @@
 //
 // A workgroup takes the call's tokens of one page, in pieces of 32 slots, and a group of the heads; of a piece it computes the
 // rotation's cosines and sines once, in LDS, for all its heads (in 64 bits: some 150 instructions an angle, which 40 heads that
-// did it for themselves would spend twice the copy's time on).  A wave then takes a head at a time: eight channels to a
-// lane, 64 / lanes tokens at once.  Whole pages belong to one workgroup, so that bounds and half-filled bytes are read, changed and
+// did it for themselves would spend twice the copy's time on).  A wave then takes a head at a time, 16 channels to a lane: two vectors
+// of eight that the rotation mixes, so that no lane needs another's.  Whole pages belong to one workgroup, so that bounds and half-filled bytes are read, changed and
 // written by one wave.  Bound by the rows' bytes; for single tokens by the chain of a launch, a search, a read, two sums and a write.
 #include <algorithm>
 
@@ -17,94 +17,212 @@ constexpr int kPiece = 32;  // slots that are dealt with at once
 struct AppendParams {
   evconv_append_args a;
   int dp, log;      // padded channels, log2 of the page
-  int lanes;        // of a row: the power of two that holds dp / 8
+  double per_channel;  // 1 / d
   int per;          // pages that a sequence of equal lengths can reach, or -1
   int roles;        // heads of queries and of keys with their values together
   int groups;       // workgroups that share the roles of a page
   int64_t block0;   // first workgroup of this launch
-  bool pairs_wide;  // partners of rotated channels in whole vectors
+  bool single;      // one token of every sequence
 };
 
-__device__ __forceinline__ double lanes_sum(double v, int lanes) {
-  for (int d = 1; d < lanes; d *= 2) v += __shfl_xor(v, d);
+// How the rows of a call are read and turned: anything, a value at a time; vectors, partners of the rotation in whole vectors (or no
+// rotation); vectors, partners next to each other.
+enum { kAnyRows, kHalves, kNeighbours };
+
+template <int LANES>
+__device__ __forceinline__ double lanes_sum(double v) {
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) v += __shfl_xor(v, d);
   return v;
 }
-__device__ __forceinline__ unsigned lanes_max(unsigned v, int lanes) {
-  for (int d = 1; d < lanes; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
+template <int LANES>
+__device__ __forceinline__ unsigned lanes_max(unsigned v) {
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
   return v;
 }
 
-// 1 / sqrt(m) rounded to fp32, of m in 64 bits (positive): the hardware's estimate and two terms of the series of its error e,
-// y (1 + e / 2 + 3 e^2 / 8), which leaves 2^-60.
+// 1 / sqrt(m) rounded to fp32, of m in 64 bits: the hardware's estimate (2^-26 and better) and two terms of the series of its error e,
+// y (1 + e / 2 + 3 e^2 / 8), which leaves less than 2^-60.
 __device__ __forceinline__ float inverse_root(double m) {
-  if (!(m > 1e-37 && m < 1e37)) return (float)(1.0 / sqrt(m));
-  const double y = (double)__builtin_amdgcn_rsqf((float)m);
-  const double e = 1.0 - m * y * y;
-  return (float)(y + y * e * (0.5 + 0.375 * e));
+  const double y = __builtin_amdgcn_rsq(m);
+  const double e = fma(-m * y, y, 1.0);
+  return (float)fma(y * e, fma(e, 0.375, 0.5), y);
 }
 
-// Norm and rotation of eight channels from `ch` on of one row.  No contraction: each product and sum is rounded by itself, so that
-// the codes of a 4-bit row do not depend on how the compiler joins them.
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void head_row(const AppendParams& p, const void* src, int64_t at, int ch, int left, const float* weight, const float* cosines,
-                                         const float* sines, float (&x)[8]) {
+// Sine and cosine of an angle in 64 bits, rounded to fp32: the angle less the nearest multiple of pi / 2 (in two parts of 53 bits; their
+// product with the multiple is exact in the fused operation as far as it counts), then the Taylor series, whose first terms left out are
+// 2^-54 and 2^-49 at pi / 4.  Angles from 2^45 on, of which 64 bits hold less than 2^-8, are none.
+__device__ __forceinline__ void sine_cosine(double angle, float& sine, float& cosine) {
+  if (!(fabs(angle) < 0x1p45)) angle = 0.0;
+  const double turns = rint(angle * 0.63661977236758134308);
+  double r = fma(-turns, 1.57079632679489661923, angle);
+  r = fma(-turns, 6.12323399573676603587e-17, r);
+  const double z = r * r;
+  double s = fma(z, -1.0 / 1307674368000.0, 1.0 / 6227020800.0), c = fma(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  c = fma(c, z, -1.0 / 720.0);
+  s = fma(s, z, 1.0 / 120.0);
+  c = fma(c, z, 1.0 / 24.0);
+  s = fma(s, z, -1.0 / 6.0);
+  c = fma(c, z, -0.5);
+  s = fma(s * z, r, r);
+  c = fma(c, z, 1.0);
+  const int quarter = (int)((long long)turns & 3);
+  const double u = quarter & 1 ? c : s, v = quarter & 1 ? s : c;
+  sine = (float)(quarter & 2 ? -u : u);
+  cosine = (float)(quarter == 1 || quarter == 2 ? -v : v);
+}
+
+// The channels of a lane: two vectors of eight, ch[0] and ch[1] on, with left[] of them inside (not positive: none).
+struct Channels {
+  int ch[2], left[2];
+  int at[2];  // ch, inside the padded row
+};
+template <int MODE>
+__device__ __forceinline__ Channels channels_of(const AppendParams& p, int l) {
+  Channels c;
+  c.ch[0] = 16 * l;
+  c.ch[1] = c.ch[0] + 8;
+  if (MODE == kHalves) {
+    const int pairs = p.a.rot / 16;
+    if (l < pairs) {
+      c.ch[0] = 8 * l;
+      c.ch[1] = p.a.rot / 2 + 8 * l;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    c.left[i] = p.a.cache.d - c.ch[i];
+    c.at[i] = min(c.ch[i], p.dp - 8);
+  }
+  return c;
+}
+
+// A row's two vectors.  (Vectors: what is outside is read inside, where it costs no branch, and set to zero.)
+template <bool BF16, int MODE>
+__device__ __forceinline__ void load_row(const void* src, int64_t at, const Channels& c, int d, float (&x)[2][8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (MODE == kAnyRows) {
+      load_run<BF16, 8, false>(src, at + c.ch[i], c.left[i], x[i]);
+    } else {
+      load_run<BF16, 8, true>(src, at + min(c.ch[i], d - 8), 8, x[i]);
+    }
+  }
+}
+template <int MODE>
+__device__ __forceinline__ void zero_outside(const Channels& c, float (&x)[2][8]) {
+  if constexpr (MODE != kAnyRows)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c.left[i] <= 0) x[i][j] = 0.0f;
+}
+
+// Cosines and sines of a token's angles: a row of LDS, or computed where they are wanted.
+struct SharedAngles {
+  const float *cosines, *sines;
+  __device__ __forceinline__ void one(int f, float& co, float& si) const { co = cosines[f], si = sines[f]; }
+  __device__ __forceinline__ void eight(int f, float (&co)[8], float (&si)[8]) const {  // (f a multiple of eight, and the row's length)
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      const f32x4 c = *(const f32x4*)(cosines + f + j), s = *(const f32x4*)(sines + f + j);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) co[j + k] = c[k], si[j + k] = s[k];
+    }
+  }
+};
+struct OwnAngles {
+  double position;
+  const float* freqs;
+  __device__ __forceinline__ void one(int f, float& co, float& si) const { sine_cosine(position * (double)freqs[f], si, co); }
+  __device__ __forceinline__ void eight(int f, float (&co)[8], float (&si)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) one(f + j, co[j], si[j]);
+  }
+};
+
+// Norm and rotation of a row; `weight` has whole padded rows.  No contraction: each product and sum is rounded by itself, so
+// that the codes of a 4-bit row do not depend on how the compiler joins them.
+template <bool BF16, int MODE, int LANES, typename Angles>
+__device__ __forceinline__ void turn_row(const AppendParams& p, const void* src, int64_t at, const Channels& c, bool norm, const float* weight,
+                                         const Angles& angles, float (&x)[2][8]) {
 #pragma clang fp contract(off)
-  load_run<BF16, 8, VEC>(src, at + ch, left, x);
   const int rot = p.a.rot, half = rot / 2;
   float scale = 1.0f;
-  if (weight) {
+  if (norm) {
     double sum = 0.0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += (double)x[j] * (double)x[j];
-    sum = lanes_sum(sum, p.lanes);
-    scale = inverse_root(sum / (double)p.a.cache.d + (double)p.a.eps);
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) x[j] = x[j] * scale * weight[ch + j];
-  }
-  if (ch >= rot) return;
-  if (p.a.pairs == EVCONV_PAIRS_NEIGHBOURS) {
+      for (int j = 0; j < 8; ++j) sum = fma((double)x[i][j], (double)x[i][j], sum);
+    scale = inverse_root(fma(lanes_sum<LANES>(sum), p.per_channel, (double)p.a.eps));
 #pragma unroll
-    for (int j = 0; j < 8; j += 2)
-      if (ch + j < rot) {
-        const float c = cosines[(ch + j) / 2], s = sines[(ch + j) / 2], u = x[j], v = x[j + 1];
-        x[j] = u * c - v * s;
-        x[j + 1] = v * c + u * s;
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; j += 4) {
+        const f32x4 w = *(const f32x4*)(weight + c.at[i] + j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[i][j + k] = x[i][j + k] * scale * w[k];
       }
-    return;
   }
-  if (p.pairs_wide) {  // a vector is of one half
-    const bool low = ch < half;
-    const int other = low ? ch + half : ch - half, f = low ? ch : other;
-    float y[8];
-    load_run<BF16, 8, VEC>(src, at + other, 8, y);
+  if (!rot) return;
+  if constexpr (MODE == kHalves) {
+    if (c.ch[0] >= half) return;
+    float co[8], si[8];
+    angles.eight(c.ch[0], co, si);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (weight) y[j] = y[j] * scale * weight[other + j];
-      const float c = cosines[f + j], s = sines[f + j];
-      const float xc = x[j] * c, ys = y[j] * s;
-      x[j] = low ? xc - ys : xc + ys;
+      const float u = x[0][j], v = x[1][j];
+      x[0][j] = u * co[j] - v * si[j];
+      x[1][j] = v * co[j] + u * si[j];
     }
-    return;
-  }
+  } else if (MODE == kNeighbours || p.a.pairs == EVCONV_PAIRS_NEIGHBOURS) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (ch + j >= rot) break;
-    const bool low = ch + j < half;
-    const int other = low ? ch + j + half : ch + j - half, f = low ? ch + j : other;
-    float y = load_one<BF16>(src, at + other);
-    if (weight) y = y * scale * weight[other];
-    const float xc = x[j] * cosines[f], ys = y * sines[f];
-    x[j] = low ? xc - ys : xc + ys;
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; j += 2)
+        if (c.ch[i] + j < rot) {
+          float co, si;
+          angles.one((c.ch[i] + j) / 2, co, si);
+          const float u = x[i][j], v = x[i][j + 1];
+          x[i][j] = u * co - v * si;
+          x[i][j + 1] = v * co + u * si;
+        }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int ch = c.ch[i] + j;
+        if (ch >= rot) break;
+        const bool low = ch < half;
+        const int other = low ? ch + half : ch - half, f = low ? ch : other;
+        float v = load_one<BF16>(src, at + other);
+        if (norm) v = v * scale * weight[other];
+        float co, si;
+        angles.one(f, co, si);
+        const float xc = x[i][j] * co, ys = v * si;
+        x[i][j] = low ? xc - ys : xc + ys;
+      }
   }
 }
 
 // Largest magnitude's bits of a row, over its lanes
-__device__ __forceinline__ unsigned row_largest(const float (&x)[8], int lanes) {
+template <int LANES>
+__device__ __forceinline__ unsigned row_largest(const float (&x)[2][8]) {
   unsigned m = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
-  return lanes_max(m, lanes);
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[i][j]) & 0x7fffffffu);
+  return lanes_max<LANES>(m);
 }
 constexpr unsigned kNoBf16 = 0x7f7f8000u;  // magnitudes from these bits on are no finite bf16 numbers
 
@@ -150,9 +268,12 @@ __device__ __forceinline__ void store_row(void* q, int64_t at, int ch, int left,
 // and those of its neighbours do not meet in a bank.
 __host__ __device__ constexpr int value_row(bool fp4) { return (fp4 ? 1 : 2) * kPiece + 4; }
 
-template <bool BF16, bool FP4, bool VEC>
-__global__ __launch_bounds__(256) void cache_append(AppendParams p) {
-  extern __shared__ char s_mem[];
+template <bool BF16, bool FP4, int MODE, int LANES>
+__global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(AppendParams p) {
+  constexpr bool VEC = MODE != kAnyRows;
+  constexpr int ROWS = 64 / LANES;                    // tokens that a wave deals with at once
+  constexpr int AT_ONCE = !VEC || LANES < 4 ? 1 : 2;  // ... has under way, of a query head, times that
+  extern __shared__ __align__(16) char s_mem[];
   const evconv_append_args& a = p.a;
   const evconv_cache& c = a.cache;
   const evconv_tokens& tk = a.tokens;
@@ -165,11 +286,18 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
   if (begin >= end) return;
   const int to = page_of(c, tk, piece.seq, page);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  const int rows = 64 / p.lanes, row = lane / p.lanes, ch = lane % p.lanes * 8, left = d - ch;
+  const int row = lane / LANES;
+  const Channels own = channels_of<MODE>(p, lane % LANES);
   float* const s_cos = (float*)s_mem;
   float* const s_sin = s_cos + kPiece * half;
-  char* const s_v = s_mem + 2 * sizeof(float) * kPiece * half + wave * p.dp * value_row(FP4);
+  char* const s_v = s_mem + 2 * sizeof(float) * (kPiece * half + p.dp) + wave * p.dp * value_row(FP4);
   const int per_group = (p.roles + p.groups - 1) / p.groups, role_end = min((group + 1) * per_group, p.roles);
+  float* const s_wq = (float*)(s_mem + 2 * sizeof(float) * kPiece * half);  // weights of the norms, zeros behind them
+  float* const s_wk = s_wq + p.dp;
+  for (int i = threadIdx.x; i < p.dp; i += blockDim.x) {
+    s_wq[i] = a.q_norm && i < d ? a.q_norm[i] : 0.0f;
+    s_wk[i] = a.k_norm && i < d ? a.k_norm[i] : 0.0f;
+  }
   for (int64_t sub = begin & ~(int64_t)(kPiece - 1); sub < end; sub += kPiece) {
     const int64_t from = max(sub, begin);
     const int count = (int)(min(sub + kPiece, end) - from), token = piece.first + (int)(from - past);
@@ -177,50 +305,64 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
     __syncthreads();  // (the last piece's angles have been read)
     for (int i = threadIdx.x; i < count * half; i += blockDim.x) {
       const int r = i / half, f = i - r * half;
-      double s, co;
-      sincos((double)(a.positions ? a.positions[token + r] : from + r) * (double)a.freqs[f], &s, &co);
-      s_cos[i] = (float)co;
-      s_sin[i] = (float)s;
+      sine_cosine((double)(a.positions ? a.positions[token + r] : from + r) * (double)a.freqs[f], s_sin[i], s_cos[i]);
     }
     __syncthreads();
-    for (int role = group * per_group + wave; role < role_end; role += waves) {
-      if (role < a.heads_q) {  // ---- a head of the queries
-        for (int r0 = 0; r0 < count; r0 += rows) {
-          const int r = r0 + row;
-          const bool live = r < count;
-          const int64_t t = token + (live ? r : 0);
-          float x[8];
-          head_row<BF16, VEC>(p, a.q.data, t * a.q.token_stride + role * a.q.head_stride, ch, live ? left : 0, a.q_norm, s_cos + (live ? r : 0) * half,
-                              s_sin + (live ? r : 0) * half, x);
-          store_row<VEC>(a.q_out, t * a.q_out_token_stride + role * a.q_out_head_stride, ch, live ? left : 0, x, BF16);
+    int role = group * per_group + wave;
+    for (; role < min(role_end, a.heads_q); role += waves) {  // ---- a head of the queries
+      const int64_t head_in = role * a.q.head_stride, head_out = role * a.q_out_head_stride;
+      for (int r0 = 0; r0 < count; r0 += AT_ONCE * ROWS) {
+        float x[AT_ONCE][2][8];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int r = min(r0 + i * ROWS + row, count - 1);
+          load_row<BF16, MODE>(a.q.data, (token + r) * a.q.token_stride + head_in, own, d, x[i]);
         }
-        continue;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (r0 + i * ROWS >= count) break;
+          const int r = r0 + i * ROWS + row, r_in = min(r, count - 1);
+          zero_outside<MODE>(own, x[i]);
+          turn_row<BF16, MODE, LANES>(p, a.q.data, (token + r_in) * a.q.token_stride + head_in, own, a.q_norm, s_wq, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x[i]);
+          const int64_t at = (token + r_in) * a.q_out_token_stride + head_out;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) store_row<VEC>(a.q_out, at, own.ch[h], r < count ? own.left[h] : 0, x[i][h], BF16);
+        }
       }
-      // ---- a head of the keys and the values
-      if (to < 0) continue;
+    }
+    for (; role < role_end && to >= 0; role += waves) {  // ---- a head of the keys and the values
       const int head = role - a.heads_q;
       const int64_t at = ((int64_t)to * c.heads + head) * c.page;  // tokens before this head's of the page
-      float lo[8], hi[8];
+      const int64_t k_head = head * a.k.head_stride, v_head = head * a.v.head_stride;
+      float lo[2][8], hi[2][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) lo[j] = INFINITY, hi[j] = -INFINITY;
-      for (int r0 = 0; r0 < count; r0 += rows) {
-        const int r = r0 + row;
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lo[h][j] = INFINITY, hi[h][j] = -INFINITY;
+      for (int r0 = 0; r0 < count; r0 += ROWS) {
+        const int r = r0 + row, r_in = min(r, count - 1);
         const bool live = r < count;
-        const int64_t t = token + (live ? r : 0);
-        float x[8], v[8];
-        load_run<BF16, 8, VEC>(a.v.data, t * a.v.token_stride + head * a.v.head_stride + ch, live ? left : 0, v);
-        head_row<BF16, VEC>(p, a.k.data, t * a.k.token_stride + head * a.k.head_stride, ch, live ? left : 0, a.k_norm, s_cos + (live ? r : 0) * half,
-                            s_sin + (live ? r : 0) * half, x);
-        const unsigned big_k = row_largest(x, p.lanes), big_v = row_largest(v, p.lanes);
-        const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
-        if (bad)
+        const int64_t k_row = (token + r_in) * a.k.token_stride + k_head;
+        float x[2][8], v[2][8];
+        load_row<BF16, MODE>(a.k.data, k_row, own, d, x);
+        load_row<BF16, MODE>(a.v.data, (token + r_in) * a.v.token_stride + v_head, own, d, v);
+        zero_outside<MODE>(own, x);
+        zero_outside<MODE>(own, v);
+        turn_row<BF16, MODE, LANES>(p, a.k.data, k_row, own, a.k_norm, s_wk, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x);
+        const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
+        if (big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16))
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < left) x[j] = NAN;
-        const bool there = live && ch < p.dp;
-        if constexpr (FP4) {
-          const unsigned k4 = codes_of(x, big_k), v4 = codes_of(v, big_v);
-          if (there) {
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < own.left[h]) x[h][j] = NAN;
+        if (!live) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int ch = own.ch[h];
+          if (ch >= p.dp) continue;
+          if constexpr (FP4) {
+            const unsigned k4 = codes_of(x[h], big_k), v4 = codes_of(v[h], big_v);
             *(unsigned*)((char*)c.k + (at + slot + r) * (p.dp / 2) + ch / 2) = k4;
 #pragma unroll
             for (int j = 0; j < 8; ++j) s_v[(ch + j) * value_row(true) + slot % kPiece + r] = (char)(v4 >> (4 * j) & 15);
@@ -228,32 +370,33 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
               c.k_scale[at + slot + r] = scale_of(big_k);
               c.v_scale[at + slot + r] = scale_of(big_v);
             }
-          }
-        } else if (there) {
-          *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) =
-              make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+          } else {
+            *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) =
+                make_uint4(pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7]));
 #pragma unroll
-          for (int j = 0; j < 8; j += 2) {
-            unsigned w = pack_bf16(v[j], v[j + 1]);
-            if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;  // (no value of v that is not finite)
-            if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
-            if (count == kPiece) {
-              *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * r) = (uint16_t)w;
-              *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * r) = (uint16_t)(w >> 16);
-            } else {
-              uint16_t* const q = (uint16_t*)c.v + ((int64_t)to * c.heads + head) * p.dp * c.page + (int64_t)(ch + j) * c.page + slot + r;
-              q[0] = (uint16_t)w;
-              q[c.page] = (uint16_t)(w >> 16);
+            for (int j = 0; j < 8; j += 2) {
+              unsigned w = pack_bf16(v[h][j], v[h][j + 1]);
+              if (big_v >= kNoBf16) {  // (no value of v that is not finite)
+                if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+                if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+              }
+              if (count == kPiece) {
+                *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * r) = (uint16_t)w;
+                *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * r) = (uint16_t)(w >> 16);
+              } else {
+                uint16_t* const q = (uint16_t*)c.v + ((int64_t)to * c.heads + head) * p.dp * c.page + (int64_t)(ch + j) * c.page + slot + r;
+                q[0] = (uint16_t)w;
+                q[c.page] = (uint16_t)(w >> 16);
+              }
             }
           }
-        }
-        if (live)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float k = bf16_low(pack_bf16(x[j], 0.0f));  // (as the cache in bf16 has it; a NaN stays in both bounds)
-            if (k < lo[j] || k != k) lo[j] = k;
-            if (k > hi[j] || k != k) hi[j] = k;
+            const float k = bf16_low(pack_bf16(x[h][j], 0.0f));  // (as the cache in bf16 has it; a NaN stays in both bounds)
+            if (k < lo[h][j] || k != k) lo[h][j] = k;
+            if (k > hi[h][j] || k != k) hi[h][j] = k;
           }
+        }
       }
       lds_turn();
       // ---- the values' rows of channels
@@ -287,32 +430,135 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
       }
       lds_turn();
       // ---- bounds: over the piece's tokens, then with what the page had unless it begins here
-      if (c.bounds) {
+      if (!c.bounds) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          for (int s = p.lanes; s < 64; s *= 2) {
-            const float l = __shfl_xor(lo[j], s), h = __shfl_xor(hi[j], s);
-            if (l < lo[j] || l != l) lo[j] = l;
-            if (h > hi[j] || h != h) hi[j] = h;
+#pragma unroll
+          for (int s = LANES; s < 64; s *= 2) {
+            const float l = __shfl_xor(lo[h][j], s), u = __shfl_xor(hi[h][j], s);
+            if (l < lo[h][j] || l != l) lo[h][j] = l;
+            if (u > hi[h][j] || u != u) hi[h][j] = u;
           }
-        if (row == 0 && ch < p.dp) {
-          uint4* const q = (uint4*)((uint16_t*)c.bounds + (((int64_t)to * c.heads + head) * 2) * p.dp + ch);
+        if (row == 0 && own.ch[h] < p.dp) {
+          uint4* const q = (uint4*)((uint16_t*)c.bounds + (((int64_t)to * c.heads + head) * 2) * p.dp + own.ch[h]);
           uint4* const q_hi = (uint4*)((uint16_t*)q + p.dp);
           if (slot > 0) {
             float old[8];
             load_run<true, 8, true>(q, 0, 8, old);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              if (old[j] < lo[j] || old[j] != old[j]) lo[j] = old[j];
+              if (old[j] < lo[h][j] || old[j] != old[j]) lo[h][j] = old[j];
             load_run<true, 8, true>(q_hi, 0, 8, old);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              if (old[j] > hi[j] || old[j] != old[j]) hi[j] = old[j];
+              if (old[j] > hi[h][j] || old[j] != old[j]) hi[h][j] = old[j];
           }
-          *q = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(lo[4], lo[5]), pack_bf16(lo[6], lo[7]));
-          *q_hi = make_uint4(pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]), pack_bf16(hi[4], hi[5]), pack_bf16(hi[6], hi[7]));
+          *q = make_uint4(pack_bf16(lo[h][0], lo[h][1]), pack_bf16(lo[h][2], lo[h][3]), pack_bf16(lo[h][4], lo[h][5]), pack_bf16(lo[h][6], lo[h][7]));
+          *q_hi = make_uint4(pack_bf16(hi[h][0], hi[h][1]), pack_bf16(hi[h][2], hi[h][3]), pack_bf16(hi[h][4], hi[h][5]), pack_bf16(hi[h][6], hi[h][7]));
         }
       }
+    }
+  }
+}
+
+// One new token of every sequence: a wave to a head of 64 / LANES of them, each lane with its own angles, nothing shared: no barrier and no
+// second round of anything, since all that such a call takes is the chain from the launch to the last write.
+template <bool BF16, bool FP4, int MODE, int LANES>
+__global__ __launch_bounds__(64) void append_single(AppendParams p) {
+  constexpr bool VEC = MODE != kAnyRows;
+  constexpr int ROWS = 64 / LANES;
+  __shared__ float s_weight[256];
+  const evconv_append_args& a = p.a;
+  const evconv_cache& c = a.cache;
+  const evconv_tokens& tk = a.tokens;
+  const int64_t block = p.block0 + blockIdx.x;
+  const int lane = threadIdx.x, d = c.d, role = (int)(block % p.roles);
+  const int64_t t0 = block / p.roles * ROWS + lane / LANES;
+  const bool live = t0 < tk.n_tokens;
+  const int64_t token = min(t0, tk.n_tokens - 1);
+  const Channels own = channels_of<MODE>(p, lane % LANES);
+  const bool query = role < a.heads_q;
+  const evconv_heads& src = query ? a.q : a.k;
+  const int head = query ? role : role - a.heads_q;
+  const int64_t row = token * src.token_stride + head * src.head_stride;
+  const float* const norm = query ? a.q_norm : a.k_norm;
+  float x[2][8], v[2][8];
+  load_row<BF16, MODE>(src.data, row, own, d, x);
+  if (!query) load_row<BF16, MODE>(a.v.data, token * a.v.token_stride + head * a.v.head_stride, own, d, v);
+  const int past = tk.past[token];
+  if (norm)
+    for (int i = lane; i < p.dp; i += 64) s_weight[i] = i < d ? norm[i] : 0.0f;
+  lds_turn();
+  const double position = (double)(a.positions ? a.positions[token] : (int64_t)past);
+  const int to = past < 0 ? -1 : page_of(c, tk, (int)token, past >> p.log);
+  zero_outside<MODE>(own, x);
+  turn_row<BF16, MODE, LANES>(p, src.data, row, own, norm, s_weight, OwnAngles{position, a.freqs}, x);
+  if (query) {
+    const int64_t at = token * a.q_out_token_stride + head * a.q_out_head_stride;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) store_row<VEC>(a.q_out, at, own.ch[h], live ? own.left[h] : 0, x[h], BF16);
+    return;
+  }
+  zero_outside<MODE>(own, v);
+  const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
+  if (big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16))
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < own.left[h]) x[h][j] = NAN;
+  if (!live || to < 0) return;
+  const int slot = past & (c.page - 1);
+  const int64_t at = ((int64_t)to * c.heads + head) * c.page + slot, column = ((int64_t)to * c.heads + head) * p.dp;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int ch = own.ch[h];
+    if (ch >= p.dp) continue;
+    if constexpr (FP4) {
+      uint8_t* const q = (uint8_t*)c.v + (column + ch) * (c.page / 2) + slot / 2;
+      unsigned old[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) old[j] = q[j * (c.page / 2)];
+      const unsigned v4 = codes_of(v[h], big_v);
+      const int shift = slot % 2 * 4;
+      *(unsigned*)((char*)c.k + at * (p.dp / 2) + ch / 2) = codes_of(x[h], big_k);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j * (c.page / 2)] = (uint8_t)((old[j] & (0xf0u >> shift)) | (v4 >> (4 * j) & 15) << shift);
+      if (ch == 0) {
+        c.k_scale[at] = scale_of(big_k);
+        c.v_scale[at] = scale_of(big_v);
+      }
+    } else {
+      *(uint4*)((uint16_t*)c.k + at * p.dp + ch) =
+          make_uint4(pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7]));
+      uint16_t* const q = (uint16_t*)c.v + (column + ch) * c.page + slot;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned w = pack_bf16(v[h][j], 0.0f) & 0xffffu;
+        q[j * c.page] = (uint16_t)((w & 0x7f80u) == 0x7f80u ? 0 : w);
+      }
+    }
+    if (c.bounds) {
+      uint4* const q = (uint4*)((uint16_t*)c.bounds + 2 * column + ch);
+      uint4* const q_hi = (uint4*)((uint16_t*)q + p.dp);
+      float lo[8], hi[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lo[j] = hi[j] = bf16_low(pack_bf16(x[h][j], 0.0f));
+      if (slot > 0) {
+        float old[8];
+        load_run<true, 8, true>(q, 0, 8, old);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (old[j] < lo[j] || old[j] != old[j]) lo[j] = old[j];
+        load_run<true, 8, true>(q_hi, 0, 8, old);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (old[j] > hi[j] || old[j] != old[j]) hi[j] = old[j];
+      }
+      *q = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(lo[4], lo[5]), pack_bf16(lo[6], lo[7]));
+      *q_hi = make_uint4(pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]), pack_bf16(hi[4], hi[5]), pack_bf16(hi[6], hi[7]));
     }
   }
 }
@@ -370,15 +616,32 @@ __global__ __launch_bounds__(256) void cache_read(ReadParams p) {
   }
 }
 
-template <bool BF16, bool FP4>
-void start_append(AppendParams p, bool vec, int64_t blocks, hipStream_t s) {
-  const size_t lds = 2 * sizeof(float) * kPiece * (p.a.rot / 2) + 4 * p.dp * value_row(FP4);
-  const int64_t most = kMostThreads / 256;
-  for (; p.block0 < blocks; p.block0 += most) {
-    const unsigned grid = (unsigned)std::min(most, blocks - p.block0);
-    if (vec) cache_append<BF16, FP4, true><<<grid, 256, lds, s>>>(p);
-    else cache_append<BF16, FP4, false><<<grid, 256, lds, s>>>(p);
+template <bool BF16, bool FP4, int MODE, int LANES>
+void start_append(AppendParams p, int64_t blocks, hipStream_t s) {
+  if (p.single) {
+    const int64_t blocks_single = (p.a.tokens.n_tokens + 64 / LANES - 1) / (64 / LANES) * p.roles, most = kMostThreads / 64;
+    for (; p.block0 < blocks_single; p.block0 += most)
+      append_single<BF16, FP4, MODE, LANES><<<(unsigned)std::min(most, blocks_single - p.block0), 64, 0, s>>>(p);
+    return;
   }
+  const size_t lds = 2 * sizeof(float) * (kPiece * (p.a.rot / 2) + p.dp) + 4 * p.dp * value_row(FP4);
+  const int64_t most = kMostThreads / 256;
+  for (; p.block0 < blocks; p.block0 += most)
+    cache_append<BF16, FP4, MODE, LANES><<<(unsigned)std::min(most, blocks - p.block0), 256, lds, s>>>(p);
+}
+// Lanes of a row: the power of two that holds its channels by sixteens.
+template <bool BF16, bool FP4, int MODE>
+void start_append(const AppendParams& p, int64_t blocks, hipStream_t s) {
+  if (p.dp <= 32) start_append<BF16, FP4, MODE, 2>(p, blocks, s);
+  else if (p.dp <= 64) start_append<BF16, FP4, MODE, 4>(p, blocks, s);
+  else if (p.dp <= 128) start_append<BF16, FP4, MODE, 8>(p, blocks, s);
+  else start_append<BF16, FP4, MODE, 16>(p, blocks, s);
+}
+template <bool BF16, bool FP4>
+void start_append(const AppendParams& p, bool vec, int64_t blocks, hipStream_t s) {
+  if (vec && p.a.rot && p.a.pairs == EVCONV_PAIRS_NEIGHBOURS) start_append<BF16, FP4, kNeighbours>(p, blocks, s);
+  else if (vec && p.a.rot % 16 == 0) start_append<BF16, FP4, kHalves>(p, blocks, s);
+  else start_append<BF16, FP4, kAnyRows>(p, blocks, s);
 }
 
 }  // namespace
@@ -388,12 +651,11 @@ void launch_cache_append(const evconv_append_args& a, bool vec, hipStream_t s) {
   p.a = a;
   p.dp = cache_channels(a.cache.d);
   p.log = __builtin_ctz(a.cache.page);
-  p.lanes = 1;
-  while (p.lanes * 8 < p.dp) p.lanes *= 2;
+  p.per_channel = 1.0 / a.cache.d;
   const evconv_tokens& t = a.tokens;
   p.per = t.seq_offsets ? -1 : (int)((t.n_tokens / t.n_seq + a.cache.page - 2) / a.cache.page) + 1;
   p.roles = a.heads_q + a.cache.heads;
-  p.pairs_wide = vec && a.rot % 16 == 0;
+  p.single = !t.seq_offsets && t.n_tokens == t.n_seq;
   const int64_t pages = p.per >= 0 ? (int64_t)p.per * t.n_seq : t.n_tokens / a.cache.page + 2 * (int64_t)t.n_seq;
   // Workgroups of a page: as many as fill the chip a few times over, with a role at least for each of their waves.
   p.groups = (int)std::max<int64_t>(1, std::min<int64_t>((p.roles + 3) / 4, 2048 / std::max<int64_t>(pages, 1)));
