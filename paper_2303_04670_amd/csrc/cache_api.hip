@@ -81,6 +81,7 @@ evconv_status plan(const evconv_attend_args* a, AttendParams* p, size_t* bytes) 
   *p = AttendParams{};
   p->a = *a;
   p->vec = a->cache.d % 8 == 0 && wide(a->dtype, a->q);
+  p->vec_o = a->cache.d % 4 == 0 && a->o_token_stride % 4 == 0 && a->o_head_stride % 4 == 0 && aligned(a->o, 4 * type_size(a->dtype));
   *bytes = a->tokens.n_tokens ? plan_attend(*p) : 0;
   return EVCONV_OK;
 }

@@ -51,6 +51,13 @@ __device__ __forceinline__ void seen_by(const AttendParams& p, int64_t past, int
   lo = p.a.window ? (int)min(max(position + 1 - p.a.window, (int64_t)0), (int64_t)hi) : 0;
 }
 
+// What a workgroup does with what it found of such a row in stretch `split`: 0 nothing, 1 the output, 2 a part of it.
+__device__ __forceinline__ int fate_of(int lo, int hi, int split, int chunk) {
+  if (hi <= lo) return split == 0;
+  const int s0 = lo / chunk, s1 = (hi - 1) / chunk;
+  return split < s0 || split > s1 ? 0 : s0 == s1 ? 1 : 2;
+}
+
 template <bool FP4, bool BF16, int DP, bool LIST>
 __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0) {
   constexpr int PARTS = BF16 ? 1 : 3, STEPS = DP / 32, VT = DP / 16, GROUPS = FP4 ? 4 : 1, TOK = 32 * GROUPS;
@@ -70,22 +77,24 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
   int seq, token, within, rows_left;  // of row 0 of this tile: its token; rows from there on
   int64_t row0;
   if constexpr (LIST) {
-    token = (int)(unit / p.row_tiles);
+    token = (int)(unit / p.rows.tiles);
     const Piece piece = find_piece(tk, token, tk.seq_offsets ? -1 : (int)(tk.n_tokens / tk.n_seq), 1, 1, 0);
     seq = piece.seq;
     within = token - piece.first;
     if (within < 0 || within >= piece.count) return;
-    row0 = unit % p.row_tiles * 16;
+    row0 = unit % p.rows.tiles * 16;
     rows_left = p.share - (int)row0;
   } else {
-    const Piece piece = find_piece(tk, unit, p.row_tiles, p.share, 16, 1);
-    seq = piece.seq;
-    row0 = (int64_t)piece.at * 16;
-    const int64_t left = (int64_t)piece.count * p.share - row0;
-    if (piece.at < 0 || left <= 0) return;
-    rows_left = (int)min(left, (int64_t)16);
-    token = piece.first;
-    within = 0;
+    seq = (int)unit;
+    int count = (int)(tk.n_tokens / tk.n_seq);
+    token = seq * count;
+    if (tk.seq_offsets) {
+      token = offset_of(tk, seq);
+      count = offset_of(tk, seq + 1) - token;
+    }
+    row0 = within = 0;
+    if (count <= 0 || (int64_t)count * p.share > kFewRows) return;
+    rows_left = count * p.share;
   }
   const int past = tk.past[seq];
   const int64_t r = row0 + n;
@@ -102,20 +111,15 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
     lo_min = min(lo_min, __shfl_xor(lo_min, s));
     lo_max = max(lo_max, __shfl_xor(lo_max, s));
   }
-  int64_t begin = (int64_t)split * p.chunk, end = begin + p.chunk;
+  int64_t begin = (int64_t)split * p.rows.chunk, end = begin + p.rows.chunk;
   int fate;
   if constexpr (LIST) {
     end = min(end, (int64_t)a.count << p.log);
-    fate = p.splits == 1 ? 1 : 2;
+    fate = p.rows.splits == 1 ? 1 : 2;
   } else {
     begin = max(begin, (int64_t)lo_min);
     end = min(end, (int64_t)hi_max);
-    if (hi <= lo) {
-      fate = split == 0;
-    } else {
-      const int s0 = lo / p.chunk, s1 = (hi - 1) / p.chunk;
-      fate = split < s0 || split > s1 ? 0 : s0 == s1 ? 1 : 2;
-    }
+    fate = fate_of(lo, hi, split, p.rows.chunk);
   }
   if (!live) fate = 0;
   if (!__any(fate)) return;  // (alike in all waves)
@@ -354,10 +358,10 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
 
 template <bool FP4, bool BF16, int DP>
 void start_rows(const AttendParams& p, hipStream_t s) {
-  const int64_t units = p.row_units * p.a.cache.heads;
-  const int64_t most = std::min<int64_t>(kMostThreads / 256 / p.splits, INT32_MAX);
+  const int64_t units = p.rows.units * p.a.cache.heads;
+  const int64_t most = std::min<int64_t>(kMostThreads / 256 / p.rows.splits, INT32_MAX);
   for (int64_t at = 0; at < units; at += most) {
-    const dim3 grid((unsigned)std::min(most, units - at), (unsigned)p.splits);
+    const dim3 grid((unsigned)std::min(most, units - at), (unsigned)p.rows.splits);
     if (p.a.selected) attend_rows<FP4, BF16, DP, true><<<grid, 256, 0, s>>>(p, at);
     else attend_rows<FP4, BF16, DP, false><<<grid, 256, 0, s>>>(p, at);
   }

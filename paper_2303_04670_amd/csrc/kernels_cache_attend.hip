@@ -1,5 +1,5 @@
 // Attention over a paged cache (evconv_cache_attend): how a call is cut into launches, and the join of what several workgroups
-// found of a row.  The kernels: cache_attend_rows.h.
+// found of a row.  The kernels: cache_attend_rows.h, cache_attend_pieces.h.
 #include <algorithm>
 
 #include "cache_attend_rows.h"
@@ -20,13 +20,14 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0)
   const Piece piece = find_piece(tk, token, tk.seq_offsets ? -1 : (int)(tk.n_tokens / tk.n_seq), 1, 1, 0);
   const int within = (int)(token - piece.first);
   if (within < 0 || within >= piece.count) return;
-  int s0 = 0, s1 = p.splits - 1;
+  int s0 = 0, s1 = p.rows.splits - 1;
   if (!a.selected) {
+    const int chunk = (int64_t)piece.count * p.share <= kFewRows ? p.rows.chunk : p.pieces.chunk;
     int lo, hi;
     seen_by(p, tk.past[piece.seq], within, lo, hi);
     if (hi <= lo) return;
-    s0 = lo / p.chunk;
-    s1 = (hi - 1) / p.chunk;
+    s0 = lo / chunk;
+    s1 = (hi - 1) / chunk;
     if (s0 == s1) return;
   }
   const int64_t rows = tk.n_tokens * a.heads_q;
@@ -68,41 +69,53 @@ size_t plan_attend(AttendParams& p) {
   p.most = (int64_t)t.width * a.cache.page;
   if (a.max_len) p.most = std::min(p.most, a.max_len);
   p.scale2 = a.scale * 1.44269504f;
-  int64_t extent;
+  const bool fp4 = a.cache.kind == EVCONV_CACHE_FP4;
+  const int64_t len = t.n_tokens / t.n_seq;
+  // Stretches of `extent` tokens for `units` workgroups a stretch: so many that there are `wanted` workgroups, but none shorter than `least`.
+  auto cut = [&](AttendWay& way, int64_t extent, int64_t all, int64_t least, int64_t wanted) {
+    const int64_t workgroups = std::max<int64_t>(way.units * a.cache.heads, 1);
+    int64_t chunk = std::max(least, (int64_t)((double)workgroups * extent / wanted));
+    chunk = std::max(chunk, (all + 65534) / 65535);  // (a grid's second size)
+    way.chunk = (int)std::min<int64_t>((chunk + 127) / 128 * 128, 1 << 30);
+    way.splits = (int)std::max<int64_t>((all + way.chunk - 1) / way.chunk, 1);
+  };
+  p.rows = p.pieces = AttendWay{0, -1, 128, 1};
   if (a.selected) {
-    p.row_tiles = (p.share + 15) / 16;
-    p.row_units = t.n_tokens * p.row_tiles;
-    extent = (int64_t)a.count * a.cache.page;
+    p.rows.tiles = (p.share + kFewRows - 1) / kFewRows;
+    p.rows.units = t.n_tokens * p.rows.tiles;
+    const int64_t extent = (int64_t)a.count * a.cache.page;
+    cut(p.rows, extent, extent, fp4 ? 1024 : 512, 4096);
   } else {
-    const int64_t len = t.n_tokens / t.n_seq;
-    p.row_tiles = t.seq_offsets ? -1 : (int)((len * p.share + 15) / 16);
-    p.row_units = t.seq_offsets ? t.n_tokens * p.share / 16 + t.n_seq : (int64_t)t.n_seq * p.row_tiles;
-    extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
+    const int64_t extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
+    if (t.seq_offsets || len * p.share <= kFewRows) {
+      p.rows.units = t.n_seq;
+      cut(p.rows, extent, p.most, fp4 ? 1024 : 512, 4096);
+    }
+    const int rows = a.dtype == EVCONV_BF16 ? 128 : 64;
+    if (t.seq_offsets) {
+      if (t.n_tokens * p.share > kFewRows) p.pieces.units = t.n_tokens * p.share / rows + t.n_seq;
+    } else if (len * p.share > kFewRows) {
+      p.pieces.tiles = (int)((len * p.share + rows - 1) / rows);
+      p.pieces.units = (int64_t)t.n_seq * p.pieces.tiles;
+    }
+    if (p.pieces.units) cut(p.pieces, extent, p.most, 512, 1024);
   }
-  extent = std::max<int64_t>(extent, 1);
-  // Tokens to a workgroup: so many that there are workgroups for the chip a few times over, at least as many as make its start worth while.
-  const int64_t units = std::max<int64_t>(p.row_units * a.cache.heads, 1);
-  const int64_t least = a.cache.kind == EVCONV_CACHE_FP4 ? 1024 : 512;
-  const int64_t chunk = std::max(least, (int64_t)((units * (double)extent) / 4096));
-  p.chunk = (int)std::min<int64_t>((chunk + 127) / 128 * 128, 1 << 30);
-  p.splits = (int)std::min<int64_t>((p.most + p.chunk - 1) / p.chunk, 65535);
-  if (a.selected) p.splits = (int)std::min<int64_t>((extent + p.chunk - 1) / p.chunk, 65535);
-  if (p.splits < 1) p.splits = 1;
-  if ((int64_t)p.splits * p.chunk < (a.selected ? extent : p.most)) p.chunk = (int)(((a.selected ? extent : p.most) / p.splits + 128) / 128 * 128);
-  if (p.splits == 1) return 0;
-  const size_t rows = (size_t)t.n_tokens * a.heads_q * p.splits;
+  const int splits = std::max(p.rows.splits, p.pieces.splits);
+  if (splits == 1) return 0;
+  const size_t rows = (size_t)t.n_tokens * a.heads_q * splits;
   return up(rows * 2 * sizeof(float)) + rows * p.dp * sizeof(float);
 }
 
 void place_attend(AttendParams& p, char* workspace) {
   p.stat = (float*)workspace;
-  p.part = (float*)(workspace + up((size_t)p.a.tokens.n_tokens * p.a.heads_q * p.splits * 2 * sizeof(float)));
+  p.part = (float*)(workspace + up((size_t)p.a.tokens.n_tokens * p.a.heads_q * std::max(p.rows.splits, p.pieces.splits) * 2 * sizeof(float)));
 }
 
 void launch_attend(const AttendParams& p, hipStream_t s) {
-  if (p.a.cache.kind == EVCONV_CACHE_FP4) launch_attend_rows_fp4(p, s);
-  else launch_attend_rows_bf16(p, s);
-  if (p.splits == 1) return;
+  const bool fp4 = p.a.cache.kind == EVCONV_CACHE_FP4;
+  if (p.rows.units) fp4 ? launch_attend_rows_fp4(p, s) : launch_attend_rows_bf16(p, s);
+  if (p.pieces.units) fp4 ? launch_attend_pieces_fp4(p, s) : launch_attend_pieces_bf16(p, s);
+  if (p.rows.splits == 1 && p.pieces.splits == 1) return;
   const int64_t rows = p.a.tokens.n_tokens * p.a.heads_q, most = kMostThreads / 256;
   for (int64_t at = 0; at < rows; at += most) {
     const unsigned grid = (unsigned)std::min(most, rows - at);

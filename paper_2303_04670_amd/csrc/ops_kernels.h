@@ -69,26 +69,34 @@ constexpr int cache_channels(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 
 void launch_cache_append(const evconv_append_args& a, bool vec, hipStream_t s);
 void launch_cache_read(const evconv_read_args& a, hipStream_t s);
 
+// How the rows of a call (tokens x query heads that share a key head) are dealt out over workgroups.
+struct AttendWay {
+  int64_t units;  // tiles of rows; 0: none goes this way
+  int tiles;      // of a sequence of equal lengths (of a token with chosen pages), or -1
+  int chunk;      // tokens that a workgroup looks at (with chosen pages: of their list)
+  int splits;     // workgroups that share a row's tokens
+};
+constexpr int kFewRows = 16;  // sequences of up to so many rows go the first way
+
 struct AttendParams {
   evconv_attend_args a;
-  int dp, log;         // padded channels, log2 of the page
-  int share;           // query heads to a key head
-  bool vec;            // rows of q may be read in 16-byte loads
-  int64_t most;        // tokens of a sequence that are looked at, at most
-  float scale2;        // scale * log2(e)
-  // few rows: 16 of them to a workgroup
-  int row_tiles;       // of a sequence of equal lengths (of a token with chosen pages), or -1
-  int64_t row_units;   // row tiles of all sequences, as find_piece numbers them
-  int chunk, splits;   // tokens that one workgroup looks at (with chosen pages: of their list), pieces
+  int dp, log;      // padded channels, log2 of the page
+  int share;        // query heads to a key head
+  bool vec, vec_o;  // rows of q may be read in 16-byte loads, rows of o written four values at a time
+  int64_t most;     // tokens of a sequence that are looked at, at most
+  float scale2;     // scale * log2(e)
+  AttendWay rows, pieces;
   // workspace
-  float* part;         // [splits][n_tokens * heads_q][dp] sums
-  float* stat;         // [splits][n_tokens * heads_q][2] largest exponent, sum of weights
+  float* part;      // [splits][n_tokens * heads_q][dp] sums
+  float* stat;      // [splits][n_tokens * heads_q][2] largest exponent, sum of weights
 };
-size_t plan_attend(AttendParams& p);                     // bytes of workspace
+size_t plan_attend(AttendParams& p);  // bytes of workspace
 void place_attend(AttendParams& p, char* workspace);
 void launch_attend(const AttendParams& p, hipStream_t s);
 void launch_attend_rows_bf16(const AttendParams& p, hipStream_t s);
 void launch_attend_rows_fp4(const AttendParams& p, hipStream_t s);
+void launch_attend_pieces_bf16(const AttendParams& p, hipStream_t s);
+void launch_attend_pieces_fp4(const AttendParams& p, hipStream_t s);
 
 struct SelectParams {
   evconv_select_args a;
