@@ -58,14 +58,15 @@ __device__ __forceinline__ int fate_of(int lo, int hi, int split, int chunk) {
   return split < s0 || split > s1 ? 0 : s0 == s1 ? 1 : 2;
 }
 
-template <bool FP4, bool BF16, int DP, bool LIST>
-__global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0) {
-  constexpr int PARTS = BF16 ? 1 : 3, STEPS = DP / 32, VT = DP / 16, GROUPS = FP4 ? 4 : 1, TOK = 32 * GROUPS;
+template <bool FP4, int GROUPS, bool BF16, int DP, bool LIST>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF16)) void attend_rows(AttendParams p, int64_t unit0) {
+  constexpr int PARTS = BF16 ? 1 : 3, STEPS = DP / 32, VT = DP / 16;
+  constexpr int MINE = 8 * GROUPS, TOK = 4 * MINE;  // tokens of a lane's weights, of a tile (which lies in one page)
   constexpr int KW = FP4 ? STEPS : 4 * STEPS;  // 32-bit words of a lane's part of a key
   __shared__ float s_o[4][16][DP + 4];
   __shared__ float s_stat[4][16][2];
   __shared__ int s_row[16][3];  // token, query head, what becomes of it: 0 nothing, 1 output, 2 part
-  __shared__ float s_scale[FP4 ? 4 : 1][2][FP4 ? 128 : 1];
+  __shared__ __align__(16) float s_scale[FP4 ? 4 : 1][2][FP4 ? TOK : 4];
   const evconv_attend_args& a = p.a;
   const evconv_cache& c = a.cache;
   const evconv_tokens& tk = a.tokens;
@@ -128,79 +129,78 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
     s_row[n][1] = q_head;
     s_row[n][2] = fate;
   }
-  begin &= ~(int64_t)(TOK - 1);
-  // ---- where tokens lie
+  begin &= ~(int64_t)(TOK - 1);  // (stretches are whole tiles)
+  // ---- where tokens lie: table entries (with chosen pages: from the list) two tiles ahead, pages one, so that no request waits for them
   const int* const list = LIST ? a.selected + ((int64_t)token * c.heads + head) * a.count : nullptr;
-  auto look = [&](int64_t base, int& page, int& real) __attribute__((always_inline)) {  // of 32 tokens from `base` on
-    const int64_t entry = base >> p.log;
-    const int slot = (int)(base & (c.page - 1));
-    if constexpr (LIST) {
-      const int e = entry < a.count ? list[entry] : -1;
-      page = e < 0 ? -1 : page_of(c, tk, seq, e);
-      real = page < 0 ? kNowhere : (e << p.log) + slot;
-    } else {
-      page = page_of(c, tk, seq, entry);
-      real = page < 0 ? kNowhere : (int)base;
-    }
-    page = max(page, 0);  // (of a page that is not there the first one's are read, and not seen)
+  const int* const table = tk.table + seq * tk.table_stride;
+  auto entry_at = [&](int64_t base) __attribute__((always_inline)) -> int {
+    const int64_t i = base >> p.log;
+    if constexpr (LIST) return i < a.count ? __builtin_amdgcn_readfirstlane(list[i]) : -1;
+    return (int)i;
   };
-  const int gk = FP4 ? n >> 2 : 0, gv = FP4 ? g : 0;
-  int page_k, page_v, real_k, real_v, slot_k, slot_v;
-  auto find_tile = [&](int64_t base) __attribute__((always_inline)) {
-    look(base + 32 * gv, page_v, real_v);
-    slot_v = (int)((base + 32 * gv) & (c.page - 1));
-    if constexpr (FP4) {
-      look(base + 32 * gk, page_k, real_k);
-      slot_k = (int)((base + 32 * gk) & (c.page - 1));
-    } else {
-      page_k = page_v, slot_k = slot_v;
-    }
+  auto page_at = [&](int entry) __attribute__((always_inline)) -> int { return entry >= 0 && entry < tk.width ? table[entry] : -1; };
+  int64_t at_page = 0;                               // heads before this one's of the tile's page
+  int slot = 0, real = kNowhere;                     // the tile's place in it, its first token's position
+  int next_entry = -1, next_page = -1, entry = -1;   // of the next tile, of the one after it
+  auto use_next = [&](int64_t base) __attribute__((always_inline)) {  // the next tile's place, and requests for those behind it
+    const int page = __builtin_amdgcn_readfirstlane(next_page);
+    const bool there = page >= 0 && page < c.n_pages;
+    at_page = (int64_t)(there ? page : 0) * c.heads + head;  // (of a page that is not there the first one's tokens are read, and not seen)
+    slot = (int)(base & (c.page - 1));
+    real = there ? (next_entry << p.log) + slot : kNowhere;
+    next_entry = entry;
+    next_page = page_at(entry);
+    entry = entry_at(base + 8 * TOK);
   };
   unsigned kw[2 * GROUPS][KW];
-  uint4 vw[VT];
-  float2 ks, vs;
+  unsigned vw[VT][FP4 ? GROUPS : 4];
+  float ks, vs;  // scales of the token of the tile whose number is the lane's (of 32 tokens: lanes 32 and up have none)
+  // (addresses: what is alike in the wave, what the lane adds to it, constants)
+  const unsigned lane_k = FP4 ? (MINE * (n >> 2) + (n & 3)) * (DP / 2) + g * (DP / 8) : ((MINE * (n >> 2) + (n & 3)) * DP + 8 * g) * 2;
+  const unsigned lane_v = FP4 ? (unsigned)(n * c.page + MINE * g) / 2 : (unsigned)(n * c.page + MINE * g) * 2;
+  auto load_scales = [&](const float* scales, float& to) __attribute__((always_inline)) {
+    to = scales[at_page * c.page + slot + (lane & (TOK - 1))];
+  };
   auto load_k = [&]() __attribute__((always_inline)) {
-    const int64_t at = ((int64_t)page_k * c.heads + head) * c.page + slot_k;
+    const char* const tile = (const char*)c.k + (at_page * c.page + slot) * (FP4 ? DP / 2 : DP * 2);
 #pragma unroll
     for (int i = 0; i < 2 * GROUPS; ++i) {
-      const int t = (FP4 ? 8 * (i / 2) : 8 * (n >> 2)) + 4 * (i % 2) + (n & 3);
-      if constexpr (FP4) {
-        const char* const q = (const char*)c.k + (at + t) * (DP / 2) + g * (DP / 8);
-        if constexpr (STEPS % 4 == 0) {
+      const char* const from = tile + (8 * (i / 2) + 4 * (i % 2)) * (FP4 ? DP / 2 : DP * 2) + lane_k;
+      if constexpr (!FP4) {
 #pragma unroll
-          for (int w = 0; w < STEPS; w += 4) *(uint4*)&kw[i][w] = *(const uint4*)(q + 4 * w);
-        } else if constexpr (STEPS % 2 == 0) {
+        for (int st = 0; st < STEPS; ++st) *(uint4*)&kw[i][4 * st] = *(const uint4*)(from + 64 * st);
+      } else if constexpr (STEPS % 4 == 0) {
 #pragma unroll
-          for (int w = 0; w < STEPS; w += 2) *(uint2*)&kw[i][w] = *(const uint2*)(q + 4 * w);
-        } else {
+        for (int w = 0; w < STEPS; w += 4) *(uint4*)&kw[i][w] = *(const uint4*)(from + 4 * w);
+      } else if constexpr (STEPS % 2 == 0) {
 #pragma unroll
-          for (int w = 0; w < STEPS; ++w) kw[i][w] = *(const unsigned*)(q + 4 * w);
-        }
+        for (int w = 0; w < STEPS; w += 2) *(uint2*)&kw[i][w] = *(const uint2*)(from + 4 * w);
       } else {
-        const uint16_t* const q = (const uint16_t*)c.k + (at + t) * DP + 8 * g;
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) *(uint4*)&kw[i][4 * st] = *(const uint4*)(q + 32 * st);
+        for (int w = 0; w < STEPS; ++w) kw[i][w] = *(const unsigned*)(from + 4 * w);
       }
     }
-    if constexpr (FP4) {
-      const int64_t at_v = ((int64_t)page_v * c.heads + head) * c.page + slot_v + 2 * n;
-      ks = *(const float2*)(c.k_scale + at_v);
-    }
+    if constexpr (FP4) load_scales(c.k_scale, ks);
   };
   auto load_v = [&]() __attribute__((always_inline)) {
-    const int64_t at = ((int64_t)page_v * c.heads + head) * DP;
+    const char* const tile = (const char*)c.v + (FP4 ? (at_page * DP * c.page + slot) / 2 : (at_page * DP * c.page + slot) * 2);
 #pragma unroll
     for (int i = 0; i < VT; ++i) {
-      if constexpr (FP4) vw[i] = *(const uint4*)((const char*)c.v + ((at + 16 * i + n) * c.page + slot_v) / 2);
-      else vw[i] = *(const uint4*)((const uint16_t*)c.v + (at + 16 * i + n) * c.page + slot_v + 8 * g);
+      const char* const from = tile + (FP4 ? (int64_t)i * 8 * c.page : (int64_t)i * 32 * c.page) + lane_v;
+      if constexpr (!FP4) *(uint4*)vw[i] = *(const uint4*)from;
+      else if constexpr (GROUPS == 2) *(uint2*)vw[i] = *(const uint2*)from;
+      else vw[i][0] = *(const unsigned*)from;
     }
-    if constexpr (FP4) vs = *(const float2*)(c.v_scale + ((int64_t)page_v * c.heads + head) * c.page + slot_v + 2 * n);
+    if constexpr (FP4) load_scales(c.v_scale, vs);
   };
   int64_t base = begin + wave * TOK;
   int seen_real = kNowhere;
   if (base < end) {
-    find_tile(base);
-    seen_real = real_v;
+    next_entry = entry_at(base);
+    next_page = page_at(next_entry);
+    entry = entry_at(base + 4 * TOK);
+    use_next(base);
+    seen_real = real;
     load_k();
     load_v();
   }
@@ -225,8 +225,8 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
     float x[GROUPS][8];
     if constexpr (FP4) {
       lds_turn();
-      *(float2*)&s_scale[wave][0][2 * lane] = ks;
-      *(float2*)&s_scale[wave][1][2 * lane] = vs;
+      s_scale[wave][0][lane & (TOK - 1)] = ks;
+      s_scale[wave][1][lane & (TOK - 1)] = vs;
       lds_turn();
     }
 #pragma unroll
@@ -240,21 +240,19 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[st][part], acc, 0, 0, 0);
       }
-      if constexpr (FP4) acc *= *(const f32x4*)&s_scale[wave][0][32 * g + 8 * (i / 2) + 4 * (i % 2)];
+      if constexpr (FP4) acc *= *(const f32x4*)&s_scale[wave][0][MINE * g + 8 * (i / 2) + 4 * (i % 2)];
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[i / 2][4 * (i % 2) + j] = acc[j];
     }
-    const int real = real_v;
     int next_real = kNowhere;
     if (next < end) {
-      find_tile(next);
-      next_real = real_v;
+      use_next(next);
+      next_real = real;
       load_k();
     }
-    (void)real;
     // ---- what is not seen
-    const int first = FP4 ? seen_real : seen_real + 8 * g;  // of this lane's weights
-    const bool whole = __all(seen_real >= lo_max && seen_real + 32 <= hi_min);
+    const int first = seen_real + MINE * g;  // of the lane's weights
+    const bool whole = seen_real >= lo_max && seen_real + TOK <= hi_min;
     if (!whole)
 #pragma unroll
       for (int s = 0; s < GROUPS; ++s)
@@ -291,7 +289,7 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
         l += w[j];
       }
       if constexpr (FP4) {
-        const f32x4 v0 = *(const f32x4*)&s_scale[wave][1][32 * g + 8 * s], v1 = *(const f32x4*)&s_scale[wave][1][32 * g + 8 * s + 4];
+        const f32x4 v0 = *(const f32x4*)&s_scale[wave][1][MINE * g + 8 * s], v1 = *(const f32x4*)&s_scale[wave][1][MINE * g + 8 * s + 4];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float scale = j < 4 ? v0[j & 3] : v1[j & 3];
@@ -305,10 +303,9 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
       for (int i = 0; i < VT; ++i) {
         b16x8 v;
         if constexpr (FP4) {
-          const unsigned words[4] = {vw[i].x, vw[i].y, vw[i].z, vw[i].w};
-          v = codes_to_bf16(words[s]);
+          v = codes_to_bf16(vw[i][s]);
         } else {
-          v = __builtin_bit_cast(b16x8, vw[i]);
+          v = __builtin_bit_cast(b16x8, *(uint4*)vw[i]);
           if (!whole) v = keep_range(v, lo_min - first, hi_max - first);
         }
 #pragma unroll
@@ -356,15 +353,22 @@ __global__ __launch_bounds__(256) void attend_rows(AttendParams p, int64_t unit0
   }
 }
 
-template <bool FP4, bool BF16, int DP>
-void start_rows(const AttendParams& p, hipStream_t s) {
+template <bool FP4, int GROUPS, bool BF16, int DP>
+void start_tiles(const AttendParams& p, hipStream_t s) {
   const int64_t units = p.rows.units * p.a.cache.heads;
   const int64_t most = std::min<int64_t>(kMostThreads / 256 / p.rows.splits, INT32_MAX);
   for (int64_t at = 0; at < units; at += most) {
     const dim3 grid((unsigned)std::min(most, units - at), (unsigned)p.rows.splits);
-    if (p.a.selected) attend_rows<FP4, BF16, DP, true><<<grid, 256, 0, s>>>(p, at);
-    else attend_rows<FP4, BF16, DP, false><<<grid, 256, 0, s>>>(p, at);
+    if (p.a.selected) attend_rows<FP4, GROUPS, BF16, DP, true><<<grid, 256, 0, s>>>(p, at);
+    else attend_rows<FP4, GROUPS, BF16, DP, false><<<grid, 256, 0, s>>>(p, at);
   }
+}
+// Tiles of 64 tokens in 4 bits, which have the bytes of 16 in bf16, where a page holds them.
+template <bool FP4, bool BF16, int DP>
+void start_rows(const AttendParams& p, hipStream_t s) {
+  if constexpr (FP4)
+    if (p.a.cache.page >= 64) return start_tiles<true, 2, BF16, DP>(p, s);
+  start_tiles<FP4, 1, BF16, DP>(p, s);
 }
 
 template <bool FP4, bool BF16>

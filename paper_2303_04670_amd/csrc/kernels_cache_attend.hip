@@ -7,11 +7,11 @@
 namespace evk {
 namespace {
 
-// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row, its waves to every fourth
-// stretch.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
+// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
 template <bool BF16>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0) {
-  __shared__ float s_sum[4][256], s_total[4];
+  __shared__ __align__(16) float s_sum[1024];
+  __shared__ float s_total[256];
   const evconv_attend_args& a = p.a;
   const evconv_tokens& tk = a.tokens;
   const int64_t row = row0 + blockIdx.x;
@@ -31,29 +31,35 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0)
     if (s0 == s1) return;
   }
   const int64_t rows = tk.n_tokens * a.heads_q;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63;
   float big = -INFINITY;
   for (int s = s0 + lane; s <= s1; s += 64) big = fmaxf(big, p.stat[2 * (s * rows + row)]);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d));
-  float sum[4] = {0, 0, 0, 0}, total = 0.0f;
-  for (int s = s0 + wave; s <= s1; s += 4) {
-    const int64_t at = s * rows + row;
-    const float m = p.stat[2 * at], factor = m == big ? 1.0f : __builtin_amdgcn_exp2f(m - big);
-    total += factor * p.stat[2 * at + 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (64 * i + lane < p.dp) sum[i] += factor * p.part[at * p.dp + 64 * i + lane];
+  // four channels to a thread, the rest of the threads to other stretches
+  const int quads = p.dp / 4, beside = 256 / quads, mine = threadIdx.x / quads, ch = threadIdx.x % quads * 4;
+  f32x4 sum = {0, 0, 0, 0};
+  float total = 0.0f;
+  if (mine < beside) {
+#pragma unroll 4
+    for (int s = s0 + mine; s <= s1; s += beside) {
+      const int64_t at = s * rows + row;
+      const float m = p.stat[2 * at], factor = m == big ? 1.0f : __builtin_amdgcn_exp2f(m - big);
+      total += factor * p.stat[2 * at + 1];
+      sum += factor * *(const f32x4*)(p.part + at * p.dp + ch);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s_sum[wave][64 * i + lane] = sum[i];
-  if (lane == 0) s_total[wave] = total;
+  *(f32x4*)&s_sum[4 * threadIdx.x] = sum;
+  s_total[threadIdx.x] = total;
   __syncthreads();
-  const int ch = threadIdx.x;
-  if (ch >= a.cache.d) return;
-  const float all = (s_total[0] + s_total[1]) + (s_total[2] + s_total[3]);
-  const float o = (s_sum[0][ch] + s_sum[1][ch]) + (s_sum[2][ch] + s_sum[3][ch]);
-  store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + ch, all == 0.0f ? 0.0f : o / all);
+  const int c = threadIdx.x;
+  if (c >= a.cache.d) return;
+  float o = 0.0f, all = 0.0f;
+  for (int i = 0; i < beside; ++i) {
+    o += s_sum[i * p.dp + c];
+    all += s_total[i * quads];
+  }
+  store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + c, all == 0.0f ? 0.0f : o / all);
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -84,12 +90,12 @@ size_t plan_attend(AttendParams& p) {
     p.rows.tiles = (p.share + kFewRows - 1) / kFewRows;
     p.rows.units = t.n_tokens * p.rows.tiles;
     const int64_t extent = (int64_t)a.count * a.cache.page;
-    cut(p.rows, extent, extent, fp4 ? 1024 : 512, 4096);
+    cut(p.rows, extent, extent, fp4 ? 1024 : 512, 2048);
   } else {
     const int64_t extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
     if (t.seq_offsets || len * p.share <= kFewRows) {
       p.rows.units = t.n_seq;
-      cut(p.rows, extent, p.most, fp4 ? 1024 : 512, 4096);
+      cut(p.rows, extent, p.most, fp4 ? 1024 : 512, 2048);
     }
     const int rows = a.dtype == EVCONV_BF16 ? 128 : 64;
     if (t.seq_offsets) {
