@@ -27,6 +27,11 @@ struct PieceTile {
   }
 };
 
+template <bool V>
+struct Whole {
+  static constexpr bool value = V;
+};
+
 template <bool FP4, bool BF16, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendParams p, int64_t block0) {
   using Tile = PieceTile<DP>;
@@ -53,7 +58,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
     piece = find_piece(tk, number, -1, p.share, ROWS, 1);
   }
   const int64_t total = (int64_t)piece.count * p.share, row0 = (int64_t)piece.at * ROWS;
-  if (piece.at < 0 || row0 >= total || total <= kFewRows) return;
+  if (piece.at < 0 || row0 >= total || total <= p.few) return;
   const int past = tk.past[piece.seq];
   const int last = (int)min(row0 + ROWS, total) - 1;
   int lo_min, hi_max, other;
@@ -92,61 +97,71 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
       split8<PARTS>(x, q[ct][st]);
     }
   }
-  // ---- a tile into LDS
-  int real[HALVES], page[HALVES];
+  // ---- a tile into LDS.  Addresses: where the halves' tokens begin is alike for all lanes, what a lane adds to it the same for every tile
+  // (the permutation is its own inverse: what a lane writes to its place is what it finds by it).
+  int real[HALVES];
+  const char *k_at[HALVES], *v_at[HALVES];
+  int64_t scale_at[HALVES];
   uint4 k_new, v_new;
   float scale_new;
+  constexpr int kLoads = Tile::kBytes / 4096;  // of keys and of values, by each wave
+  unsigned k_lane[kLoads], v_lane;             // bytes; keys: from their half's first on; values: of the first load
+  const int v_part = Tile::value_at((wave * 64 + lane) / (TT / 8), lane % (TT / 8)) - (wave * 64 + lane) / (TT / 8) * (TT / 8);
+  if constexpr (!FP4) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int place = (4 * i + wave) * 64 + lane, t = place / Tile::kPlaces;
+      k_lane[i] = 2 * (t % 32 * DP + 8 * (Tile::key_at(t, place % Tile::kPlaces) - t * Tile::kPlaces));
+    }
+    v_lane = 2 * ((wave * 64 + lane) / (TT / 8) * c.page + 8 * (v_part % 4));
+  } else {
+    const int i = threadIdx.x;
+    k_lane[0] = i / (DP / 32) % 32 * (DP / 2) + 16 * (i % (DP / 32));
+    v_lane = i / HALVES * c.page / 2;
+  }
+  int ahead[HALVES];  // table entries of the next tile: looked up a tile before they are wanted
+  const int* const table = tk.table + piece.seq * tk.table_stride;
+  auto look_ahead = [&](int64_t base) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) ahead[h] = table[min((base + 32 * h) >> p.log, (int64_t)tk.width - 1)];
+  };
   auto find_tile = [&](int64_t base) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       const int64_t at = base + 32 * h;
-      const int found = __builtin_amdgcn_readfirstlane(page_of(c, tk, piece.seq, at >> p.log));
-      page[h] = max(found, 0);
+      const int entry = __builtin_amdgcn_readfirstlane(ahead[h]), found = (at >> p.log) < tk.width && entry < c.n_pages ? entry : -1;
+      const int slot = (int)(at & (c.page - 1));
       real[h] = found < 0 ? kNowhere : (int)at;
+      const int64_t heads = (int64_t)max(found, 0) * c.heads + head;  // (of a page that is not there the first one's tokens are read, and not seen)
+      scale_at[h] = heads * c.page + slot;
+      k_at[h] = (const char*)c.k + scale_at[h] * (FP4 ? DP / 2 : DP * 2);
+      v_at[h] = (const char*)c.v + (FP4 ? (heads * DP * c.page + slot) / 2 : (heads * DP * c.page + slot) * 2);
     }
   };
-  auto request = [&](int64_t base, int buffer) __attribute__((always_inline)) {
-    const int in_page = (int)(base & (c.page - 1));  // (of the first half; the second one's page begins with it, or goes on)
-    const int in_page1 = (int)((base + 32) & (c.page - 1));
+  const int wave_of = __builtin_amdgcn_readfirstlane(wave);
+  auto request = [&](int buffer) __attribute__((always_inline)) {
     if constexpr (!FP4) {
+      auto copy = [&](const char* from, char* to) __attribute__((always_inline)) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+      };
 #pragma unroll
-      for (int i = 0; i < Tile::kBytes / 4096; ++i) {
-        const int place = (4 * i + wave) * 64 + lane, t = place / Tile::kPlaces, h = t / 32;
-        const int piece_of = Tile::key_at(t, place % Tile::kPlaces) - t * Tile::kPlaces;  // (the permutation is its own inverse)
-        const int64_t pg = HALVES == 1 || h == 0 ? page[0] : page[HALVES - 1];
-        const int slot = (HALVES == 1 || h == 0 ? in_page : in_page1) + t % 32;
-        const uint16_t* const from = (const uint16_t*)c.k + ((pg * c.heads + head) * c.page + slot) * DP + 8 * piece_of;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                         (__attribute__((address_space(3))) void*)(s_k + buffer * Tile::kBytes + (4 * i + wave) * 1024), 16, 0, 0);
+      for (int i = 0; i < kLoads; ++i) {
+        char* const to = s_k + buffer * Tile::kBytes + (4 * i + wave_of) * 1024;
+        // (a load's keys are of one half, but for rows of 12 pieces)
+        const int first = (4 * i + wave) * 64, t0 = first / Tile::kPlaces, t1 = (first + 63) / Tile::kPlaces;
+        if (HALVES == 1 || t1 < 32) copy(k_at[0] + k_lane[i], to);
+        else if (t0 >= 32) copy(k_at[HALVES - 1] + k_lane[i], to);
+        else copy((first + lane < 32 * Tile::kPlaces ? k_at[0] : k_at[HALVES - 1]) + k_lane[i], to);
       }
+      const int64_t step = (int64_t)(256 / (TT / 8)) * 2 * c.page;  // (channels of a load by all waves: whole periods of the permutation)
+      const char* const lane_at = (HALVES == 1 || v_part < 4 ? v_at[0] : v_at[HALVES - 1]) + v_lane;
 #pragma unroll
-      for (int i = 0; i < Tile::kBytes / 4096; ++i) {
-        const int place = (4 * i + wave) * 64 + lane, channel = place / (TT / 8);
-        const int piece_of = Tile::value_at(channel, place % (TT / 8)) - channel * (TT / 8), h = piece_of / 4;
-        const int64_t pg = HALVES == 1 || h == 0 ? page[0] : page[HALVES - 1];
-        const int slot = (HALVES == 1 || h == 0 ? in_page : in_page1) + 8 * (piece_of % 4);
-        const uint16_t* const from = (const uint16_t*)c.v + ((pg * c.heads + head) * DP + channel) * c.page + slot;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                         (__attribute__((address_space(3))) void*)(s_v + buffer * Tile::kBytes + (4 * i + wave) * 1024), 16, 0, 0);
-      }
+      for (int i = 0; i < kLoads; ++i) copy(lane_at + i * step, s_v + buffer * Tile::kBytes + (4 * i + wave_of) * 1024);
     } else {
-      const int i = threadIdx.x;
-      if (i < TT * DP / 32) {
-        const int t = i / (DP / 32), part = i % (DP / 32), h = t / 32;
-        const int64_t pg = HALVES == 1 || h == 0 ? page[0] : page[HALVES - 1];
-        const int slot = (HALVES == 1 || h == 0 ? in_page : in_page1) + t % 32;
-        k_new = *(const uint4*)((const char*)c.k + ((pg * c.heads + head) * c.page + slot) * (DP / 2) + 16 * part);
-      }
-      if (i < DP * HALVES) {
-        const int channel = i / HALVES, h = i % HALVES;
-        const int64_t pg = HALVES == 1 || h == 0 ? page[0] : page[HALVES - 1];
-        v_new = *(const uint4*)((const char*)c.v + (((pg * c.heads + head) * DP + channel) * c.page + (HALVES == 1 || h == 0 ? in_page : in_page1)) / 2);
-      }
-      if (i < 2 * TT) {
-        const int t = i % TT, h = t / 32;
-        const int64_t pg = HALVES == 1 || h == 0 ? page[0] : page[HALVES - 1];
-        scale_new = (i < TT ? c.k_scale : c.v_scale)[(pg * c.heads + head) * c.page + (HALVES == 1 || h == 0 ? in_page : in_page1) + t % 32];
-      }
+      const int i = threadIdx.x, t = i % TT;
+      if (i < TT * DP / 32) k_new = *(const uint4*)((HALVES == 1 || i < 32 * (DP / 32) ? k_at[0] : k_at[HALVES - 1]) + k_lane[0]);
+      if (i < DP * HALVES) v_new = *(const uint4*)((i % HALVES == 0 ? v_at[0] : v_at[HALVES - 1]) + v_lane);
+      if (i < 2 * TT) scale_new = (i < TT ? c.k_scale : c.v_scale)[(HALVES == 1 || t < 32 ? scale_at[0] : scale_at[HALVES - 1]) + t % 32];
     }
   };
   auto deliver = [&](int buffer) __attribute__((always_inline)) {  // codes into LDS as bf16
@@ -180,9 +195,129 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
 #pragma unroll
     for (int i = 0; i < VT; ++i) o[ct][i] = f32x4{0, 0, 0, 0};
   }
+  // A tile that is in LDS: operands are read a step before the products that want them, values' while the weights are made.
+  auto work = [&](const int (&at)[HALVES], int buffer, auto is_whole) __attribute__((always_inline)) {
+    constexpr bool whole = decltype(is_whole)::value;
+    const char* const keys = s_k + buffer * Tile::kBytes;
+    const char* const values = s_v + buffer * Tile::kBytes;
+    const float* const scales = s_scale + buffer * 2 * TT;
+    auto read_keys = [&](int i, b16x8 (&k)[STEPS]) __attribute__((always_inline)) {
+      const int t = 32 * (i / 2) + 8 * (n >> 2) + 4 * (i % 2) + (n & 3);
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) k[st] = *(const b16x8*)(keys + 16 * Tile::key_at(t, 4 * st + g));
+    };
+    auto read_value = [&](int h, int i) __attribute__((always_inline)) { return *(const b16x8*)(values + 16 * Tile::value_at(16 * i + n, 4 * h + g)); };
+    __builtin_amdgcn_s_setprio(1);  // (matrix instructions first: the other wave of the SIMD has vector ones meanwhile)
+    // ---- scores
+    float x[CT][HALVES][8];
+    b16x8 k[2][STEPS];
+    read_keys(0, k[0]);
+#pragma unroll
+    for (int i = 0; i < 2 * HALVES; ++i) {
+      if (i + 1 < 2 * HALVES) read_keys(i + 1, k[(i + 1) & 1]);
+      f32x4 acc[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i & 1][st], q[ct][st][part], acc[ct], 0, 0, 0);
+      if constexpr (FP4) {
+        const f32x4 scale = *(const f32x4*)(scales + 32 * (i / 2) + 8 * g + 4 * (i % 2));
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) acc[ct] *= scale;
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[ct][i / 2][4 * (i % 2) + j] = acc[ct][j];
+    }
+    b16x8 v[VT];
+#pragma unroll
+    for (int i = 0; i < VT; ++i) v[i] = read_value(0, i);
+    __builtin_amdgcn_sched_barrier(0);  // (requested here, not where they are wanted)
+    __builtin_amdgcn_s_setprio(0);
+    // ---- what is not seen
+    if constexpr (!whole)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = at[h] + 8 * g + j;
+            if (t < lo[ct] || t >= hi[ct]) x[ct][h][j] = -INFINITY;
+          }
+    // ---- the running maxima
+    float top[CT];
+    bool raise = false;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      top[ct] = x[ct][0][0];
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top[ct] = fmaxf(top[ct], x[ct][h][j]);
+      top[ct] *= p.scale2;
+      raise = raise || top[ct] > m[ct] + kRaise;
+    }
+    if (__any(raise))
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 16));
+        top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 32));
+        const float raised = fmaxf(m[ct], top[ct]);
+        const float factor = m[ct] == raised ? 1.0f : __builtin_amdgcn_exp2f(m[ct] - raised);
+        m[ct] = raised;
+        l[ct] *= factor;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) o[ct][i] *= factor;
+      }
+    // ---- weights, sums
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      b16x8 weights[CT][PARTS];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const float off = m[ct] == -INFINITY ? 0.0f : m[ct];
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          w[j] = __builtin_amdgcn_exp2f(fmaf(x[ct][h][j], p.scale2, -off));
+          l[ct] += w[j];
+        }
+        if constexpr (FP4) {
+          const f32x4 s0 = *(const f32x4*)(scales + TT + 32 * h + 8 * g), s1 = *(const f32x4*)(scales + TT + 32 * h + 8 * g + 4);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float scale = j < 4 ? s0[j & 3] : s1[j & 3];
+            const int t = at[h] + 8 * g + j;
+            w[j] = whole || (t >= lo[ct] && t < hi[ct]) ? w[j] * scale : 0.0f;
+          }
+        }
+        split8<PARTS>(w, weights[ct]);
+      }
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < VT; ++i) {
+        b16x8 value = v[i];
+        if (h + 1 < HALVES) v[i] = read_value(h + 1, i);
+        if constexpr (!FP4 && !whole) value = keep_range(value, wave_lo_min - (at[h] + 8 * g), wave_hi_max - (at[h] + 8 * g));
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, weights[ct][part], o[ct][i], 0, 0, 0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    }
+  };
   if (begin < end) {
+    look_ahead(begin);
     find_tile(begin);
-    request(begin, 0);
+    request(0);
+    look_ahead(begin + TT);
     deliver(0);
     turn();
   }
@@ -194,112 +329,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
     const bool more = base + TT < end;
     if (more) {
       find_tile(base + TT);
-      request(base + TT, buffer ^ 1);
+      request(buffer ^ 1);
+      look_ahead(base + 2 * TT);
     }
     // (a tile that no row of the wave sees: the others' diagonal)
     if (working && base < wave_hi_max && base + TT > wave_lo_min) {
-      const char* const keys = s_k + buffer * Tile::kBytes;
-      const char* const values = s_v + buffer * Tile::kBytes;
-      const float* const scales = s_scale + buffer * 2 * TT;
-      // ---- scores
-      float x[CT][HALVES][8];
-#pragma unroll
-      for (int i = 0; i < 2 * HALVES; ++i) {
-        const int t = 32 * (i / 2) + 8 * (n >> 2) + 4 * (i % 2) + (n & 3);
-        f32x4 acc[CT];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const b16x8 k = *(const b16x8*)(keys + 16 * Tile::key_at(t, 4 * st + g));
-#pragma unroll
-          for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[ct][st][part], acc[ct], 0, 0, 0);
-        }
-        if constexpr (FP4) {
-          const f32x4 scale = *(const f32x4*)(scales + 32 * (i / 2) + 8 * g + 4 * (i % 2));
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) acc[ct] *= scale;
-        }
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[ct][i / 2][4 * (i % 2) + j] = acc[ct][j];
-      }
-      // ---- what is not seen
       bool whole = true;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) whole = whole && at[h] >= wave_lo_max && at[h] + 32 <= wave_hi_min;
-      if (!whole)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int t = at[h] + 8 * g + j;
-              if (t < lo[ct] || t >= hi[ct]) x[ct][h][j] = -INFINITY;
-            }
-      // ---- the running maxima
-      float top[CT];
-      bool raise = false;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        top[ct] = x[ct][0][0];
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) top[ct] = fmaxf(top[ct], x[ct][h][j]);
-        top[ct] *= p.scale2;
-        raise = raise || top[ct] > m[ct] + kRaise;
-      }
-      if (__any(raise))
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 16));
-          top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 32));
-          const float raised = fmaxf(m[ct], top[ct]);
-          const float factor = m[ct] == raised ? 1.0f : __builtin_amdgcn_exp2f(m[ct] - raised);
-          m[ct] = raised;
-          l[ct] *= factor;
-#pragma unroll
-          for (int i = 0; i < VT; ++i) o[ct][i] *= factor;
-        }
-      // ---- weights, sums
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        b16x8 weights[CT][PARTS];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const float off = m[ct] == -INFINITY ? 0.0f : m[ct];
-          float w[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            w[j] = __builtin_amdgcn_exp2f(fmaf(x[ct][h][j], p.scale2, -off));
-            l[ct] += w[j];
-          }
-          if constexpr (FP4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float scale = scales[TT + 32 * h + 8 * g + j];
-              const int t = at[h] + 8 * g + j;
-              w[j] = whole || (t >= lo[ct] && t < hi[ct]) ? w[j] * scale : 0.0f;
-            }
-          }
-          split8<PARTS>(w, weights[ct]);
-        }
-#pragma unroll
-        for (int i = 0; i < VT; ++i) {
-          b16x8 v = *(const b16x8*)(values + 16 * Tile::value_at(16 * i + n, 4 * h + g));
-          if constexpr (!FP4)
-            if (!whole) v = keep_range(v, wave_lo_min - (at[h] + 8 * g), wave_hi_max - (at[h] + 8 * g));
-#pragma unroll
-          for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, weights[ct][part], o[ct][i], 0, 0, 0);
-        }
-      }
+      if (whole) work(at, buffer, Whole<true>{});
+      else work(at, buffer, Whole<false>{});
     }
     if (more) deliver(buffer ^ 1);
     turn();

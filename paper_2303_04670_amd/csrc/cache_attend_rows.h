@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF
       count = offset_of(tk, seq + 1) - token;
     }
     row0 = within = 0;
-    if (count <= 0 || (int64_t)count * p.share > kFewRows) return;
+    if (count <= 0 || (int64_t)count * p.share > p.few) return;
     rows_left = count * p.share;
   }
   const int past = tk.past[seq];

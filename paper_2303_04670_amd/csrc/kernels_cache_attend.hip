@@ -7,22 +7,22 @@
 namespace evk {
 namespace {
 
-// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
+// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row, or
+// (many tokens, of which most may have one) to a token.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
 template <bool BF16>
-__global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0) {
+__global__ __launch_bounds__(256) void attend_join(AttendParams p, int groups, int64_t block0) {
   __shared__ __align__(16) float s_sum[1024];
   __shared__ float s_total[256];
   const evconv_attend_args& a = p.a;
   const evconv_tokens& tk = a.tokens;
-  const int64_t row = row0 + blockIdx.x;
-  const int64_t token = row / a.heads_q;
-  const int head = (int)(row - token * a.heads_q);
+  const int64_t block = block0 + blockIdx.x;
+  const int64_t token = block / groups;
   const Piece piece = find_piece(tk, token, tk.seq_offsets ? -1 : (int)(tk.n_tokens / tk.n_seq), 1, 1, 0);
   const int within = (int)(token - piece.first);
   if (within < 0 || within >= piece.count) return;
   int s0 = 0, s1 = p.rows.splits - 1;
   if (!a.selected) {
-    const int chunk = (int64_t)piece.count * p.share <= kFewRows ? p.rows.chunk : p.pieces.chunk;
+    const int chunk = (int64_t)piece.count * p.share <= p.few ? p.rows.chunk : p.pieces.chunk;
     int lo, hi;
     seen_by(p, tk.past[piece.seq], within, lo, hi);
     if (hi <= lo) return;
@@ -32,34 +32,37 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int64_t row0)
   }
   const int64_t rows = tk.n_tokens * a.heads_q;
   const int lane = threadIdx.x & 63;
-  float big = -INFINITY;
-  for (int s = s0 + lane; s <= s1; s += 64) big = fmaxf(big, p.stat[2 * (s * rows + row)]);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d));
   // four channels to a thread, the rest of the threads to other stretches
-  const int quads = p.dp / 4, beside = 256 / quads, mine = threadIdx.x / quads, ch = threadIdx.x % quads * 4;
-  f32x4 sum = {0, 0, 0, 0};
-  float total = 0.0f;
-  if (mine < beside) {
+  const int quads = p.dp / 4, beside = 256 / quads, mine = threadIdx.x / quads, ch = threadIdx.x % quads * 4, c = threadIdx.x;
+  for (int head = (int)(block % groups); head < a.heads_q; head += groups) {
+    const int64_t row = token * a.heads_q + head;
+    float big = -INFINITY;
+    for (int s = s0 + lane; s <= s1; s += 64) big = fmaxf(big, p.stat[2 * (s * rows + row)]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d));
+    f32x4 sum = {0, 0, 0, 0};
+    float total = 0.0f;
+    if (mine < beside) {
 #pragma unroll 4
-    for (int s = s0 + mine; s <= s1; s += beside) {
-      const int64_t at = s * rows + row;
-      const float m = p.stat[2 * at], factor = m == big ? 1.0f : __builtin_amdgcn_exp2f(m - big);
-      total += factor * p.stat[2 * at + 1];
-      sum += factor * *(const f32x4*)(p.part + at * p.dp + ch);
+      for (int s = s0 + mine; s <= s1; s += beside) {
+        const int64_t at = s * rows + row;
+        const float m = p.stat[2 * at], factor = m == big ? 1.0f : __builtin_amdgcn_exp2f(m - big);
+        total += factor * p.stat[2 * at + 1];
+        sum += factor * *(const f32x4*)(p.part + at * p.dp + ch);
+      }
     }
+    __syncthreads();  // (the last head's sums have been read)
+    *(f32x4*)&s_sum[4 * threadIdx.x] = sum;
+    s_total[threadIdx.x] = total;
+    __syncthreads();
+    if (c >= a.cache.d) continue;
+    float o = 0.0f, all = 0.0f;
+    for (int i = 0; i < beside; ++i) {
+      o += s_sum[i * p.dp + c];
+      all += s_total[i * quads];
+    }
+    store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + c, all == 0.0f ? 0.0f : o / all);
   }
-  *(f32x4*)&s_sum[4 * threadIdx.x] = sum;
-  s_total[threadIdx.x] = total;
-  __syncthreads();
-  const int c = threadIdx.x;
-  if (c >= a.cache.d) return;
-  float o = 0.0f, all = 0.0f;
-  for (int i = 0; i < beside; ++i) {
-    o += s_sum[i * p.dp + c];
-    all += s_total[i * quads];
-  }
-  store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + c, all == 0.0f ? 0.0f : o / all);
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -93,18 +96,21 @@ size_t plan_attend(AttendParams& p) {
     cut(p.rows, extent, extent, fp4 ? 1024 : 512, 2048);
   } else {
     const int64_t extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
-    if (t.seq_offsets || len * p.share <= kFewRows) {
+    // (lengths of their own, many rows on average: the few short ones do not get a launch of their own)
+    p.few = t.seq_offsets && t.n_tokens * p.share >= 64 * (int64_t)t.n_seq ? 0 : kFewRows;
+    if (p.few && (t.seq_offsets || len * p.share <= kFewRows)) {
       p.rows.units = t.n_seq;
       cut(p.rows, extent, p.most, fp4 ? 1024 : 512, 2048);
     }
     const int rows = a.dtype == EVCONV_BF16 ? 128 : 64;
     if (t.seq_offsets) {
-      if (t.n_tokens * p.share > kFewRows) p.pieces.units = t.n_tokens * p.share / rows + t.n_seq;
+      if (t.n_tokens * p.share > p.few) p.pieces.units = t.n_tokens * p.share / rows + t.n_seq;
     } else if (len * p.share > kFewRows) {
       p.pieces.tiles = (int)((len * p.share + rows - 1) / rows);
       p.pieces.units = (int64_t)t.n_seq * p.pieces.tiles;
     }
-    if (p.pieces.units) cut(p.pieces, extent, p.most, 512, 1024);
+    // (a workgroup for every CU is enough where it has its rows' tokens to itself: the join costs more than a half-filled last round)
+    if (p.pieces.units) cut(p.pieces, extent, p.most, p.pieces.units * a.cache.heads >= 256 ? std::max<int64_t>(p.most, 1) : 512, 512);
   }
   const int splits = std::max(p.rows.splits, p.pieces.splits);
   if (splits == 1) return 0;
@@ -122,11 +128,12 @@ void launch_attend(const AttendParams& p, hipStream_t s) {
   if (p.rows.units) fp4 ? launch_attend_rows_fp4(p, s) : launch_attend_rows_bf16(p, s);
   if (p.pieces.units) fp4 ? launch_attend_pieces_fp4(p, s) : launch_attend_pieces_bf16(p, s);
   if (p.rows.splits == 1 && p.pieces.splits == 1) return;
-  const int64_t rows = p.a.tokens.n_tokens * p.a.heads_q, most = kMostThreads / 256;
-  for (int64_t at = 0; at < rows; at += most) {
-    const unsigned grid = (unsigned)std::min(most, rows - at);
-    if (p.a.dtype == EVCONV_BF16) attend_join<true><<<grid, 256, 0, s>>>(p, at);
-    else attend_join<false><<<grid, 256, 0, s>>>(p, at);
+  const int groups = p.a.tokens.n_tokens < 1024 ? p.a.heads_q : 1;
+  const int64_t blocks = p.a.tokens.n_tokens * groups, most = kMostThreads / 256;
+  for (int64_t at = 0; at < blocks; at += most) {
+    const unsigned grid = (unsigned)std::min(most, blocks - at);
+    if (p.a.dtype == EVCONV_BF16) attend_join<true><<<grid, 256, 0, s>>>(p, groups, at);
+    else attend_join<false><<<grid, 256, 0, s>>>(p, groups, at);
   }
 }
 

@@ -76,7 +76,7 @@ struct AttendWay {
   int chunk;      // tokens that a workgroup looks at (with chosen pages: of their list)
   int splits;     // workgroups that share a row's tokens
 };
-constexpr int kFewRows = 16;  // sequences of up to so many rows go the first way
+constexpr int kFewRows = 16;  // rows of a workgroup of the first way
 
 struct AttendParams {
   evconv_attend_args a;
@@ -86,6 +86,7 @@ struct AttendParams {
   int64_t most;     // tokens of a sequence that are looked at, at most
   float scale2;     // scale * log2(e)
   AttendWay rows, pieces;
+  int few;          // sequences of up to so many rows go the first way
   // workspace
   float* part;      // [splits][n_tokens * heads_q][dp] sums
   float* stat;      // [splits][n_tokens * heads_q][2] largest exponent, sum of weights
