@@ -20,6 +20,7 @@ struct AppendParams {
   double per_channel;  // 1 / d
   int per;          // pages that a sequence of equal lengths can reach, or -1
   int roles;        // heads of queries and of keys with their values together
+  int per_group;    // of them, those of a workgroup
   int groups;       // workgroups that share the roles of a page
   int64_t block0;   // first workgroup of this launch
   bool single;      // one token of every sequence
@@ -268,6 +269,53 @@ __device__ __forceinline__ void store_row(void* q, int64_t at, int ch, int left,
 // and those of its neighbours do not meet in a bank.
 __host__ __device__ constexpr int value_row(bool fp4) { return (fp4 ? 1 : 2) * kPiece + 4; }
 
+// Least and largest of keys, two to a word: bf16 numbers as 16-bit integers of the same order.  What is no number counts as beyond both
+// ends, and becomes one again.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ i16x2 ordered(unsigned two) {
+  const i16x2 v = __builtin_bit_cast(i16x2, two);
+  return v ^ ((v >> 15) & (short)0x7fff);
+}
+__device__ __forceinline__ unsigned as_bf16(i16x2 v) { return __builtin_bit_cast(unsigned, v ^ ((v >> 15) & (short)0x7fff)); }
+struct Bounds {
+  i16x2 lo[2][4], hi[2][4];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lo[h][j] = 32767, hi[h][j] = -32768;
+  }
+  __device__ __forceinline__ void add(int h, int j, i16x2 l, i16x2 u) {
+    lo[h][j] = __builtin_elementwise_min(lo[h][j], l);
+    hi[h][j] = __builtin_elementwise_max(hi[h][j], u);
+  }
+  // A key's eight values, as the cache in bf16 has them; of a row that is marked the numbers are none.
+  __device__ __forceinline__ void add_key(int h, const unsigned (&w)[4], bool bad) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const i16x2 v = ordered(w[j]);
+      const bool low = bad && (w[j] & 0x7fffu) > 0x7f80u, high = bad && (w[j] >> 16 & 0x7fffu) > 0x7f80u;
+      i16x2 l = v, u = v;
+      if (low) l.x = -32768, u.x = 32767;
+      if (high) l.y = -32768, u.y = 32767;
+      add(h, j, l, u);
+    }
+  }
+  // Those that a page had: numbers, or none in both.
+  __device__ __forceinline__ void add_old(int h, const uint4& low, const uint4& high) {
+    const unsigned l[4] = {low.x, low.y, low.z, low.w}, u[4] = {high.x, high.y, high.z, high.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      i16x2 a = ordered(l[j]), b = ordered(u[j]);
+      if ((l[j] & 0x7fffu) > 0x7f80u) a.x = -32768, b.x = 32767;
+      if ((l[j] >> 16 & 0x7fffu) > 0x7f80u) a.y = -32768, b.y = 32767;
+      add(h, j, a, b);
+    }
+  }
+  __device__ __forceinline__ uint4 low(int h) const { return make_uint4(as_bf16(lo[h][0]), as_bf16(lo[h][1]), as_bf16(lo[h][2]), as_bf16(lo[h][3])); }
+  __device__ __forceinline__ uint4 high(int h) const { return make_uint4(as_bf16(hi[h][0]), as_bf16(hi[h][1]), as_bf16(hi[h][2]), as_bf16(hi[h][3])); }
+};
+
 template <bool BF16, bool FP4, int MODE, int LANES>
 __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(AppendParams p) {
   constexpr bool VEC = MODE != kAnyRows;
@@ -291,7 +339,7 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
   float* const s_cos = (float*)s_mem;
   float* const s_sin = s_cos + kPiece * half;
   char* const s_v = s_mem + 2 * sizeof(float) * (kPiece * half + p.dp) + wave * p.dp * value_row(FP4);
-  const int per_group = (p.roles + p.groups - 1) / p.groups, role_end = min((group + 1) * per_group, p.roles);
+  const int role_end = min((group + 1) * p.per_group, p.roles);
   float* const s_wq = (float*)(s_mem + 2 * sizeof(float) * kPiece * half);  // weights of the norms, zeros behind them
   float* const s_wk = s_wq + p.dp;
   for (int i = threadIdx.x; i < p.dp; i += blockDim.x) {
@@ -308,7 +356,7 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
       sine_cosine((double)(a.positions ? a.positions[token + r] : from + r) * (double)a.freqs[f], s_sin[i], s_cos[i]);
     }
     __syncthreads();
-    int role = group * per_group + wave;
+    int role = group * p.per_group + wave;
     for (; role < min(role_end, a.heads_q); role += waves) {  // ---- a head of the queries
       const int64_t head_in = role * a.q.head_stride, head_out = role * a.q_out_head_stride;
       for (int r0 = 0; r0 < count; r0 += AT_ONCE * ROWS) {
@@ -334,11 +382,8 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
       const int head = role - a.heads_q;
       const int64_t at = ((int64_t)to * c.heads + head) * c.page;  // tokens before this head's of the page
       const int64_t k_head = head * a.k.head_stride, v_head = head * a.v.head_stride;
-      float lo[2][8], hi[2][8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) lo[h][j] = INFINITY, hi[h][j] = -INFINITY;
+      Bounds bounds;
+      bounds.clear();
       for (int r0 = 0; r0 < count; r0 += ROWS) {
         const int r = r0 + row, r_in = min(r, count - 1);
         const bool live = r < count;
@@ -350,7 +395,8 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
         zero_outside<MODE>(own, v);
         turn_row<BF16, MODE, LANES>(p, a.k.data, k_row, own, a.k_norm, s_wk, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x);
         const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
-        if (big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16))
+        const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
+        if (bad)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -361,9 +407,11 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
         for (int h = 0; h < 2; ++h) {
           const int ch = own.ch[h];
           if (ch >= p.dp) continue;
+          const unsigned kw[4] = {pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7])};
+          bounds.add_key(h, kw, bad);
           if constexpr (FP4) {
-            const unsigned k4 = codes_of(x[h], big_k), v4 = codes_of(v[h], big_v);
-            *(unsigned*)((char*)c.k + (at + slot + r) * (p.dp / 2) + ch / 2) = k4;
+            const unsigned v4 = codes_of(v[h], big_v);
+            *(unsigned*)((char*)c.k + (at + slot + r) * (p.dp / 2) + ch / 2) = codes_of(x[h], big_k);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s_v[(ch + j) * value_row(true) + slot % kPiece + r] = (char)(v4 >> (4 * j) & 15);
             if (ch == 0) {
@@ -371,8 +419,7 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
               c.v_scale[at + slot + r] = scale_of(big_v);
             }
           } else {
-            *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) =
-                make_uint4(pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7]));
+            *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
               unsigned w = pack_bf16(v[h][j], v[h][j + 1]);
@@ -380,21 +427,9 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
                 if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
                 if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
               }
-              if (count == kPiece) {
-                *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * r) = (uint16_t)w;
-                *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * r) = (uint16_t)(w >> 16);
-              } else {
-                uint16_t* const q = (uint16_t*)c.v + ((int64_t)to * c.heads + head) * p.dp * c.page + (int64_t)(ch + j) * c.page + slot + r;
-                q[0] = (uint16_t)w;
-                q[c.page] = (uint16_t)(w >> 16);
-              }
+              *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)w;
+              *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)(w >> 16);
             }
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float k = bf16_low(pack_bf16(x[h][j], 0.0f));  // (as the cache in bf16 has it; a NaN stays in both bounds)
-            if (k < lo[h][j] || k != k) lo[h][j] = k;
-            if (k > hi[h][j] || k != k) hi[h][j] = k;
           }
         }
       }
@@ -427,6 +462,11 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
           const unsigned* const row32 = (const unsigned*)(s_v + k * value_row(false)) + 4 * part;
           *(uint4*)(v_rows + ((int64_t)k * c.page + slot + 8 * part) * 2) = make_uint4(row32[0], row32[1], row32[2], row32[3]);
         }
+      } else {  // the call's tokens alone
+        const int first = slot % kPiece, t = lane % kPiece;
+        if (t >= first && t < first + count)
+          for (int k = lane / kPiece; k < p.dp; k += 64 / kPiece)
+            *(uint16_t*)(v_rows + ((int64_t)k * c.page + slot - first + t) * 2) = *(const uint16_t*)(s_v + k * value_row(false) + 2 * t);
       }
       lds_turn();
       // ---- bounds: over the piece's tokens, then with what the page had unless it begins here
@@ -434,29 +474,17 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int s = LANES; s < 64; s *= 2) {
-            const float l = __shfl_xor(lo[h][j], s), u = __shfl_xor(hi[h][j], s);
-            if (l < lo[h][j] || l != l) lo[h][j] = l;
-            if (u > hi[h][j] || u != u) hi[h][j] = u;
-          }
+          for (int s = LANES; s < 64; s *= 2)
+            bounds.add(h, j, __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, bounds.lo[h][j]), s)),
+                       __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, bounds.hi[h][j]), s)));
         if (row == 0 && own.ch[h] < p.dp) {
           uint4* const q = (uint4*)((uint16_t*)c.bounds + (((int64_t)to * c.heads + head) * 2) * p.dp + own.ch[h]);
           uint4* const q_hi = (uint4*)((uint16_t*)q + p.dp);
-          if (slot > 0) {
-            float old[8];
-            load_run<true, 8, true>(q, 0, 8, old);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (old[j] < lo[h][j] || old[j] != old[j]) lo[h][j] = old[j];
-            load_run<true, 8, true>(q_hi, 0, 8, old);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (old[j] > hi[h][j] || old[j] != old[j]) hi[h][j] = old[j];
-          }
-          *q = make_uint4(pack_bf16(lo[h][0], lo[h][1]), pack_bf16(lo[h][2], lo[h][3]), pack_bf16(lo[h][4], lo[h][5]), pack_bf16(lo[h][6], lo[h][7]));
-          *q_hi = make_uint4(pack_bf16(hi[h][0], hi[h][1]), pack_bf16(hi[h][2], hi[h][3]), pack_bf16(hi[h][4], hi[h][5]), pack_bf16(hi[h][6], hi[h][7]));
+          if (slot > 0) bounds.add_old(h, *q, *q_hi);
+          *q = bounds.low(h);
+          *q_hi = bounds.high(h);
         }
       }
     }
@@ -503,7 +531,8 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
   }
   zero_outside<MODE>(own, v);
   const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
-  if (big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16))
+  const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
+  if (bad)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -516,6 +545,7 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
   for (int h = 0; h < 2; ++h) {
     const int ch = own.ch[h];
     if (ch >= p.dp) continue;
+    const unsigned kw[4] = {pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7])};
     if constexpr (FP4) {
       uint8_t* const q = (uint8_t*)c.v + (column + ch) * (c.page / 2) + slot / 2;
       unsigned old[8];
@@ -531,8 +561,7 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
         c.v_scale[at] = scale_of(big_v);
       }
     } else {
-      *(uint4*)((uint16_t*)c.k + at * p.dp + ch) =
-          make_uint4(pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7]));
+      *(uint4*)((uint16_t*)c.k + at * p.dp + ch) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
       uint16_t* const q = (uint16_t*)c.v + (column + ch) * c.page + slot;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -543,22 +572,12 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
     if (c.bounds) {
       uint4* const q = (uint4*)((uint16_t*)c.bounds + 2 * column + ch);
       uint4* const q_hi = (uint4*)((uint16_t*)q + p.dp);
-      float lo[8], hi[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) lo[j] = hi[j] = bf16_low(pack_bf16(x[h][j], 0.0f));
-      if (slot > 0) {
-        float old[8];
-        load_run<true, 8, true>(q, 0, 8, old);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (old[j] < lo[j] || old[j] != old[j]) lo[j] = old[j];
-        load_run<true, 8, true>(q_hi, 0, 8, old);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (old[j] > hi[j] || old[j] != old[j]) hi[j] = old[j];
-      }
-      *q = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(lo[4], lo[5]), pack_bf16(lo[6], lo[7]));
-      *q_hi = make_uint4(pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]), pack_bf16(hi[4], hi[5]), pack_bf16(hi[6], hi[7]));
+      Bounds bounds;
+      bounds.clear();
+      bounds.add_key(h, kw, bad);
+      if (slot > 0) bounds.add_old(h, *q, *q_hi);
+      *q = bounds.low(h);
+      *q_hi = bounds.high(h);
     }
   }
 }
@@ -657,8 +676,11 @@ void launch_cache_append(const evconv_append_args& a, bool vec, hipStream_t s) {
   p.roles = a.heads_q + a.cache.heads;
   p.single = !t.seq_offsets && t.n_tokens == t.n_seq;
   const int64_t pages = p.per >= 0 ? (int64_t)p.per * t.n_seq : t.n_tokens / a.cache.page + 2 * (int64_t)t.n_seq;
-  // Workgroups of a page: as many as fill the chip a few times over, with a role at least for each of their waves.
-  p.groups = (int)std::max<int64_t>(1, std::min<int64_t>((p.roles + 3) / 4, 2048 / std::max<int64_t>(pages, 1)));
+  // Workgroups of a page: as many as fill the chip a few times over, each with whole rounds of roles for its four waves.  (More compute the
+  // angles more often; 8 x 4096 tokens of 40 roles, us: 3 groups 275, 5 237, 10 247.)
+  const int64_t rounds = (p.roles + 3) / 4;
+  p.per_group = 4 * (int)std::max<int64_t>(1, std::min(rounds, rounds * pages / 2048));
+  p.groups = (p.roles + p.per_group - 1) / p.per_group;
   const int64_t blocks = pages * p.groups;
   const bool fp4 = a.cache.kind == EVCONV_CACHE_FP4;
   if (a.dtype == EVCONV_BF16) fp4 ? start_append<true, true>(p, vec, blocks, s) : start_append<true, false>(p, vec, blocks, s);
