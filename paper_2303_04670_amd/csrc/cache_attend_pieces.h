@@ -35,7 +35,7 @@ struct Whole {
 template <bool FP4, bool BF16, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendParams p, int64_t block0) {
   using Tile = PieceTile<DP>;
-  constexpr int PARTS = BF16 ? 1 : 3, CT = BF16 ? 2 : 1, ROWS = 64 * CT, STEPS = DP / 32, VT = DP / 16, TT = Tile::kTokens, HALVES = Tile::kHalves;
+  constexpr int PARTS = BF16 ? 1 : 3, CT = BF16 ? 2 : 1, ROWS = BF16 ? kPieceRowsBf16 : kPieceRowsF32, STEPS = DP / 32, VT = DP / 16, TT = Tile::kTokens, HALVES = Tile::kHalves;
   extern __shared__ __align__(16) char s_mem[];
   char* const s_k = s_mem;
   char* const s_v = s_mem + 2 * Tile::kBytes;
@@ -65,7 +65,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
   seen_by(p, past, (int)(row0 / p.share), lo_min, other);
   seen_by(p, past, last / p.share, other, hi_max);
   const int chunk = p.pieces.chunk;
-  const int64_t begin = max((int64_t)split * chunk, (int64_t)lo_min) & ~(int64_t)(TT - 1), end = min((int64_t)(split + 1) * chunk, (int64_t)hi_max);
+  const int base0 = stretch_base(lo_min);
+  const int64_t begin = max(base0 + (int64_t)split * chunk, (int64_t)lo_min) & ~(int64_t)(TT - 1), end = min(base0 + (int64_t)(split + 1) * chunk, (int64_t)hi_max);
   if (begin >= end && split != 0) return;
   // of this wave: its first and last row, what all of them and what any of them sees
   const int64_t wave_row = row0 + wave * 16 * CT;
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
   for (int ct = 0; ct < CT; ++ct) {
     l[ct] += __shfl_xor(l[ct], 16);
     l[ct] += __shfl_xor(l[ct], 32);
-    const int fate = live[ct] ? fate_of(lo[ct], hi[ct], split, chunk) : 0;
+    const int fate = live[ct] ? fate_of(lo[ct], hi[ct], base0, split, chunk) : 0;
     if (fate == 1) {
       const float inverse = l[ct] == 0.0f ? 0.0f : 1.0f / l[ct];
       const int64_t at = (int64_t)token[ct] * a.o_token_stride + q_head[ct] * a.o_head_stride;

@@ -51,10 +51,12 @@ __device__ __forceinline__ void seen_by(const AttendParams& p, int64_t past, int
   lo = p.a.window ? (int)min(max(position + 1 - p.a.window, (int64_t)0), (int64_t)hi) : 0;
 }
 
-// What a workgroup does with what it found of such a row in stretch `split`: 0 nothing, 1 the output, 2 a part of it.
-__device__ __forceinline__ int fate_of(int lo, int hi, int split, int chunk) {
+// Where the stretches of a workgroup's rows begin, of the first position that its first row sees.
+__device__ __forceinline__ int stretch_base(int lo) { return lo & ~127; }
+// What a workgroup does with what it found of a row in stretch `split`: 0 nothing, 1 the output, 2 a part of it.
+__device__ __forceinline__ int fate_of(int lo, int hi, int base, int split, int chunk) {
   if (hi <= lo) return split == 0;
-  const int s0 = lo / chunk, s1 = (hi - 1) / chunk;
+  const int s0 = (lo - base) / chunk, s1 = (hi - 1 - base) / chunk;
   return split < s0 || split > s1 ? 0 : s0 == s1 ? 1 : 2;
 }
 
@@ -112,7 +114,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF
     lo_min = min(lo_min, __shfl_xor(lo_min, s));
     lo_max = max(lo_max, __shfl_xor(lo_max, s));
   }
-  int64_t begin = (int64_t)split * p.rows.chunk, end = begin + p.rows.chunk;
+  const int base0 = LIST ? 0 : stretch_base(__shfl(lo, 0));
+  int64_t begin = base0 + (int64_t)split * p.rows.chunk, end = begin + p.rows.chunk;
   int fate;
   if constexpr (LIST) {
     end = min(end, (int64_t)a.count << p.log);
@@ -120,7 +123,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF
   } else {
     begin = max(begin, (int64_t)lo_min);
     end = min(end, (int64_t)hi_max);
-    fate = fate_of(lo, hi, split, p.rows.chunk);
+    fate = fate_of(lo, hi, base0, split, p.rows.chunk);
   }
   if (!live) fate = 0;
   if (!__any(fate)) return;  // (alike in all waves)

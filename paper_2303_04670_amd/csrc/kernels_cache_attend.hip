@@ -20,22 +20,29 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int groups, i
   const Piece piece = find_piece(tk, token, tk.seq_offsets ? -1 : (int)(tk.n_tokens / tk.n_seq), 1, 1, 0);
   const int within = (int)(token - piece.first);
   if (within < 0 || within >= piece.count) return;
-  int s0 = 0, s1 = p.rows.splits - 1;
-  if (!a.selected) {
-    const int chunk = (int64_t)piece.count * p.share <= p.few ? p.rows.chunk : p.pieces.chunk;
-    int lo, hi;
-    seen_by(p, tk.past[piece.seq], within, lo, hi);
-    if (hi <= lo) return;
-    s0 = lo / chunk;
-    s1 = (hi - 1) / chunk;
-    if (s0 == s1) return;
-  }
+  const bool few = (int64_t)piece.count * p.share <= p.few;
+  const int past = tk.past[piece.seq], chunk = few ? p.rows.chunk : p.pieces.chunk;
+  int lo, hi;
+  seen_by(p, past, within, lo, hi);
+  if (!a.selected && hi - lo <= 1) return;  // (no stretch, or one)
   const int64_t rows = tk.n_tokens * a.heads_q;
   const int lane = threadIdx.x & 63;
   // four channels to a thread, the rest of the threads to other stretches
   const int quads = p.dp / 4, beside = 256 / quads, mine = threadIdx.x / quads, ch = threadIdx.x % quads * 4, c = threadIdx.x;
   for (int head = (int)(block % groups); head < a.heads_q; head += groups) {
     const int64_t row = token * a.heads_q + head;
+    int s0 = 0, s1 = p.rows.splits - 1;
+    if (!a.selected) {
+      // (the tile of rows that the workgroup had: its first row's token)
+      constexpr int kTile = BF16 ? kPieceRowsBf16 : kPieceRowsF32;
+      const int64_t in_group = (int64_t)within * p.share + head % p.share;
+      int first, other;
+      seen_by(p, past, few ? 0 : (int)(in_group / kTile * kTile / p.share), first, other);
+      const int base = stretch_base(first);
+      s0 = (lo - base) / chunk;
+      s1 = (hi - 1 - base) / chunk;
+      if (s0 == s1) continue;
+    }
     float big = -INFINITY;
     for (int s = s0 + lane; s <= s1; s += 64) big = fmaxf(big, p.stat[2 * (s * rows + row)]);
 #pragma unroll
@@ -81,28 +88,28 @@ size_t plan_attend(AttendParams& p) {
   const bool fp4 = a.cache.kind == EVCONV_CACHE_FP4;
   const int64_t len = t.n_tokens / t.n_seq;
   // Stretches of `extent` tokens for `units` workgroups a stretch: so many that there are `wanted` workgroups, but none shorter than `least`.
-  auto cut = [&](AttendWay& way, int64_t extent, int64_t all, int64_t least, int64_t wanted) {
+  auto cut = [&](AttendWay& way, int64_t extent, int64_t least, int64_t wanted) {
     const int64_t workgroups = std::max<int64_t>(way.units * a.cache.heads, 1);
     int64_t chunk = std::max(least, (int64_t)((double)workgroups * extent / wanted));
-    chunk = std::max(chunk, (all + 65534) / 65535);  // (a grid's second size)
+    chunk = std::max(chunk, (extent + 65534) / 65535);  // (a grid's second size)
     way.chunk = (int)std::min<int64_t>((chunk + 127) / 128 * 128, 1 << 30);
-    way.splits = (int)std::max<int64_t>((all + way.chunk - 1) / way.chunk, 1);
+    way.splits = (int)std::max<int64_t>((extent + way.chunk - 1) / way.chunk, 1);
   };
   p.rows = p.pieces = AttendWay{0, -1, 128, 1};
   if (a.selected) {
     p.rows.tiles = (p.share + kFewRows - 1) / kFewRows;
     p.rows.units = t.n_tokens * p.rows.tiles;
-    const int64_t extent = (int64_t)a.count * a.cache.page;
-    cut(p.rows, extent, extent, fp4 ? 1024 : 512, 2048);
+    cut(p.rows, (int64_t)a.count * a.cache.page, 256, 2048);
   } else {
-    const int64_t extent = a.window ? std::min<int64_t>(p.most, (int64_t)a.window + (t.seq_offsets ? t.n_tokens : len)) : p.most;
+    // (a workgroup's rows are of so many tokens at most, and its stretches begin up to 127 before the first that they see)
+    auto seen = [&](int64_t tokens) { return a.window ? std::min<int64_t>(p.most, (int64_t)a.window + tokens + 127) : p.most; };
     // (lengths of their own, many rows on average: the few short ones do not get a launch of their own)
     p.few = t.seq_offsets && t.n_tokens * p.share >= 64 * (int64_t)t.n_seq ? 0 : kFewRows;
     if (p.few && (t.seq_offsets || len * p.share <= kFewRows)) {
       p.rows.units = t.n_seq;
-      cut(p.rows, extent, p.most, fp4 ? 1024 : 512, 2048);
+      cut(p.rows, seen(kFewRows), fp4 ? 1024 : 512, 2048);
     }
-    const int rows = a.dtype == EVCONV_BF16 ? 128 : 64;
+    const int rows = a.dtype == EVCONV_BF16 ? kPieceRowsBf16 : kPieceRowsF32;
     if (t.seq_offsets) {
       if (t.n_tokens * p.share > p.few) p.pieces.units = t.n_tokens * p.share / rows + t.n_seq;
     } else if (len * p.share > kFewRows) {
@@ -110,7 +117,7 @@ size_t plan_attend(AttendParams& p) {
       p.pieces.units = (int64_t)t.n_seq * p.pieces.tiles;
     }
     // (a workgroup for every CU is enough where it has its rows' tokens to itself: the join costs more than a half-filled last round)
-    if (p.pieces.units) cut(p.pieces, extent, p.most, p.pieces.units * a.cache.heads >= 256 ? std::max<int64_t>(p.most, 1) : 512, 512);
+    if (p.pieces.units) cut(p.pieces, seen(rows), p.pieces.units * a.cache.heads >= 256 ? std::max<int64_t>(p.most, 1) : 512, 512);
   }
   const int splits = std::max(p.rows.splits, p.pieces.splits);
   if (splits == 1) return 0;

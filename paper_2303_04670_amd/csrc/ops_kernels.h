@@ -76,7 +76,8 @@ struct AttendWay {
   int chunk;      // tokens that a workgroup looks at (with chosen pages: of their list)
   int splits;     // workgroups that share a row's tokens
 };
-constexpr int kFewRows = 16;  // rows of a workgroup of the first way
+constexpr int kFewRows = 16;                             // rows of a workgroup of the first way
+constexpr int kPieceRowsBf16 = 128, kPieceRowsF32 = 64;  // of the second
 
 struct AttendParams {
   evconv_attend_args a;

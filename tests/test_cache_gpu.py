@@ -374,3 +374,259 @@ def test_select_of_many_pages(n_pages):
     for count in (1, 2, 3, 64, 1000, 4999, 6000):
         got = ops.cache_select(q, cache, table, past, count, first=min(count - 1, 1)).cpu().tolist()[0][0]
         assert got == ops_ref.choose(32 * values, count, min(count - 1, 1), 1), count
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("news", [[1, 1, 1], [40, 3, 150]])
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_bad_values_reach_those_who_look_at_them(value, where, news, dtype, kind):
+    """One token of one head: its stream's queries of that head from its position on are NaN, all others as without it."""
+    torch, ops = torch_ops()
+    past = [70, 0, 33]
+    st = whole(past, news, 2, 2, 64, kind, 32)
+    t, n = torch.float32 if dtype == "f32" else torch.bfloat16, sum(news)
+    q = torch.from_numpy(st.rng.standard_normal((n, 4, 64))).to(t).cuda()
+    clean = ops.cache_attend(q, st.cache, **st.args())
+    # the stream's last tokens again, one of them with a bad value
+    s, again = 0, 40 if news[0] > 1 else 1
+    at = past[0] + news[0] - again
+    rows = {i: torch.from_numpy(getattr(st, i)[s][at:at + again]).float() for i in ("k", "v")}
+    bad = again // 2
+    rows[where][bad, 1, 17] = value
+    args = st.args()
+    ops.cache_append(st.cache, rows["k"].cuda(), rows["v"].cuda(), args["table"][:1], torch.tensor([at], dtype=torch.int32, device="cuda"))
+    got = ops.cache_attend(q, st.cache, **st.args())
+    hit = torch.zeros(n, 4, dtype=torch.bool)
+    hit[max(at + bad - past[0], 0):news[0], 2:] = True
+    assert got[hit.cuda()].isnan().all()
+    if kind == "bf16":  # (rows of 4 bits are rounded once more by being appended again)
+        assert torch.equal(got[~hit.cuda()], clean[~hit.cuda()])
+    else:
+        assert torch.isfinite(got[~hit.cuda()]).all()
+    # and a page that holds such a key is always worth a look
+    if where == "k" or kind == "bf16":
+        last = past[0] + news[0] - 1
+        chosen = ops.cache_select(q[news[0] - 1:news[0]].contiguous(), st.cache, args["table"][:1], torch.tensor([last], dtype=torch.int32, device="cuda"), 3)
+        assert (at + bad) // 32 in chosen[0, 1].tolist()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("news", [[1, 1], [50, 3]])
+def test_rows_anywhere(news, dtype, kind):
+    """Slices of one projection at odd places, results between others', queries in place, angles by positions of their own."""
+    torch, ops = torch_ops()
+    t, n, d, g = torch.float32 if dtype == "f32" else torch.bfloat16, sum(news), 24, torch.Generator().manual_seed(3)
+    wide = torch.randn(n, 3 + 6 * d + 5, generator=g).to(t).cuda()
+    parts = [wide[:, 3 + a * d:3 + b * d].unflatten(1, (-1, d)) for a, b in ((0, 2), (2, 4), (4, 6))]
+    positions = torch.randint(0, 1 << 40, (n,), generator=g).cuda()
+    one, two = Streams(4, [40, 0], news, 2, d, kind, 32).fill(), Streams(4, [40, 0], news, 2, d, kind, 32).fill()
+    kw = dict(freqs=freqs_of(24) * 1e-6, positions=positions, q_norm=torch.ones(d, device="cuda"))
+    plain = [p.contiguous() for p in parts]
+    before = wide.clone()
+    q = ops.cache_append(one.cache, plain[1], plain[2], q=plain[0], **kw, **one.args())
+    assert torch.equal(wide, before)
+    same = ops.cache_append(two.cache, parts[1], parts[2], q=parts[0], q_out=parts[0], **kw, **two.args())
+    assert same is parts[0] and torch.equal(same, q) and torch.equal(wide[:, :3], before[:, :3]) and torch.equal(wide[:, 3 + 2 * d:], before[:, 3 + 2 * d:])
+    for a, b in zip(ops.cache_read(one.cache, n=n, **one.args()), ops.cache_read(two.cache, n=n, **two.args())):
+        assert torch.equal(a, b)
+    close_rows(q, ops_ref.head_rows(before[:, 3:3 + 2 * d].unflatten(1, (-1, d)).float().cpu().numpy(), np.ones(d), 1e-6, kw["freqs"].cpu().numpy(), "halves",
+                                    positions.cpu().numpy()), dtype == "bf16")
+    want = ops.cache_attend(q, one.cache, **one.args())
+    room = torch.full((n, 4, d + 3), 7.0, dtype=t, device="cuda")
+    out = ops.cache_attend(parts[0], two.cache, out=room[:, 1:3, 2:2 + d], **two.args())
+    assert torch.equal(out, want) and room[:, 0].eq(7).all() and room[:, 3].eq(7).all() and room[:, :, :2].eq(7).all() and room[:, :, -1].eq(7).all()
+    a, b = (ops.cache_select(x, st.cache, count=4, **st.args()) for x, st in ((q, one), (parts[0], two)))
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("news", [[1] * 6, [30, 1, 70, 2, 90, 5]])
+def test_tokens_that_have_no_place(news, kind):
+    """Table entries and positions out of range hold nothing, and nothing is written for them."""
+    torch, ops = torch_ops()
+    past = [100, 100, 100, -3, 60, 2 ** 31 - 1]
+    st = Streams(5, [100, 100, 100, 0, 60, 0], news, 1, 32, kind, 32).fill()
+    st.past = past
+    st.table[0, 1], st.table[1, 3], st.table[2, 0] = -1, st.n_pages, -2 ** 31
+    st.table[5] = -1  # (its past is said to be long, but was never written)
+    args = st.args()
+    args["table"] = args["table"][:, :5].contiguous()  # stream 2 and 4 run out of it
+    n, g = sum(news), torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(n, 1, 32, generator=g).cuda() for _ in range(3))
+    before = [x if x is None else x.clone() for x in st.cache[:5]]
+    ops.cache_append(st.cache, k, v, q=q, **args)
+    back_k, back_v = (x.cpu().numpy() for x in ops.cache_read(st.cache, n=n, **args))
+    got = ops.cache_attend(q, st.cache, **args).cpu().numpy()
+    chosen = ops.cache_select(q, st.cache, count=6, **args).cpu().numpy()
+    looked = ops.cache_attend(q, st.cache, selected=torch.from_numpy(chosen).cuda(), **args).cpu().numpy()
+    pages, i, written = st.table[:, :5], 0, set()
+    there = lambda s, t: 0 <= t < 5 * 32 and 0 <= pages[s, t // 32] < st.n_pages
+    for s, new in enumerate(news):
+        held = {t: (st.k[s][t], st.v[s][t]) for t in range(max(min(past[s], 160), 0)) if t < len(st.k[s]) and there(s, t)}
+        for j in range(new):
+            t = past[s] + j
+            if there(s, t):
+                held[t] = (st.held(k[i].cpu().numpy()), st.held(v[i].cpu().numpy()))
+                written.add(int(pages[s, t // 32]))
+                assert np.allclose(back_k[i], held[t][0], atol=1e-6) and np.allclose(back_v[i], held[t][1], atol=1e-6)
+            else:
+                assert not back_k[i].any() and not back_v[i].any()
+            seen = [x for u, x in held.items() if u <= t]
+            want = np.zeros((1, 32))
+            if seen:
+                kk, vv = np.stack([x[0] for x in seen])[:, 0], np.stack([x[1] for x in seen])[:, 0]
+                want, _ = ops_ref.attend(q[i].cpu().numpy().astype(np.float64), kk, vv, 32 ** -0.5, np.ones((1, len(kk)), bool))
+            assert np.allclose(got[i], want, atol=2e-5) and np.allclose(looked[i], want, atol=2e-5), (s, j)
+            assert [c for c in chosen[i, 0] if c >= 0] == [c for c in range(min(max(t, -1) // 32, 4) + 1) if 0 <= pages[s, c] < st.n_pages]
+            i += 1
+    for page in set(range(st.n_pages)) - written:
+        for x, y in zip(before, st.cache[:5]):
+            assert x is None or torch.equal(x[page].view(torch.uint8), y[page].view(torch.uint8))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+def test_offsets_out_of_order_stay_inside(kind):
+    torch, ops = torch_ops()
+    st = whole([100] * 4, [20] * 4, 1, 2, 64, kind, 32)
+    args, q = st.args(), torch.randn(80, 4, 64, device="cuda")
+    for bad in ([0, 50, 20, 70, 80], [-5, 20, 200, 60, 80], [80, 60, 40, 20, 0], [0, 0, 0, 0, 0], [30, 31, 32, 33, 34], [2 ** 31 - 1, -2 ** 31, 5, 90, 7]):
+        args["seq_offsets"] = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        k = torch.randn(80, 2, 64, device="cuda")
+        ops.cache_append(st.cache, k, k, q=q, **args)
+        ops.cache_read(st.cache, n=80, **args)
+        chosen = ops.cache_select(q, st.cache, count=3, out=torch.full((80, 2, 3), 99, dtype=torch.int32, device="cuda"), **args)
+        ops.cache_attend(q, st.cache, **args)
+        ops.cache_attend(q, st.cache, selected=chosen, **args)
+    torch.cuda.synchronize()
+    # rows of no sequence are left as they were
+    args["seq_offsets"] = torch.tensor([10, 20, 20, 50, 60], dtype=torch.int32, device="cuda")
+    out = torch.full((80, 4, 64), 3.0, device="cuda")
+    ops.cache_attend(q, st.cache, out=out, **args)
+    rotated = ops.cache_append(st.cache, k, k, q=q, q_out=torch.full_like(q, 3.0), freqs=freqs_of(64), **args)
+    for x in (out, rotated):
+        assert x[:10].eq(3).all() and x[60:].eq(3).all() and not x[10:60].eq(3).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+def test_cache_behind_32_bits(kind):
+    """Pages whose values begin behind 2^32 bytes."""
+    torch, ops = torch_ops()
+    d, page, pages = 128, 256, 70000 if kind == "bf16" else 280000
+    cache = ops.cache_new(pages, 1, d, page=page, kind=kind)
+    table = torch.arange(pages - 1, pages - 5, -1, dtype=torch.int32, device="cuda").view(2, 2).contiguous()
+    past, n = torch.zeros(2, dtype=torch.int32, device="cuda"), 600
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(n, h, d, generator=g).cuda() for h in (2, 1, 1))
+    ops.cache_append(cache, k, v, table, past, q)
+    small = ops.cache_new(4, 1, d, page=page, kind=kind)
+    near = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    ops.cache_append(small, k, v, near, past, q)
+    for a, b in zip(ops.cache_read(cache, table, past, n), ops.cache_read(small, near, past, n)):
+        assert torch.equal(a, b)
+    last = torch.full((2,), 299, dtype=torch.int32, device="cuda")
+    for rows, at in ((q, past), (q[:2].contiguous(), last)):
+        assert torch.equal(ops.cache_attend(rows, cache, table, at), ops.cache_attend(rows, small, near, at))
+        one, two = (ops.cache_select(rows, c, t, at, 2) for c, t in ((cache, table), (small, near)))
+        assert torch.equal(one, two)
+        assert torch.equal(ops.cache_attend(rows, cache, table, at, selected=one), ops.cache_attend(rows, small, near, at, selected=two))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("hq,hk,past,new", [(4, 2, 3000, 1), (4, 2, 200, 1), (40, 1, 2500, 2), (4, 4, 900, 70)])
+def test_steps_in_a_graph_and_on_another_stream(hq, hk, past, new, kind):
+    """The calls of a step recorded once and replayed with other tokens, beside the same calls made one by one; two such graphs, whose
+    workspaces are their own, by turns."""
+    torch, ops = torch_ops()
+
+    def setting(seed):
+        st = whole([past, past // 3, 0], [new] * 3, seed, hk, 64, kind, 64)
+        room = st.args(equal=True)
+        wide = torch.cat([room["table"], torch.arange(8, dtype=torch.int32, device="cuda").expand(3, 8) % st.n_pages], dim=1).contiguous()
+        torch.manual_seed(seed)
+        x = [torch.randn(3 * new, h, 64, device="cuda") for h in (hq, hk, hk)]
+        return st.cache, wide, room["past"], x
+
+    def step(cache, table, at, x):
+        q = ops.cache_append(cache, x[1], x[2], table, at, x[0], freqs=freqs)
+        pages = ops.cache_select(q, cache, table, at, 5)
+        o = ops.cache_attend(q, cache, table, at), ops.cache_attend(q, cache, table, at, selected=pages)
+        at.add_(0)
+        return q, pages, *o
+    freqs = freqs_of(64)
+    both = []
+    for seed in (1, 2):
+        a, b = setting(seed), setting(seed)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            first = step(*a)
+            second = step(*b)
+        side.synchronize()
+        for u, w in zip(first, second):
+            assert torch.equal(u, w)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = step(*a)
+        both.append((graph, a, b, got))
+    for turn in range(4):
+        for graph, a, b, _ in both:
+            for u, w in zip(a[3], b[3]):
+                u.normal_()
+                w.copy_(u)
+            graph.replay()
+        for graph, a, b, got in both:
+            for u, w in zip(got, step(*b)):
+                assert torch.equal(u, w), turn
+        torch.cuda.synchronize()
+
+
+def test_refusals_leave_the_device_usable_and_gradients_are_refused():
+    torch, ops = torch_ops()
+    st = whole([40, 9], [1, 1], 1, 2, 64, "bf16", 32)
+    args = st.args(equal=True)
+    q, k = torch.randn(2, 4, 64, device="cuda"), torch.randn(2, 2, 64, device="cuda")
+    want = ops.cache_attend(q, st.cache, **args)
+    wrong = dict(args, past=args["past"].long())
+    for call in (lambda: ops.cache_attend(q[:, :3], st.cache, **args), lambda: ops.cache_attend(q, st.cache, **wrong), lambda: ops.cache_attend(q.half(), st.cache, **args),
+                 lambda: ops.cache_attend(q[..., :63], st.cache, **args), lambda: ops.cache_attend(q, st.cache, window=0, **args),
+                 lambda: ops.cache_attend(q, st.cache, max_len=0, **args), lambda: ops.cache_attend(q, st.cache, scale=float("nan"), **args),
+                 lambda: ops.cache_attend(q, st.cache, selected=torch.zeros(2, 2, 0, dtype=torch.int32, device="cuda"), **args),
+                 lambda: ops.cache_attend(q, st.cache, selected=torch.zeros(2, 4, 3, dtype=torch.int32, device="cuda"), **args),
+                 lambda: ops.cache_attend(q, st.cache, causal=False, window=3, **args), lambda: ops.cache_attend(q.cpu(), st.cache, **args),
+                 lambda: ops.cache_attend(q, st.cache._replace(k=st.cache.k.float()), **args), lambda: ops.cache_attend(q, st.cache._replace(d=32), **args),
+                 lambda: ops.cache_append(st.cache, k, k[:, :1], **args), lambda: ops.cache_append(st.cache, k, k, pairs="thirds", **args),
+                 lambda: ops.cache_append(st.cache, k, k, freqs=torch.ones(33, device="cuda"), **args), lambda: ops.cache_append(st.cache, k.bfloat16(), k, **args),
+                 lambda: ops.cache_append(st.cache, k, k, k_norm=torch.ones(63, device="cuda"), **args), lambda: ops.cache_read(st.cache, n=3, **args),
+                 lambda: ops.cache_select(q, st.cache, count=1, **args), lambda: ops.cache_select(q, st.cache._replace(bounds=None), count=3, **args),
+                 lambda: ops.cache_attend(q.clone().requires_grad_(), st.cache, **args), lambda: ops.cache_append(st.cache, k.clone().requires_grad_(), k, **args),
+                 lambda: ops.cache_append(st.cache, k, k, k_norm=torch.ones(64, device="cuda", requires_grad=True), **args)):
+        with pytest.raises(ev.EvConvError):
+            call()
+    with torch.no_grad():
+        assert torch.equal(ops.cache_attend(q.clone().requires_grad_(), st.cache, **args), want)
+    none = dict(table=args["table"], past=args["past"])
+    assert ops.cache_attend(q[:0], st.cache, **none).shape == (0, 4, 64) and ops.cache_select(q[:0], st.cache, count=3, **none).shape == (0, 2, 3)
+    assert ops.cache_append(st.cache, k[:0], k[:0], q=q[:0], **none).shape == (0, 4, 64) and ops.cache_read(st.cache, n=0, **none)[0].shape == (0, 2, 64)
+    assert torch.equal(ops.cache_attend(q, st.cache, **args), want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_far_apart(dtype, kind):
+    """Weights from 1 down to nothing, maxima that rise and fall along the tokens; and all alike."""
+    torch, ops = torch_ops()
+    for hq, news in ((4, [1, 1]), (4, [90, 40])):
+        st = whole([900, 300], news, 6, 2, 64, kind, 64)
+        t, n = torch.float32 if dtype == "f32" else torch.bfloat16, sum(news)
+        q = torch.from_numpy(20 * st.rng.standard_normal((n, hq, 64))).to(t)
+        got, want, spread = attend_case(st, hq, dtype, q=q)
+        if dtype == "f32":  # a score of s = 160 is off by up to 2^-24 * s * 8 (three parts, 64 terms), and so is the weight's exponent
+            diff = np.abs(got.float().cpu().numpy() - want)
+            assert (diff <= 2.0 ** -13 * spread + 1e-6).all(), (diff / spread).max()
+        else:
+            diff = np.abs(got.float().cpu().numpy() - want)
+            assert (diff <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -13) * spread).all()
+        check_attention(*attend_case(st, hq, dtype, q=q * 0), dtype)

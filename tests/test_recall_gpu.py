@@ -1,0 +1,155 @@
+"""Layers of the memory that look back into a paged cache (memory.py), against their formulas in 64 bits.
+
+Tolerance: that of test_memory_gpu.py, 2^-4 of the norm, whose reasons hold here too: 8-bit rows that round differently are what there is
+to be off by, and a value of 4 bits that rounds to its other neighbour counts as one of them."""
+import numpy as np
+import pytest
+
+import ops_ref
+
+pytestmark = pytest.mark.gpu
+
+
+def make(**kw):
+    import torch
+    from paper_2303_04670_amd.memory import Memory
+    torch.manual_seed(1)
+    return torch, Memory(**{**dict(dim=96, n_streams=4, n_out=11, dtype=torch.float32, seed=3, recall=(0, 1), recall_windows=200, longest=300), **kw})
+
+
+def held(x, kind):
+    import torch
+    if kind == "bf16":
+        return torch.from_numpy(np.asarray(x, np.float32)).bfloat16().double().numpy()
+    return ops_ref.fp4_values(*ops_ref.fp4_rows(x))
+
+
+def reference(memory, x, spans, kind="fp4", pages=None):
+    """Outputs of whole streams' features; spans: (first, windows)."""
+    hk, hv, d = memory.heads_k, memory.heads_v, memory.d_v
+    product = lambda a, w, **kw: ops_ref.quant_matmul(*ops_ref.quantize_rows(a), *ops_ref.quantize_rows(w), **kw)
+    _, h = ops_ref.block_norm(x, pre_norm=True, pre_weight=memory.weights[0]["pre_norm"])
+    freqs = memory.freqs.cpu().numpy()
+    for i, w in enumerate(memory.weights[:-1]):
+        p = product(h, w["w_in"])
+        n, o = len(p), np.zeros((len(p), hv, d))
+        cut = np.cumsum([0, hv * d, hk * d, hk * d, hv * d])
+        q, k, v, z = (p[:, a:b] for a, b in zip(cut, cut[1:]))
+        for first, count in spans:
+            at, t = slice(first, first + count), np.arange(count)
+            turn = lambda y, heads, norm: ops_ref.head_rows(y[at].reshape(count, heads, d), w[norm], 1e-6, freqs, "halves", t)
+            qs, raw = turn(q, hv, "q_norm"), turn(k, hk, "k_norm")
+            ks, vs = held(raw, kind), held(v[at].reshape(count, hk, d), kind)
+            for head in range(hv):
+                g = head // (hv // hk)
+                seen = (t <= t[:, None]) & (t > t[:, None] - memory.recall_windows)
+                if pages:
+                    seen = np.zeros((count, count), bool)
+                    low = held(raw, "bf16")[:, g]
+                    for j in range(count):
+                        score = []
+                        for page in range(j // 64 + 1):
+                            mine = low[page * 64:min(page * 64 + 64, count)]
+                            each = qs[j, g * (hv // hk):(g + 1) * (hv // hk)]
+                            score.append(np.maximum(each * mine.min(0), each * mine.max(0)).sum(-1).max())
+                        for page in ops_ref.choose(np.float32(score), pages, 1, 1):
+                            if page >= 0:
+                                seen[j, page * 64:min(page * 64 + 64, j + 1)] = True
+                o[at, head], _ = ops_ref.attend(qs[:, head], ks[:, g], vs[:, g], d ** -0.5, seen)
+        _, g = ops_ref.block_norm(None, o.reshape(n, -1), z, post_weight=w["head_norm"], gate_act="silu", group=d)
+        following = memory.weights[i + 1]
+        x, h = ops_ref.block_norm(x, product(g, w["w_out"]), post_weight=w["post_norm"], res_scale=w["res_scale"], pre_norm=True,
+                                  pre_weight=following["pre_norm"] if "pre_norm" in following else following["norm"])
+    return product(h, memory.weights[-1]["head"], bias=memory.weights[-1]["bias"])
+
+
+def near(got, want):
+    got = got.detach().double().cpu().numpy()
+    assert got.shape == np.shape(want) and np.isfinite(got).all()
+    assert np.linalg.norm(got - want) <= 2.0 ** -4 * np.linalg.norm(want), np.linalg.norm(got - want) / np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("sizes", [{}, dict(recall_kind="bf16", d_v=40, heads_v=3, heads_k=1), dict(recall_windows=30), dict(recall_windows=256, recall_pages=3)])
+def test_windows_one_by_one_and_at_once(sizes):
+    torch, memory = make(**sizes)
+    _, other = make(**sizes)
+    lens = [230, 0, 1, 65]
+    first = np.concatenate([[0], np.cumsum(lens)])
+    x = torch.randn(sum(lens), 96, device="cuda")
+    want = reference(memory, x.cpu().numpy(), [(int(a), n) for a, n in zip(first, lens)], sizes.get("recall_kind", "fp4"), sizes.get("recall_pages"))
+    near(memory(x, seq_offsets=torch.tensor(first, dtype=torch.int32, device="cuda")), want)
+    assert memory.past.tolist() == lens
+    if sizes.get("recall_pages"):
+        return  # (which pages are taken may hang on an 8-bit rounding)
+    one = torch.zeros(sum(lens), 11, device="cuda")
+    for i in range(max(lens)):
+        live = [s for s in range(4) if lens[s] > i]
+        rows = torch.tensor([int(first[s]) + i for s in live], device="cuda")
+        one[rows] = other(x[rows], slots=torch.tensor(live, dtype=torch.int32, device="cuda"))
+    near(one, want)
+    assert other.past.tolist() == lens
+
+
+def test_pages_go_round():
+    """A stream that is longer than all its pages sees its last windows only."""
+    torch, memory = make(recall_windows=64, longest=100, n_streams=2)
+    assert memory.n_pages == 2 * 4
+    x = torch.randn(2 * 500, 96, device="cuda")
+    want = reference(memory, x.cpu().numpy(), [(0, 500), (500, 500)])
+    got = []
+    for at in range(0, 500, 50):
+        rows = torch.cat([x[at:at + 50], x[500 + at:550 + at]])
+        got.append(memory(rows, seq_offsets=torch.tensor([0, 50, 100], dtype=torch.int32, device="cuda")).view(2, 50, 11))
+    near(torch.cat(got, dim=1).reshape(1000, 11), want)
+
+
+def test_layers_of_both_kinds_forget_and_mind_their_streams():
+    torch, memory = make(recall=(1,), layers=3)
+    _, other = make(recall=(1,), layers=3)
+    for i in range(5):
+        x = torch.randn(4, 96, device="cuda")
+        a, b = memory(x), other(x)
+        assert torch.equal(a, b)
+    memory.forget([2, -1])
+    assert memory.past.tolist() == [5, 5, 0, 5]
+    x = torch.randn(4, 96, device="cuda")
+    a = memory(x)
+    assert torch.equal(a[[0, 1, 3]], other(x)[[0, 1, 3]])
+    _, fresh = make(recall=(1,), layers=3)
+    near(a[2:3], fresh(x[2:3], slots=torch.tensor([2], dtype=torch.int32, device="cuda")).double().cpu().numpy())
+    before = memory.past.tolist()
+    memory(x[:1], slots=torch.tensor([-1], dtype=torch.int32, device="cuda"))
+    assert memory.past.tolist() == before
+
+
+def test_a_refused_window_leaves_everything():
+    torch, memory = make()
+    from paper_2303_04670_amd import evconv as ev
+    x = torch.randn(4, 96, device="cuda")
+    memory(x)
+    state = [t.clone() for layer in memory.layers for t in layer.cache[:5] if t is not None] + [memory.past.clone()]
+    offsets = torch.tensor([0, 301], dtype=torch.int32, device="cuda")
+    for call in (lambda: memory(x.bfloat16()), lambda: memory(x[:, :95]), lambda: memory(x[:3]), lambda: memory(torch.zeros(301, 96, device="cuda"), seq_offsets=offsets),
+                 lambda: memory(x, slots=torch.arange(3, dtype=torch.int32, device="cuda")), lambda: make(recall=(2,))):
+        with pytest.raises(ev.EvConvError):
+            call()
+    for a, b in zip(state, [t for layer in memory.layers for t in layer.cache[:5] if t is not None] + [memory.past]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_a_window_in_a_graph():
+    torch, memory = make(recall=(0,), dtype=__import__("torch").bfloat16)
+    _, other = make(recall=(0,), dtype=torch.bfloat16)
+    x = torch.randn(4, 96, device="cuda").bfloat16()
+    memory(x)
+    other(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = memory(x)
+    for _ in range(70):
+        x.normal_()
+        graph.replay()
+        assert torch.equal(y, other(x))
+    torch.cuda.synchronize()
+    assert memory.past.tolist() == other.past.tolist() == [71] * 4
