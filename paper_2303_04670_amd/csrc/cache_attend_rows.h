@@ -62,7 +62,7 @@ __device__ __forceinline__ int fate_of(int lo, int hi, int base, int split, int 
 
 template <bool FP4, int GROUPS, bool BF16, int DP, bool LIST>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF16)) void attend_rows(AttendParams p, int64_t unit0) {
-  constexpr int PARTS = BF16 ? 1 : 3, STEPS = DP / 32, VT = DP / 16;
+  constexpr int PARTS = BF16 ? 1 : 3, WPARTS = BF16 ? 2 : 3, STEPS = DP / 32, VT = DP / 16;
   constexpr int MINE = 8 * GROUPS, TOK = 4 * MINE;  // tokens of a lane's weights, of a tile (which lies in one page)
   constexpr int KW = FP4 ? STEPS : 4 * STEPS;  // 32-bit words of a lane's part of a key
   __shared__ float s_o[4][16][DP + 4];
@@ -300,8 +300,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF
           w[j] = whole || (t >= lo && t < hi) ? w[j] * scale : 0.0f;
         }
       }
-      b16x8 weights[PARTS];
-      split8<PARTS>(w, weights);
+      b16x8 weights[WPARTS];  // (bf16 calls too: the second half of their bits costs nothing beside the cache's bytes)
+      split8<WPARTS>(w, weights);
 #pragma unroll
       for (int i = 0; i < VT; ++i) {
         b16x8 v;
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : (DP <= 64 ? 3 : 2) + (FP4 && BF
           if (!whole) v = keep_range(v, lo_min - first, hi_max - first);
         }
 #pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, weights[part], o[i], 0, 0, 0);
+        for (int part = WPARTS - 1; part >= 0; --part) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, weights[part], o[i], 0, 0, 0);
       }
     }
     if (next < end) load_v();

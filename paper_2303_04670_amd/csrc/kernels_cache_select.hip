@@ -14,6 +14,7 @@ namespace {
 constexpr unsigned kForced = 0xffffffffu, kNotANumber = 0xfffffffeu;
 constexpr int kHeads = 16;  // query heads whose values are in LDS at once
 constexpr int kHeld = 4;    // pages that a lane holds
+constexpr int kRounds = 4;  // of a workgroup
 
 // Unsigned numbers in the order of the floats, all above 0: that is the mark of a page that cannot be chosen.
 __device__ __forceinline__ unsigned key_of(float score) {
@@ -62,95 +63,131 @@ __device__ __forceinline__ double pages_sum(const double (&v)[4], int lane) {
   return s;
 }
 
+// A workgroup goes over kRounds times 4 kHeld GROUPS pages: its start (whose the query is, its values as 64-bit numbers) costs as much as
+// two rounds, and the next round's bounds are on their way while one is added up.
 template <bool BF16, int DP>
-__global__ __launch_bounds__(256) void score_pages(SelectParams p, int blocks, int64_t block0) {
-  constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32, GROUPS = 64 / LANES;
+__global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks, int64_t block0) {
+  constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32, GROUPS = 64 / LANES, ROUND = 4 * kHeld * GROUPS;
   __shared__ double s_q[kHeads][2][DP];  // min(q, 0), max(q, 0)
   const evconv_select_args& a = p.a;
   const evconv_cache& c = a.cache;
   const int64_t unit = (block0 + blockIdx.x) / blocks, token = unit / c.heads;
   const int head = (int)(unit - token * c.heads);
   const Query query = find_query(p, token);
-  const int first_page = (int)(block0 + blockIdx.x - unit * blocks) * (4 * kHeld * GROUPS);
+  const int64_t first_page = (block0 + blockIdx.x - unit * blocks) * (kRounds * ROUND);
   if (query.seq < 0 || first_page > query.last) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane / LANES, ch = lane % LANES * 8;
-  // ---- the bounds
-  int at[kHeld];
-  bool there[kHeld];
-  double lo[kHeld][8], hi[kHeld][8];
+  const int rounds = (int)min((int64_t)kRounds, (query.last - first_page) / ROUND + 1);
+  auto page_number = [&](int round, int i) __attribute__((always_inline)) { return first_page + round * ROUND + (wave * kHeld + i) * GROUPS + group; };
+  int held[kHeld];         // pages of the round whose bounds are requested next
+  bool there[kHeld];       // whether those of the round that was requested are there
+  uint4 low[kHeld], high[kHeld];
+  auto look = [&](int round) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    at[i] = first_page + (wave * kHeld + i) * GROUPS + group;
-    const int page = at[i] <= query.last ? page_of(c, a.tokens, query.seq, at[i]) : -1;
-    there[i] = page >= 0;
-    float l[8], h[8];
-    const int64_t row = ((int64_t)max(page, 0) * c.heads + head) * 2 * DP;
-    load_run<true, 8, true>(c.bounds, row + ch, DP - ch, l);
-    load_run<true, 8, true>(c.bounds, row + DP + ch, DP - ch, h);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) lo[i][j] = (double)l[j], hi[i][j] = (double)h[j];
-  }
-  double best = -INFINITY;  // of the page whose sums come to this lane
-  bool bad = false;
-  for (int h0 = 0; h0 < p.share; h0 += kHeads) {
-    const int heads = min(p.share - h0, kHeads);
-    __syncthreads();
-    for (int i = threadIdx.x; i < heads * DP; i += 256) {
-      const int h = i / DP, x = i % DP;
-      const int64_t from = token * a.q.token_stride + (int64_t)(head * p.share + h0 + h) * a.q.head_stride + x;
-      const double v = x < c.d ? (double)load_one<BF16>(a.q.data, from) : 0.0;
-      s_q[h][0][x] = v > 0.0 ? 0.0 : v;  // (a NaN is in both)
-      s_q[h][1][x] = v < 0.0 ? 0.0 : v;
+    for (int i = 0; i < kHeld; ++i) {
+      const int64_t at = page_number(round, i);
+      held[i] = at <= query.last ? page_of(c, a.tokens, query.seq, at) : -1;
     }
-    __syncthreads();
-    for (int h = 0; h < heads; ++h) {
-      double sum[kHeld];
+  };
+  auto request = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) sum[i] = 0.0;
-      if (ch < DP)
+    for (int i = 0; i < kHeld; ++i) {
+      there[i] = held[i] >= 0;
+      const uint16_t* const row = (const uint16_t*)c.bounds + ((int64_t)max(held[i], 0) * c.heads + head) * 2 * DP + min(ch, DP - 8);
+      low[i] = *(const uint4*)row;
+      high[i] = *(const uint4*)(row + DP);
+    }
+  };
+  look(0);
+  request();
+  if (rounds > 1) look(1);
+  for (int round = 0; round < rounds; ++round) {
+    double lo[kHeld][8], hi[kHeld][8];
+    bool is_there[kHeld];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const double neg = s_q[h][0][ch + j], pos = s_q[h][1][ch + j];
+    for (int i = 0; i < kHeld; ++i) {
+      const unsigned l[4] = {low[i].x, low[i].y, low[i].z, low[i].w}, h[4] = {high[i].x, high[i].y, high[i].z, high[i].w};
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i) sum[i] = fma(neg, lo[i][j], fma(pos, hi[i][j], sum[i]));
+      for (int j = 0; j < 8; ++j) {
+        lo[i][j] = (double)(j % 2 ? bf16_high(l[j / 2]) : bf16_low(l[j / 2]));
+        hi[i][j] = (double)(j % 2 ? bf16_high(h[j / 2]) : bf16_low(h[j / 2]));
+      }
+      is_there[i] = there[i];
+    }
+    if (round + 1 < rounds) {
+      request();
+      if (round + 2 < rounds) look(round + 2);
+    }
+    double best = -INFINITY;  // of the page whose sums come to this lane
+    bool bad = false;
+    for (int h0 = 0; h0 < p.share; h0 += kHeads) {
+      const int heads = min(p.share - h0, kHeads);
+      if (round == 0 || p.share > kHeads) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < heads * DP; i += 256) {
+          const int h = i / DP, x = i % DP;
+          const int64_t from = token * a.q.token_stride + (int64_t)(head * p.share + h0 + h) * a.q.head_stride + x;
+          const double v = x < c.d ? (double)load_one<BF16>(a.q.data, from) : 0.0;
+          s_q[h][0][x] = v > 0.0 ? 0.0 : v;  // (a NaN is in both)
+          s_q[h][1][x] = v < 0.0 ? 0.0 : v;
         }
-      const double score = pages_sum<LANES>(sum, lane);
-      bad = bad || score != score;
-      best = fmax(best, score);
+        __syncthreads();
+      }
+      for (int h = 0; h < heads; ++h) {
+        double sum[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) sum[i] = 0.0;
+        if (ch < DP)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const double neg = s_q[h][0][ch + j], pos = s_q[h][1][ch + j];
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) sum[i] = fma(neg, lo[i][j], fma(pos, hi[i][j], sum[i]));
+          }
+        const double score = pages_sum<LANES>(sum, lane);
+        bad = bad || score != score;
+        best = fmax(best, score);
+      }
     }
-  }
-  if (lane % LANES < 4) {
-    const int i = 2 * (lane & 1) + (lane >> 1 & 1), page = i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3];
-    const bool is_there = i == 0 ? there[0] : i == 1 ? there[1] : i == 2 ? there[2] : there[3];
-    if (page <= query.last) {
-      const bool forced = page < a.first || page > query.last - a.last;
-      p.score[unit * p.pages + page] = !is_there ? 0u : forced ? kForced : bad ? kNotANumber : key_of((float)best);
+    if (lane % LANES < 4) {
+      const int i = 2 * (lane & 1) + (lane >> 1 & 1);
+      const int64_t page = page_number(round, i);
+      const bool here = i == 0 ? is_there[0] : i == 1 ? is_there[1] : i == 2 ? is_there[2] : is_there[3];
+      if (page <= query.last) {
+        const bool forced = page < a.first || page > query.last - a.last;
+        p.score[unit * p.pages + page] = !here ? 0u : forced ? kForced : bad ? kNotANumber : key_of((float)best);
+      }
     }
   }
 }
 
-// Sum over the threads of a workgroup of what stands before each of them; `all`: of all.
-__device__ __forceinline__ int sum_before(int v, int* s_wave, int* all) {
+// Sums over the threads of a workgroup of what stands before each of them, of two numbers at once; `all`: of all.
+struct Two {
+  int a, b;
+};
+__device__ __forceinline__ Two sums_before(Two v, Two* s_wave, Two* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int before = v;
+  Two before = v;
+#pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int u = __shfl_up(before, d);
-    if (lane >= d) before += u;
+    const int a = __shfl_up(before.a, d), b = __shfl_up(before.b, d);
+    if (lane >= d) before.a += a, before.b += b;
   }
-  __syncthreads();
+  __syncthreads();  // (the last sums have been read)
   if (lane == 63) s_wave[wave] = before;
   __syncthreads();
-  int others = 0, total = 0;
+  Two others{0, 0};
+  *all = Two{0, 0};
   for (int w = 0; w < waves; ++w) {
-    if (w < wave) others += s_wave[w];
-    total += s_wave[w];
+    const Two x = s_wave[w];
+    if (w < wave) others.a += x.a, others.b += x.b;
+    all->a += x.a, all->b += x.b;
   }
-  *all = total;
-  return others + before - v;
+  return {others.a + before.a - v.a, others.b + before.b - v.b};
 }
-
 // Least and largest of a value over the threads of a workgroup.
 __device__ __forceinline__ void range_of(unsigned& lo, unsigned& hi, unsigned (*s_range)[2]) {
+#pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     lo = min(lo, (unsigned)__shfl_xor((int)lo, d));
     hi = max(hi, (unsigned)__shfl_xor((int)hi, d));
@@ -163,11 +200,14 @@ __device__ __forceinline__ void range_of(unsigned& lo, unsigned& hi, unsigned (*
 
 // The `count` highest keys of a row, the lower index first among equals: the key of the last one, by counting the keys in equal parts of the
 // range that it is in, until a part is one key; then all above it and the first of those that equal it, in the order of their pages.  A
-// workgroup to a row, a thread to neighbouring pages.  (Parts of the range that the keys have, not digits of them: scores of one sequence share
-// their upper digits, and counters that all threads want are counted one after the other: 59 us against 12 for 15626 pages.)
+// workgroup to a row, a thread to neighbouring pages, whose keys (HELD: up to 16) stay in its registers.  (Parts of the range that the keys
+// have, not digits of them: scores of one sequence share their upper digits, and counters that all threads want are counted one after the
+// other: 59 us against SSS for 15626 pages.)
+template <bool HELD>
 __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t unit0) {
   constexpr int kParts = 2048;
-  __shared__ int s_parts[kParts], s_wave[16], s_found[2];
+  __shared__ int s_parts[kParts], s_found[2];
+  __shared__ Two s_wave[16];
   __shared__ unsigned s_range[16][2];
   const evconv_select_args& a = p.a;
   const int64_t unit = unit0 + blockIdx.x, token = unit / a.cache.heads;
@@ -176,29 +216,38 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
   const int n = (int)query.last + 1, threads = blockDim.x, t = threadIdx.x;
   const unsigned* const key = p.score + unit * p.pages;
   int* const out = a.selected + unit * a.count;
-  const int per = ((n + threads - 1) / threads + 3) / 4 * 4, from = min(t * per, n), to = min(from + per, n);
+  const int per = HELD ? 4 * ((n + 4 * threads - 1) / (4 * threads)) : ((n + threads - 1) / threads + 3) / 4 * 4;
+  const int from = min(t * per, n), to = min(from + per, n);
+  uint4 held[4];
+  if constexpr (HELD)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) held[i] = from + 4 * i < to ? *(const uint4*)(key + from + 4 * i) : make_uint4(0, 0, 0, 0);
+  auto four = [&](int i, const uint4& u, auto&& what) __attribute__((always_inline)) {
+    if (i < to) what(i, u.x);
+    if (i + 1 < to) what(i + 1, u.y);
+    if (i + 2 < to) what(i + 2, u.z);
+    if (i + 3 < to) what(i + 3, u.w);
+  };
   auto each = [&](auto&& what) __attribute__((always_inline)) {  // of this thread's pages (rows are whole fours)
-    for (int i = from; i < to; i += 4) {
-      const uint4 u = *(const uint4*)(key + i);
-      what(i, u.x);
-      if (i + 1 < to) what(i + 1, u.y);
-      if (i + 2 < to) what(i + 2, u.z);
-      if (i + 3 < to) what(i + 3, u.w);
+    if constexpr (HELD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) four(from + 4 * i, held[i], what);
+    } else {
+      for (int i = from; i < to; i += 4) four(i, *(const uint4*)(key + i), what);
     }
   };
-  int mine = 0, forced = 0, some, need;
+  Two mine{0, 0}, all;  // pages that can be chosen, those that have to be
   unsigned lo = kForced, hi = 0;
   each([&](int, unsigned k) {
-    mine += k != 0;
-    forced += k == kForced;
+    mine.a += k != 0;
+    mine.b += k == kForced;
     if (k != 0 && k != kForced) lo = min(lo, k), hi = max(hi, k);
   });
-  sum_before(mine, s_wave, &some);
+  sums_before(mine, s_wave, &all);
   unsigned edge = 0;  // key of the last one that is chosen
   int equal = 0;      // how many with it
-  if (some > a.count) {
-    sum_before(forced, s_wave, &need);
-    need = a.count - need;
+  if (all.a > a.count) {
+    int need = a.count - all.b;
     range_of(lo, hi, s_range);
     edge = kForced;  // (none but them)
     while (need > 0) {
@@ -211,10 +260,10 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
       __syncthreads();
       // from the top: the part where the sum reaches `need`
       const int share = (parts + threads - 1) / threads, top = parts - 1 - t * share;
-      int here = 0, all;
-      for (int i = 0; i < share; ++i) here += top - i >= 0 ? s_parts[top - i] : 0;
-      int before = sum_before(here, s_wave, &all);
-      if (before < need && before + here >= need)
+      Two here{0, 0};
+      for (int i = 0; i < share; ++i) here.a += top - i >= 0 ? s_parts[top - i] : 0;
+      int before = sums_before(here, s_wave, &all).a;
+      if (before < need && before + here.a >= need)
         for (int i = 0; i < share; ++i) {
           const int c = s_parts[top - i];
           if (before + c >= need) {
@@ -238,20 +287,19 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
     if (edge == kForced) equal = a.count;
   }
   // ---- written in the order of the pages
-  int above = 0, same = 0;
+  Two found{0, 0};  // above it, as it
   each([&](int, unsigned k) {
-    above += k > edge;
-    same += k == edge && edge != 0;
+    found.a += k > edge;
+    found.b += k == edge && edge != 0;
   });
-  int all_above, all_same;
-  int above_before = sum_before(above, s_wave, &all_above), same_before = sum_before(same, s_wave, &all_same);
+  Two before = sums_before(found, s_wave, &all);
   each([&](int i, unsigned k) {
-    const bool is_above = k > edge, is_same = k == edge && edge != 0;
-    if (is_above || (is_same && same_before < equal)) out[above_before + min(same_before, equal)] = i;
-    above_before += is_above;
-    same_before += is_same;
+    const bool above = k > edge, same = k == edge && edge != 0;
+    if (above || (same && before.b < equal)) out[before.a + min(before.b, equal)] = i;
+    before.a += above;
+    before.b += same;
   });
-  for (int i = all_above + min(all_same, equal) + t; i < a.count; i += threads) out[i] = -1;
+  for (int i = all.a + min(all.b, equal) + t; i < a.count; i += threads) out[i] = -1;
 }
 
 template <bool BF16>
@@ -266,7 +314,7 @@ void start_scores(const SelectParams& p, unsigned grid, int blocks, int64_t at, 
   }
 }
 
-int pages_of_a_workgroup(int dp) { return 4 * kHeld * (dp <= 32 ? 16 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2); }
+int pages_of_a_workgroup(int dp) { return kRounds * 4 * kHeld * (dp <= 32 ? 16 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2); }
 
 }  // namespace
 
@@ -292,9 +340,14 @@ void launch_select(const SelectParams& p, hipStream_t s) {
     if (p.a.dtype == EVCONV_BF16) start_scores<true>(p, grid, blocks, at, s);
     else start_scores<false>(p, grid, blocks, at, s);
   }
-  const int threads = p.pages <= 1024 ? 256 : 1024;
+  // (few threads meet sooner; 2048 pages: 256 CCC us, 1024 DDD)
+  const int threads = p.pages <= 4096 ? 256 : 1024;
   const int64_t rows = kMostThreads / threads;
-  for (int64_t at = 0; at < units; at += rows) choose_pages<<<(unsigned)std::min(rows, units - at), threads, 0, s>>>(p, at);
+  for (int64_t at = 0; at < units; at += rows) {
+    const unsigned grid = (unsigned)std::min(rows, units - at);
+    if (p.pages <= 16 * threads) choose_pages<true><<<grid, threads, 0, s>>>(p, at);
+    else choose_pages<false><<<grid, threads, 0, s>>>(p, at);
+  }
 }
 
 }  // namespace evk
