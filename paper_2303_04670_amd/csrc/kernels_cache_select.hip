@@ -14,7 +14,7 @@ namespace {
 constexpr unsigned kForced = 0xffffffffu, kNotANumber = 0xfffffffeu;
 constexpr int kHeads = 16;  // query heads whose values are in LDS at once
 constexpr int kHeld = 4;    // pages that a lane holds
-constexpr int kRounds = 4;  // of a workgroup
+constexpr int kRounds = 2;  // of a workgroup
 
 // Unsigned numbers in the order of the floats, all above 0: that is the mark of a page that cannot be chosen.
 __device__ __forceinline__ unsigned key_of(float score) {
@@ -63,12 +63,14 @@ __device__ __forceinline__ double pages_sum(const double (&v)[4], int lane) {
   return s;
 }
 
-// A workgroup goes over kRounds times 4 kHeld GROUPS pages: its start (whose the query is, its values as 64-bit numbers) costs as much as
-// two rounds, and the next round's bounds are on their way while one is added up.
+// A workgroup goes over kRounds times 4 kHeld GROUPS pages: its start (whose the query is, its values as 64-bit numbers) costs as much as a
+// round, and the next one's bounds are on their way while one is added up.  us for 16 streams of up to 2048 pages, 8 key heads / one of 15626,
+// 4: 1 round 25.6 / 13.2, 2 26.9 / 12.4, 4 28.2 / 15.6.  Bound by 64-bit instructions and the start: the bounds are 60 MB / 32 MB.
 template <bool BF16, int DP>
 __global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks, int64_t block0) {
   constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32, GROUPS = 64 / LANES, ROUND = 4 * kHeld * GROUPS;
-  __shared__ double s_q[kHeads][2][DP];  // min(q, 0), max(q, 0)
+  // min(q, 0), max(q, 0): of a lane's eight channels two at a time, neighbouring lanes next to each other
+  __shared__ double2 s_q[kHeads][2][4][DP / 8];
   const evconv_select_args& a = p.a;
   const evconv_cache& c = a.cache;
   const int64_t unit = (block0 + blockIdx.x) / blocks, token = unit / c.heads;
@@ -128,8 +130,8 @@ __global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks
           const int h = i / DP, x = i % DP;
           const int64_t from = token * a.q.token_stride + (int64_t)(head * p.share + h0 + h) * a.q.head_stride + x;
           const double v = x < c.d ? (double)load_one<BF16>(a.q.data, from) : 0.0;
-          s_q[h][0][x] = v > 0.0 ? 0.0 : v;  // (a NaN is in both)
-          s_q[h][1][x] = v < 0.0 ? 0.0 : v;
+          ((double*)&s_q[h][0][x % 8 / 2][x / 8])[x % 2] = v > 0.0 ? 0.0 : v;  // (a NaN is in both)
+          ((double*)&s_q[h][1][x % 8 / 2][x / 8])[x % 2] = v < 0.0 ? 0.0 : v;
         }
         __syncthreads();
       }
@@ -139,10 +141,13 @@ __global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks
         for (int i = 0; i < kHeld; ++i) sum[i] = 0.0;
         if (ch < DP)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const double neg = s_q[h][0][ch + j], pos = s_q[h][1][ch + j];
+          for (int j = 0; j < 4; ++j) {
+            const double2 neg = s_q[h][0][j][ch / 8], pos = s_q[h][1][j][ch / 8];
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) sum[i] = fma(neg, lo[i][j], fma(pos, hi[i][j], sum[i]));
+            for (int i = 0; i < kHeld; ++i) {
+              sum[i] = fma(neg.x, lo[i][2 * j], fma(pos.x, hi[i][2 * j], sum[i]));
+              sum[i] = fma(neg.y, lo[i][2 * j + 1], fma(pos.y, hi[i][2 * j + 1], sum[i]));
+            }
           }
         const double score = pages_sum<LANES>(sum, lane);
         bad = bad || score != score;
@@ -202,7 +207,7 @@ __device__ __forceinline__ void range_of(unsigned& lo, unsigned& hi, unsigned (*
 // range that it is in, until a part is one key; then all above it and the first of those that equal it, in the order of their pages.  A
 // workgroup to a row, a thread to neighbouring pages, whose keys (HELD: up to 16) stay in its registers.  (Parts of the range that the keys
 // have, not digits of them: scores of one sequence share their upper digits, and counters that all threads want are counted one after the
-// other: 59 us against SSS for 15626 pages.)
+// other: 59 us against 14 for 15626 pages.)
 template <bool HELD>
 __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t unit0) {
   constexpr int kParts = 2048;
@@ -340,7 +345,7 @@ void launch_select(const SelectParams& p, hipStream_t s) {
     if (p.a.dtype == EVCONV_BF16) start_scores<true>(p, grid, blocks, at, s);
     else start_scores<false>(p, grid, blocks, at, s);
   }
-  // (few threads meet sooner; 2048 pages: 256 CCC us, 1024 DDD)
+  // (2048 pages take 10.8 us with 256 threads, 10.3 with 1024: the barriers; the fewer leave room for other rows)
   const int threads = p.pages <= 4096 ? 256 : 1024;
   const int64_t rows = kMostThreads / threads;
   for (int64_t at = 0; at < units; at += rows) {
