@@ -180,9 +180,9 @@ evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* hip_strea
  *                       the nearest of 6 x / m (each operation rounded to fp32), ties to the even code
  *   bounds              bf16 [n_pages][heads][2][dp]: least and largest of bf16(k) per channel over what was appended
  *                       since the page's first token; or NULL (no evconv_cache_select then)
- * A key row with a value that is not finite (in bf16) makes what looks at its token NaN; so does a value row, whose
- * token's key is stored as NaN for it (v itself holds finite values only: one that is not would reach queries that do not see
- * it).  Other tokens and queries are as without it. */
+ * A key row with a value that is not finite (in bf16: 3.39e38 and more too) makes what looks at its token NaN; so does a value row.  In
+ * 4 bits its scale is NaN; in bf16 the row of the token's key is, also for its value (v itself holds finite values only: one that is not
+ * would reach queries that do not see it).  Other tokens and queries are as without it. */
 typedef enum { EVCONV_CACHE_BF16 = 0, EVCONV_CACHE_FP4 = 1 } evconv_cache_kind;
 
 typedef struct {
@@ -210,7 +210,7 @@ typedef struct {
 
 /* Per head: norm (q_norm, k_norm: weights, NULL: none): x / sqrt(mean(x^2) + eps) * weight, the sum in 64 bits; then the
  * rotation (freqs): pairs (a, b) of the first `rot` channels become (a cos - b sin, b cos + a sin) of the angle position *
- * freqs[i], taken in 64 bits; all else in fp32.  k and v then go to the cache, q to q_out (rounded once; may be q). */
+ * freqs[i], taken in 64 bits (one of 2^45 and more turns nothing); all else in fp32.  k and v then go to the cache, q to q_out (rounded once; may be q). */
 typedef enum { EVCONV_PAIRS_HALVES = 0, EVCONV_PAIRS_NEIGHBOURS = 1 } evconv_pairs; /* (i, i + rot / 2) or (2 i, 2 i + 1) */
 
 typedef struct {
@@ -247,7 +247,9 @@ evconv_status evconv_cache_read(const evconv_read_args* args, void* hip_stream);
  * sees none gets zeros.  Query head h uses key head h / (heads_q / cache.heads).  Seen are, of the query's sequence, tokens 0 .. its own
  * position (causal: of the last `window` ones of them), or all past[s] (else); of those the ones in chosen pages, if `selected`
  * is given.  Products with bf16 queries are exact; fp32 queries and the weights of fp32 calls enter them as three bf16 parts
- * (24 bits), the weights of bf16 calls rounded to bf16, relative to the row's largest. */
+ * (24 bits); the weights of bf16 calls as two (16 bits) where a sequence has up to 16 tokens x query heads of a key head, otherwise rounded
+ * to bf16, which is a rounding of the output's own size.  Weights go up to 2^8, and are divided by their sum last: values whose 2^8-fold sum is
+ * beyond fp32 are too large.  A finite query value of 3.39e38 and more counts as infinite. */
 typedef struct {
   int32_t abi_version;
   int32_t dtype;    /* of q and o: EVCONV_F32 or EVCONV_BF16 */
@@ -288,6 +290,7 @@ typedef struct {
   int32_t* selected; /* [n_tokens][cache.heads][count] */
 } evconv_select_args;
 
+/* Four bytes for every query, key head and page of max_len. */
 evconv_status evconv_cache_select_workspace(const evconv_select_args* args, size_t* bytes);
 evconv_status evconv_cache_select(const evconv_select_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -7,9 +7,11 @@
 namespace evk {
 namespace {
 
-// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: a workgroup to a row, or
-// (many tokens, of which most may have one) to a token.  Which stretches a row has follows from what it sees; a row with one was written by the kernel itself.
-template <bool BF16>
+// What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: T threads to a row (many stretches: a workgroup; few: a
+// wave, which meets no barrier; 8192 rows of 8 stretches 24 us by workgroups, 14 by waves), `groups` workgroups to a token's heads (many
+// tokens, of which most may have one stretch: one).  Which stretches a row has follows from what it sees; a row with one was written by the
+// kernel itself.
+template <bool BF16, int T>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p, int groups, int64_t block0) {
   __shared__ __align__(16) float s_sum[1024];
   __shared__ float s_total[256];
@@ -26,10 +28,17 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int groups, i
   seen_by(p, past, within, lo, hi);
   if (!a.selected && hi - lo <= 1) return;  // (no stretch, or one)
   const int64_t rows = tk.n_tokens * a.heads_q;
-  const int lane = threadIdx.x & 63;
+  constexpr int ROWS = 256 / T;
+  const int lane = threadIdx.x & 63, t = threadIdx.x % T;
+  float* const sums = s_sum + threadIdx.x / T * 4 * T;
+  float* const totals = s_total + threadIdx.x / T * T;
+  auto turn = [&]() __attribute__((always_inline)) {
+    if constexpr (T == 64) lds_turn();
+    else __syncthreads();
+  };
   // four channels to a thread, the rest of the threads to other stretches
-  const int quads = p.dp / 4, beside = 256 / quads, mine = threadIdx.x / quads, ch = threadIdx.x % quads * 4, c = threadIdx.x;
-  for (int head = (int)(block % groups); head < a.heads_q; head += groups) {
+  const int quads = p.dp / 4, beside = T / quads, mine = t / quads, ch = t % quads * 4;
+  for (int head = (int)(block % groups) * ROWS + threadIdx.x / T; head < a.heads_q; head += groups * ROWS) {
     const int64_t row = token * a.heads_q + head;
     int s0 = 0, s1 = p.rows.splits - 1;
     if (!a.selected) {
@@ -58,18 +67,26 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p, int groups, i
         sum += factor * *(const f32x4*)(p.part + at * p.dp + ch);
       }
     }
-    __syncthreads();  // (the last head's sums have been read)
-    *(f32x4*)&s_sum[4 * threadIdx.x] = sum;
-    s_total[threadIdx.x] = total;
-    __syncthreads();
-    if (c >= a.cache.d) continue;
-    float o = 0.0f, all = 0.0f;
-    for (int i = 0; i < beside; ++i) {
-      o += s_sum[i * p.dp + c];
-      all += s_total[i * quads];
+    turn();  // (the last head's sums have been read)
+    *(f32x4*)&sums[4 * t] = sum;
+    totals[t] = total;
+    turn();
+    for (int c = t; c < a.cache.d; c += T) {
+      float o = 0.0f, all = 0.0f;
+      for (int i = 0; i < beside; ++i) {
+        o += sums[i * p.dp + c];
+        all += totals[i * quads];
+      }
+      store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + c, all == 0.0f ? 0.0f : o / all);
     }
-    store_one<BF16>(a.o, token * a.o_token_stride + head * a.o_head_stride + c, all == 0.0f ? 0.0f : o / all);
   }
+}
+
+template <bool BF16, int T>
+void start_join(const AttendParams& p, hipStream_t s) {
+  const int groups = p.a.tokens.n_tokens < 1024 ? (p.a.heads_q * T + 255) / 256 : 1;
+  const int64_t blocks = p.a.tokens.n_tokens * groups, most = kMostThreads / 256;
+  for (int64_t at = 0; at < blocks; at += most) attend_join<BF16, T><<<(unsigned)std::min(most, blocks - at), 256, 0, s>>>(p, groups, at);
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -135,13 +152,9 @@ void launch_attend(const AttendParams& p, hipStream_t s) {
   if (p.rows.units) fp4 ? launch_attend_rows_fp4(p, s) : launch_attend_rows_bf16(p, s);
   if (p.pieces.units) fp4 ? launch_attend_pieces_fp4(p, s) : launch_attend_pieces_bf16(p, s);
   if (p.rows.splits == 1 && p.pieces.splits == 1) return;
-  const int groups = p.a.tokens.n_tokens < 1024 ? p.a.heads_q : 1;
-  const int64_t blocks = p.a.tokens.n_tokens * groups, most = kMostThreads / 256;
-  for (int64_t at = 0; at < blocks; at += most) {
-    const unsigned grid = (unsigned)std::min(most, blocks - at);
-    if (p.a.dtype == EVCONV_BF16) attend_join<true><<<grid, 256, 0, s>>>(p, groups, at);
-    else attend_join<false><<<grid, 256, 0, s>>>(p, groups, at);
-  }
+  const bool few = std::max(p.rows.splits, p.pieces.splits) <= 16;
+  if (p.a.dtype == EVCONV_BF16) few ? start_join<true, 64>(p, s) : start_join<true, 256>(p, s);
+  else few ? start_join<false, 64>(p, s) : start_join<false, 256>(p, s);
 }
 
 }  // namespace evk
