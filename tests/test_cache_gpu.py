@@ -453,7 +453,7 @@ def test_tokens_that_have_no_place(news, kind):
     st.table[0, 1], st.table[1, 3], st.table[2, 0] = -1, st.n_pages, -2 ** 31
     st.table[5] = -1  # (its past is said to be long, but was never written)
     args = st.args()
-    args["table"] = args["table"][:, :5].contiguous()  # stream 2 and 4 run out of it
+    args["table"] = args["table"][:, :5]  # streams 2 and 4 run out of it
     n, g = sum(news), torch.Generator().manual_seed(1)
     q, k, v = (torch.randn(n, 1, 32, generator=g).cuda() for _ in range(3))
     before = [x if x is None else x.clone() for x in st.cache[:5]]
@@ -630,3 +630,56 @@ def test_scores_far_apart(dtype, kind):
             diff = np.abs(got.float().cpu().numpy() - want)
             assert (diff <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -13) * spread).all()
         check_attention(*attend_case(st, hq, dtype, q=q * 0), dtype)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("n_seq", [63, 65, 4097, 20000])
+def test_many_sequences_with_offsets(n_seq, kind):
+    """Whose a workgroup's tokens are, among up to 64 sequences and more, empty ones too: against the same calls without offsets."""
+    torch, ops = torch_ops()
+    rng = np.random.default_rng(n_seq)
+    news = torch.from_numpy(rng.integers(0, 2, n_seq))
+    live = news.nonzero()[:, 0].cuda()
+    n = len(live)
+    past = torch.from_numpy(rng.integers(0, 40, n_seq)).int().cuda()
+    table = torch.arange(2 * n_seq, dtype=torch.int32, device="cuda").view(n_seq, 2)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), news.cumsum(0)]).int().cuda()
+    q, k, v, old = (torch.randn(n, h, 16, device="cuda") for h in (2, 1, 1, 1))
+    results = []
+    for ragged in (False, True):
+        cache = ops.cache_new(2 * n_seq, 1, 16, page=32, kind=kind)
+        torch.manual_seed(1)
+        start = torch.randn(40 * n_seq, 1, 16, device="cuda")
+        ops.cache_append(cache, start, start.roll(1, 0).contiguous(), table, torch.zeros_like(past))
+        args = dict(table=table, past=past, seq_offsets=offsets) if ragged else dict(table=table[live], past=past[live])
+        turned = ops.cache_append(cache, k, v, q=q, freqs=freqs_of(16), **args)
+        pages = ops.cache_select(turned, cache, count=2, **args)
+        results.append([turned, pages, ops.cache_attend(turned, cache, **args), ops.cache_attend(turned, cache, window=7, **args),
+                        ops.cache_attend(turned, cache, selected=pages, **args), *ops.cache_read(cache, n=n, **args), cache.bounds.view(torch.int16)])
+    for a, b in zip(*results):
+        if a.dtype == torch.float32:
+            assert torch.allclose(a, b, rtol=0, atol=2e-6)  # (sums may be cut otherwise)
+        else:
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("news", [[1, 1, 1], [60, 1, 9]])
+def test_tokens_behind_max_len_are_not_seen(news, kind):
+    torch, ops = torch_ops()
+    past = [300, 10, 129]
+    st = whole(past, news, 2, 1, 64, kind, 32)
+    q = torch.from_numpy(st.rng.standard_normal((sum(news), 2, 64))).float()
+    got = ops.cache_attend(q.cuda(), st.cache, max_len=130, **st.args())
+    x, at = q.numpy().astype(np.float64), 0
+    for s, (p, n) in enumerate(zip(past, news)):
+        token = np.arange(len(st.k[s]))
+        seen = (token <= (p + np.arange(n))[:, None]) & (token < 130)
+        for h in range(2):
+            want, _ = ops_ref.attend(x[at:at + n, h], st.k[s][:, 0], st.v[s][:, 0], 1 / 8, seen)
+            assert np.allclose(got[at:at + n, h].cpu().numpy(), want, atol=2e-5)
+        at += n
+    chosen = ops.cache_select(q.cuda(), st.cache, count=9, max_len=130, **st.args()).cpu().numpy()
+    position = np.concatenate([p + np.arange(n) for p, n in zip(past, news)])
+    for row, p in zip(chosen[:, 0], position):
+        assert [c for c in row if c >= 0] == list(range(min(p, 129) // 32 + 1))
