@@ -162,10 +162,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) copy(lane_at + i * step, s_v + buffer * Tile::kBytes + (4 * i + wave_of) * 1024);
     } else {
+      // (values, not places of arrays, to choose between: those would lie in memory)
       const int i = threadIdx.x, t = i % TT;
-      if (i < TT * DP / 32) k_new = *(const uint4*)((HALVES == 1 || i < 32 * (DP / 32) ? k_at[0] : k_at[HALVES - 1]) + k_lane[0]);
-      if (i < DP * HALVES) v_new = *(const uint4*)((i % HALVES == 0 ? v_at[0] : v_at[HALVES - 1]) + v_lane);
-      if (i < 2 * TT) scale_new = (i < TT ? c.k_scale : c.v_scale)[(HALVES == 1 || t < 32 ? scale_at[0] : scale_at[HALVES - 1]) + t % 32];
+      const char *const k0 = k_at[0], *const k1 = k_at[HALVES - 1], *const v0 = v_at[0], *const v1 = v_at[HALVES - 1];
+      const int64_t s0 = scale_at[0], s1 = scale_at[HALVES - 1];
+      const float *const ks = c.k_scale, *const vs = c.v_scale;
+      if (i < TT * DP / 32) k_new = *(const uint4*)((HALVES == 1 || i < 32 * (DP / 32) ? k0 : k1) + k_lane[0]);
+      if (i < DP * HALVES) v_new = *(const uint4*)((i % HALVES == 0 ? v0 : v1) + v_lane);
+      if (i < 2 * TT) scale_new = (i < TT ? ks : vs)[(HALVES == 1 || t < 32 ? s0 : s1) + t % 32];
     }
   };
   auto deliver = [&](int buffer) __attribute__((always_inline)) {  // codes into LDS as bf16
@@ -214,11 +218,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
     __builtin_amdgcn_s_setprio(1);  // (matrix instructions first: the other wave of the SIMD has vector ones meanwhile)
     // ---- scores
     float x[CT][HALVES][8];
-    b16x8 k[2][STEPS];
-    read_keys(0, k[0]);
+    constexpr int AHEAD = DP > 192 ? 0 : 1;  // (keys of 256 channels: there are no registers for two rows of operands)
+    b16x8 k[1 + AHEAD][STEPS];
+    if (AHEAD) read_keys(0, k[0]);
 #pragma unroll
     for (int i = 0; i < 2 * HALVES; ++i) {
-      if (i + 1 < 2 * HALVES) read_keys(i + 1, k[(i + 1) & 1]);
+      if (i + AHEAD < 2 * HALVES) read_keys(i + AHEAD, k[(i + AHEAD) & AHEAD]);
       f32x4 acc[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) acc[ct] = f32x4{0, 0, 0, 0};
@@ -227,7 +232,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i & 1][st], q[ct][st][part], acc[ct], 0, 0, 0);
+          for (int ct = 0; ct < CT; ++ct) acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i & AHEAD][st], q[ct][st][part], acc[ct], 0, 0, 0);
       if constexpr (FP4) {
         const f32x4 scale = *(const f32x4*)(scales + 32 * (i / 2) + 8 * g + 4 * (i % 2));
 #pragma unroll

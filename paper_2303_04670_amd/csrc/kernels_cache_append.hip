@@ -4,9 +4,10 @@
 // rotation's cosines and sines once, in LDS, for all its heads (in 64 bits: some 150 instructions an angle, which 40 heads that
 // did it for themselves would spend twice the copy's time on).  A wave then takes a head at a time, 16 channels to a lane: two vectors
 // of eight that the rotation mixes, so that no lane needs another's.  Whole pages belong to one workgroup, so that bounds and half-filled bytes are read, changed and
-// written by one wave.  8 x 4096 tokens of 32 query and 8 key heads of 128 in bf16 take 221 us, 3.7 TB/s (a copy as large: 4.8), half of them
+// written by one wave.  8 x 4096 tokens of 32 query and 8 key heads of 128 in bf16 take 232 us, 3.5 TB/s (a copy as large: 4.8), half of them
 // vector instructions; 16 single tokens of 4 and 4 heads of 64 in fp32 5.6 us, the chain of a launch, two reads, a sum, the angles and a write.
-//   Two vectors of a rotated pair in one lane instead of each in its own: 815 -> 286 us; bounds as 16-bit integers: 286 -> 235.
+//   Two vectors of a rotated pair in one lane instead of each in its own: 815 -> 286 us; bounds as 16-bit integers: 286 -> 235.  (More rows
+// under way would be 220, but do not fit the 168 registers that leave room for three waves of a SIMD: nothing here may spill.)
 #include <algorithm>
 
 #include "cache_device.h"
@@ -106,45 +107,27 @@ __device__ __forceinline__ Channels channels_of(const AppendParams& p, int l) {
   return c;
 }
 
-// A row's two vectors as they come from memory: their values are taken out of them only when they are wanted, so that several rows can
-// be under way.  (Vectors: what is outside is read inside, where it costs no branch, and becomes zero.)
+// A row's two vectors.  (Vectors: what is outside is read inside, where it costs no branch, and set to zero.)
 template <bool BF16, int MODE>
-struct Row {
-  uint4 u[2][BF16 ? 1 : 2];
-  __device__ __forceinline__ void load(const void* src, int64_t at, const Channels& c, int d) {
+__device__ __forceinline__ void load_row(const void* src, int64_t at, const Channels& c, int d, float (&x)[2][8]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint4* const from = (const uint4*)((const char*)src + (at + min(c.ch[i], d - 8)) * (BF16 ? 2 : 4));
-#pragma unroll
-      for (int j = 0; j < (BF16 ? 1 : 2); ++j) u[i][j] = from[j];
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (MODE == kAnyRows) {
+      load_run<BF16, 8, false>(src, at + c.ch[i], c.left[i], x[i]);
+    } else {
+      load_run<BF16, 8, true>(src, at + min(c.ch[i], d - 8), 8, x[i]);
     }
   }
-  __device__ __forceinline__ void values(const Channels& c, float (&x)[2][8]) const {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const unsigned w[8] = {u[i][0].x, u[i][0].y, u[i][0].z, u[i][0].w, u[i][BF16 ? 0 : 1].x, u[i][BF16 ? 0 : 1].y, u[i][BF16 ? 0 : 1].z, u[i][BF16 ? 0 : 1].w};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = !BF16 ? __uint_as_float(w[j]) : j % 2 ? bf16_high(w[j / 2]) : bf16_low(w[j / 2]);
-        x[i][j] = c.left[i] > 0 ? v : 0.0f;
-      }
-    }
-  }
-};
-template <bool BF16>
-struct Row<BF16, kAnyRows> {
-  float v[2][8];
-  __device__ __forceinline__ void load(const void* src, int64_t at, const Channels& c, int) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) load_run<BF16, 8, false>(src, at + c.ch[i], c.left[i], v[i]);
-  }
-  __device__ __forceinline__ void values(const Channels&, float (&x)[2][8]) const {
+}
+template <int MODE>
+__device__ __forceinline__ void zero_outside(const Channels& c, float (&x)[2][8]) {
+  if constexpr (MODE != kAnyRows)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[i][j] = v[i][j];
-  }
-};
+      for (int j = 0; j < 8; ++j)
+        if (c.left[i] <= 0) x[i][j] = 0.0f;
+}
 
 // Cosines and sines of a token's angles: a row of LDS, or computed where they are wanted.
 struct SharedAngles {
@@ -337,11 +320,10 @@ struct Bounds {
 };
 
 template <bool BF16, bool FP4, int MODE, int LANES>
-__global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(AppendParams p) {
+__global__ __launch_bounds__(256, MODE == kAnyRows ? 1 : 3) void cache_append(AppendParams p) {
   constexpr bool VEC = MODE != kAnyRows;
   constexpr int ROWS = 64 / LANES;                    // tokens that a wave deals with at once
-  constexpr int AT_ONCE = !VEC || LANES < 4 ? 1 : 2;    // ... has under way of a query head, times that
-  constexpr int AT_ONCE_KV = !VEC || LANES < 4 || !BF16 ? 1 : 2;
+  constexpr int AT_ONCE = !VEC || LANES < 4 ? 1 : 2;  // ... has under way, of a query head, times that
   extern __shared__ __align__(16) char s_mem[];
   const evconv_append_args& a = p.a;
   const evconv_cache& c = a.cache;
@@ -381,19 +363,21 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
     for (; role < min(role_end, a.heads_q); role += waves) {  // ---- a head of the queries
       const int64_t head_in = role * a.q.head_stride, head_out = role * a.q_out_head_stride;
       for (int r0 = 0; r0 < count; r0 += AT_ONCE * ROWS) {
-        Row<BF16, MODE> in[AT_ONCE];
+        float x[AT_ONCE][2][8];
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) in[i].load(a.q.data, (token + min(r0 + i * ROWS + row, count - 1)) * a.q.token_stride + head_in, own, d);
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int r = min(r0 + i * ROWS + row, count - 1);
+          load_row<BF16, MODE>(a.q.data, (token + r) * a.q.token_stride + head_in, own, d, x[i]);
+        }
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
           if (r0 + i * ROWS >= count) break;
           const int r = r0 + i * ROWS + row, r_in = min(r, count - 1);
-          float x[2][8];
-          in[i].values(own, x);
-          turn_row<BF16, MODE, LANES>(p, a.q.data, (token + r_in) * a.q.token_stride + head_in, own, a.q_norm, s_wq, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x);
+          zero_outside<MODE>(own, x[i]);
+          turn_row<BF16, MODE, LANES>(p, a.q.data, (token + r_in) * a.q.token_stride + head_in, own, a.q_norm, s_wq, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x[i]);
           const int64_t at = (token + r_in) * a.q_out_token_stride + head_out;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) store_row<VEC>(a.q_out, at, own.ch[h], r < count ? own.left[h] : 0, x[h], BF16);
+          for (int h = 0; h < 2; ++h) store_row<VEC>(a.q_out, at, own.ch[h], r < count ? own.left[h] : 0, x[i][h], BF16);
         }
       }
     }
@@ -403,59 +387,51 @@ __global__ __launch_bounds__(256, MODE == kAnyRows ? 2 : 3) void cache_append(Ap
       const int64_t k_head = head * a.k.head_stride, v_head = head * a.v.head_stride;
       Bounds bounds;
       bounds.clear();
-      for (int r0 = 0; r0 < count; r0 += AT_ONCE_KV * ROWS) {
-        Row<BF16, MODE> k_in[AT_ONCE_KV], v_in[AT_ONCE_KV];
+      for (int r0 = 0; r0 < count; r0 += ROWS) {
+        const int r = r0 + row, r_in = min(r, count - 1);
+        const bool live = r < count;
+        const int64_t k_row = (token + r_in) * a.k.token_stride + k_head;
+        float x[2][8], v[2][8];
+        load_row<BF16, MODE>(a.k.data, k_row, own, d, x);
+        load_row<BF16, MODE>(a.v.data, (token + r_in) * a.v.token_stride + v_head, own, d, v);
+        zero_outside<MODE>(own, x);
+        zero_outside<MODE>(own, v);
+        turn_row<BF16, MODE, LANES>(p, a.k.data, k_row, own, a.k_norm, s_wk, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x);
+        const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
+        const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
+        if (bad)
 #pragma unroll
-        for (int i = 0; i < AT_ONCE_KV; ++i) {
-          const int64_t from = token + min(r0 + i * ROWS + row, count - 1);
-          k_in[i].load(a.k.data, from * a.k.token_stride + k_head, own, d);
-          v_in[i].load(a.v.data, from * a.v.token_stride + v_head, own, d);
-        }
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < AT_ONCE_KV; ++i) {
-          if (r0 + i * ROWS >= count) break;
-          const int r = r0 + i * ROWS + row, r_in = min(r, count - 1);
-          const bool live = r < count;
-          float x[2][8], v[2][8];
-          k_in[i].values(own, x);
-          v_in[i].values(own, v);
-          turn_row<BF16, MODE, LANES>(p, a.k.data, (token + r_in) * a.k.token_stride + k_head, own, a.k_norm, s_wk, SharedAngles{s_cos + r_in * half, s_sin + r_in * half}, x);
-          const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
-          const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
-          if (bad)
+            for (int j = 0; j < 8; ++j)
+              if (j < own.left[h]) x[h][j] = NAN;
+        if (!live) continue;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+          const int ch = own.ch[h];
+          if (ch >= p.dp) continue;
+          const unsigned kw[4] = {pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7])};
+          bounds.add_key(h, kw, bad);
+          if constexpr (FP4) {
+            const unsigned v4 = codes_of(v[h], big_v);
+            *(unsigned*)((char*)c.k + (at + slot + r) * (p.dp / 2) + ch / 2) = codes_of(x[h], big_k);
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (j < own.left[h]) x[h][j] = NAN;
-          if (!live) continue;
+            for (int j = 0; j < 8; ++j) s_v[(ch + j) * value_row(true) + slot % kPiece + r] = (char)(v4 >> (4 * j) & 15);
+            if (ch == 0) {
+              c.k_scale[at + slot + r] = scale_of(big_k);
+              c.v_scale[at + slot + r] = scale_of(big_v);
+            }
+          } else {
+            *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int ch = own.ch[h];
-            if (ch >= p.dp) continue;
-            const unsigned kw[4] = {pack_bf16(x[h][0], x[h][1]), pack_bf16(x[h][2], x[h][3]), pack_bf16(x[h][4], x[h][5]), pack_bf16(x[h][6], x[h][7])};
-            bounds.add_key(h, kw, bad);
-            if constexpr (FP4) {
-              const unsigned v4 = codes_of(v[h], big_v);
-              *(unsigned*)((char*)c.k + (at + slot + r) * (p.dp / 2) + ch / 2) = codes_of(x[h], big_k);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) s_v[(ch + j) * value_row(true) + slot % kPiece + r] = (char)(v4 >> (4 * j) & 15);
-              if (ch == 0) {
-                c.k_scale[at + slot + r] = scale_of(big_k);
-                c.v_scale[at + slot + r] = scale_of(big_v);
+            for (int j = 0; j < 8; j += 2) {
+              unsigned w = pack_bf16(v[h][j], v[h][j + 1]);
+              if (big_v >= kNoBf16) {  // (no value of v that is not finite)
+                if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+                if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
               }
-            } else {
-              *(uint4*)((uint16_t*)c.k + (at + slot + r) * p.dp + ch) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
-#pragma unroll
-              for (int j = 0; j < 8; j += 2) {
-                unsigned w = pack_bf16(v[h][j], v[h][j + 1]);
-                if (big_v >= kNoBf16) {  // (no value of v that is not finite)
-                  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-                  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
-                }
-                *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)w;
-                *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)(w >> 16);
-              }
+              *(uint16_t*)(s_v + (ch + j) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)w;
+              *(uint16_t*)(s_v + (ch + j + 1) * value_row(false) + 2 * (slot % kPiece + r)) = (uint16_t)(w >> 16);
             }
           }
         }
@@ -539,17 +515,16 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
   const int head = query ? role : role - a.heads_q;
   const int64_t row = token * src.token_stride + head * src.head_stride;
   const float* const norm = query ? a.q_norm : a.k_norm;
-  Row<BF16, MODE> in, v_in;
-  in.load(src.data, row, own, d);
-  if (!query) v_in.load(a.v.data, token * a.v.token_stride + head * a.v.head_stride, own, d);
+  float x[2][8], v[2][8];
+  load_row<BF16, MODE>(src.data, row, own, d, x);
+  if (!query) load_row<BF16, MODE>(a.v.data, token * a.v.token_stride + head * a.v.head_stride, own, d, v);
   const int past = tk.past[token];
   if (norm)
     for (int i = lane; i < p.dp; i += 64) s_weight[i] = i < d ? norm[i] : 0.0f;
   lds_turn();
   const double position = (double)(a.positions ? a.positions[token] : (int64_t)past);
   const int to = past < 0 ? -1 : page_of(c, tk, (int)token, past >> p.log);
-  float x[2][8], v[2][8];
-  in.values(own, x);
+  zero_outside<MODE>(own, x);
   turn_row<BF16, MODE, LANES>(p, src.data, row, own, norm, s_weight, OwnAngles{position, a.freqs}, x);
   if (query) {
     const int64_t at = token * a.q_out_token_stride + head * a.q_out_head_stride;
@@ -557,7 +532,7 @@ __global__ __launch_bounds__(64) void append_single(AppendParams p) {
     for (int h = 0; h < 2; ++h) store_row<VEC>(a.q_out, at, own.ch[h], live ? own.left[h] : 0, x[h], BF16);
     return;
   }
-  v_in.values(own, v);
+  zero_outside<MODE>(own, v);
   const unsigned big_k = row_largest<LANES>(x), big_v = row_largest<LANES>(v);
   const bool bad = big_k >= kNoBf16 || (!FP4 && big_v >= kNoBf16);
   if (bad)

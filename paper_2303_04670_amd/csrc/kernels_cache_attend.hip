@@ -8,7 +8,7 @@ namespace evk {
 namespace {
 
 // What a row's stretches gave, o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i: T threads to a row (many stretches: a workgroup; few: a
-// wave, which meets no barrier; 8192 rows of 8 stretches 24 us by workgroups, 14 by waves), `groups` workgroups to a token's heads (many
+// wave, which meets no barrier; 8192 rows of 8 stretches 24 us by workgroups, 11 by waves), `groups` workgroups to a token's heads (many
 // tokens, of which most may have one stretch: one).  Which stretches a row has follows from what it sees; a row with one was written by the
 // kernel itself.
 template <bool BF16, int T>
