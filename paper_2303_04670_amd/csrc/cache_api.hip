@@ -26,8 +26,7 @@ evconv_status check_cache(const char* what, const evconv_cache& c, const evconv_
   return EVCONV_OK;
 }
 
-evconv_status check_head(const char* what, const void* args, int abi_version, int dtype) {
-  (void)args;
+evconv_status check_head(const char* what, int abi_version, int dtype) {
   if (abi_version != EVCONV_OPS_ABI_VERSION) return refuse(EVCONV_ERR_BAD_DESC, "%s: abi_version %d, expected %d", what, abi_version, EVCONV_OPS_ABI_VERSION);
   if (!float_type(dtype)) return refuse(EVCONV_ERR_INVALID_ARG, "%s: dtype %d", what, dtype);
   return EVCONV_OK;
@@ -42,7 +41,7 @@ evconv_status check_query_heads(const char* what, int heads_q, int heads) {
 evconv_status check_append(const evconv_append_args* a) {
   const char* const what = "cache append";
   if (!a) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null arguments", what);
-  evconv_status st = check_head(what, a, a->abi_version, a->dtype);
+  evconv_status st = check_head(what, a->abi_version, a->dtype);
   if (st == EVCONV_OK) st = check_cache(what, a->cache, a->tokens);
   if (st != EVCONV_OK) return st;
   if (a->heads_q < 0) return refuse(EVCONV_ERR_SHAPE, "%s: %d query heads", what, a->heads_q);
@@ -58,7 +57,7 @@ evconv_status check_append(const evconv_append_args* a) {
 evconv_status check_read(const evconv_read_args* a) {
   const char* const what = "cache read";
   if (!a) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null arguments", what);
-  evconv_status st = check_head(what, a, a->abi_version, a->dtype);
+  evconv_status st = check_head(what, a->abi_version, a->dtype);
   if (st == EVCONV_OK) st = check_cache(what, a->cache, a->tokens);
   if (st != EVCONV_OK) return st;
   if (a->tokens.n_tokens && (!a->k || !a->v)) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null tensor", what);
@@ -68,7 +67,7 @@ evconv_status check_read(const evconv_read_args* a) {
 evconv_status plan(const evconv_attend_args* a, AttendParams* p, size_t* bytes) {
   const char* const what = "cache attend";
   if (!a) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null arguments", what);
-  evconv_status st = check_head(what, a, a->abi_version, a->dtype);
+  evconv_status st = check_head(what, a->abi_version, a->dtype);
   if (st == EVCONV_OK) st = check_cache(what, a->cache, a->tokens);
   if (st == EVCONV_OK) st = check_query_heads(what, a->heads_q, a->cache.heads);
   if (st != EVCONV_OK) return st;
@@ -89,7 +88,7 @@ evconv_status plan(const evconv_attend_args* a, AttendParams* p, size_t* bytes) 
 evconv_status plan(const evconv_select_args* a, SelectParams* p, size_t* bytes) {
   const char* const what = "cache select";
   if (!a) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null arguments", what);
-  evconv_status st = check_head(what, a, a->abi_version, a->dtype);
+  evconv_status st = check_head(what, a->abi_version, a->dtype);
   if (st == EVCONV_OK) st = check_cache(what, a->cache, a->tokens);
   if (st == EVCONV_OK) st = check_query_heads(what, a->heads_q, a->cache.heads);
   if (st != EVCONV_OK) return st;
@@ -100,7 +99,6 @@ evconv_status plan(const evconv_select_args* a, SelectParams* p, size_t* bytes) 
   if (a->tokens.n_tokens && (!a->q.data || !a->selected)) return refuse(EVCONV_ERR_INVALID_ARG, "%s: null tensor", what);
   *p = SelectParams{};
   p->a = *a;
-  p->vec = a->cache.d % 8 == 0 && wide(a->dtype, a->q);
   *bytes = a->tokens.n_tokens ? plan_select(*p) : 0;
   return EVCONV_OK;
 }

@@ -7,7 +7,7 @@
 // made them.  Few workgroups over many tokens share a row's tokens and join what they found.
 //   8 sequences of 4096 tokens, 16 heads on 4 of 128 in bf16: 573 us, 960 TFLOP/s, where a large library product reaches 1215; matrix
 // instructions 40 %, vector ones (exponentials a third of them) as much.  Operands read ahead instead of where they are wanted 710 -> 661 us,
-// addresses made once 661 -> 624, priority to the matrix instructions 624 -> 611.  512 tokens on 32768 in 4 bits: 195 us, 710 TFLOP/s.
+// addresses made once 661 -> 624, priority to the matrix instructions 624 -> 611.  512 tokens on 32768 in 4 bits: 175 us, 790 TFLOP/s.
 #pragma once
 
 #include "cache_attend_rows.h"

@@ -13,7 +13,7 @@ namespace {
 
 constexpr unsigned kForced = 0xffffffffu, kNotANumber = 0xfffffffeu;
 constexpr int kHeads = 16;  // query heads whose values are in LDS at once
-constexpr int kHeld = 4;    // pages that a lane holds
+constexpr int kHeld = 2;    // pages that a lane holds
 constexpr int kRounds = 2;  // of a workgroup
 
 // Unsigned numbers in the order of the floats, all above 0: that is the mark of a page that cannot be chosen.
@@ -47,13 +47,12 @@ __device__ __forceinline__ double of_lane(double v) {
 }
 constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kTurn4 = 0x124, kTurn8 = 0x128;  // lanes l ^ 1, l ^ 2 (of four), l - 4, l - 8 (of 16, round)
 
-// Sums over LANES neighbouring lanes of four values; lane l has that of value 2 (l & 1) + (l >> 1 & 1).
+// Sums over LANES neighbouring lanes of two values; lane l has that of value l & 1.
 template <int LANES>
-__device__ __forceinline__ double pages_sum(const double (&v)[4], int lane) {
-  const bool odd = lane & 1, upper = lane & 2;
-  const double a = (odd ? v[2] : v[0]) + of_lane<kSwap1>(odd ? v[0] : v[2]);
-  const double b = (odd ? v[3] : v[1]) + of_lane<kSwap1>(odd ? v[1] : v[3]);
-  double s = (upper ? b : a) + of_lane<kSwap2>(upper ? a : b);
+__device__ __forceinline__ double pages_sum(const double (&v)[2], int lane) {
+  const bool odd = lane & 1;
+  double s = (odd ? v[1] : v[0]) + of_lane<kSwap1>(odd ? v[0] : v[1]);
+  s += of_lane<kSwap2>(s);
   if constexpr (LANES == 8) s += __shfl_xor(s, 4);
   if constexpr (LANES >= 16) {
     s += of_lane<kTurn4>(s);
@@ -65,9 +64,10 @@ __device__ __forceinline__ double pages_sum(const double (&v)[4], int lane) {
 
 // A workgroup goes over kRounds times 4 kHeld GROUPS pages: its start (whose the query is, its values as 64-bit numbers) costs as much as a
 // round, and the next one's bounds are on their way while one is added up.  us for 16 streams of up to 2048 pages, 8 key heads / one of 15626,
-// 4: 1 round 25.6 / 13.2, 2 26.9 / 12.4, 4 28.2 / 15.6.  Bound by 64-bit instructions and the start: the bounds are 60 MB / 32 MB.
+// 4, with four pages to a lane: 1 round 25.6 / 13.2, 2 26.9 / 12.4, 4 28.2 / 15.6; 2 rounds with two pages, which leave room for twice the waves,
+// 23.9 / 12.3.  Bound by 64-bit instructions and the start: the bounds are 60 MB / 32 MB.
 template <bool BF16, int DP>
-__global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks, int64_t block0) {
+__global__ __launch_bounds__(256) void score_pages(SelectParams p, int blocks, int64_t block0) {
   constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32, GROUPS = 64 / LANES, ROUND = 4 * kHeld * GROUPS;
   // min(q, 0), max(q, 0): of a lane's eight channels two at a time, neighbouring lanes next to each other
   __shared__ double2 s_q[kHeads][2][4][DP / 8];
@@ -154,10 +154,10 @@ __global__ __launch_bounds__(256, 2) void score_pages(SelectParams p, int blocks
         best = fmax(best, score);
       }
     }
-    if (lane % LANES < 4) {
-      const int i = 2 * (lane & 1) + (lane >> 1 & 1);
+    if (lane % LANES < 2) {
+      const int i = lane & 1;
       const int64_t page = page_number(round, i);
-      const bool here = i == 0 ? is_there[0] : i == 1 ? is_there[1] : i == 2 ? is_there[2] : is_there[3];
+      const bool here = i == 0 ? is_there[0] : is_there[1];
       if (page <= query.last) {
         const bool forced = page < a.first || page > query.last - a.last;
         p.score[unit * p.pages + page] = !here ? 0u : forced ? kForced : bad ? kNotANumber : key_of((float)best);
@@ -204,14 +204,17 @@ __device__ __forceinline__ void range_of(unsigned& lo, unsigned& hi, unsigned (*
 }
 
 // The `count` highest keys of a row, the lower index first among equals: the key of the last one, by counting the keys in equal parts of the
-// range that it is in, until a part is one key; then all above it and the first of those that equal it, in the order of their pages.  A
+// range that it is in, until a part is one key or has few, which are ranked (10.8 -> 9.4 us, of 15626 pages 14.7 -> 13.8); then all above it
+// and the first of those that equal it, in the order of their pages.  A
 // workgroup to a row, a thread to neighbouring pages, whose keys (HELD: up to 16) stay in its registers.  (Parts of the range that the keys
 // have, not digits of them: scores of one sequence share their upper digits, and counters that all threads want are counted one after the
-// other: 59 us against 14 for 15626 pages.)
+// other: 59 us against 14.7 for 15626 pages, before the few were ranked.)
 template <bool HELD>
 __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t unit0) {
-  constexpr int kParts = 2048;
-  __shared__ int s_parts[kParts], s_found[2];
+  constexpr int kParts = 2048, kFew = 256;
+  __shared__ int s_parts[kParts], s_found[3];
+  __shared__ unsigned s_few[kFew];  // keys of a part
+  __shared__ int s_few_at[kFew];    // and their pages
   __shared__ Two s_wave[16];
   __shared__ unsigned s_range[16][2];
   const evconv_select_args& a = p.a;
@@ -274,6 +277,7 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
           if (before + c >= need) {
             s_found[0] = top - i;
             s_found[1] = need - before;
+            s_found[2] = c;
             break;
           }
           before += c;
@@ -287,7 +291,37 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
         break;
       }
       hi = min(hi, lo + ((1u << shift) - 1));
+      const int few = s_found[2];
       __syncthreads();
+      if (few <= kFew) {  // as few as that are ranked at once
+        if (t == 0) s_found[0] = 0;
+        __syncthreads();
+        each([&](int i, unsigned k) {
+          if (k >= lo && k <= hi) {
+            const int at = atomicAdd(&s_found[0], 1);
+            s_few[at] = k;
+            s_few_at[at] = i;
+          }
+        });
+        __syncthreads();
+        if (t < few) {
+          const unsigned mine_key = s_few[t];
+          const int mine_at = s_few_at[t];
+          int larger = 0, earlier = 0;
+          for (int i = 0; i < few; ++i) {
+            larger += s_few[i] > mine_key;
+            earlier += s_few[i] == mine_key && s_few_at[i] < mine_at;
+          }
+          if (larger + earlier == need - 1) {
+            s_parts[0] = (int)mine_key;
+            s_parts[1] = need - larger;
+          }
+        }
+        __syncthreads();
+        edge = (unsigned)s_parts[0];
+        equal = s_parts[1];
+        break;
+      }
     }
     if (edge == kForced) equal = a.count;
   }
@@ -345,7 +379,7 @@ void launch_select(const SelectParams& p, hipStream_t s) {
     if (p.a.dtype == EVCONV_BF16) start_scores<true>(p, grid, blocks, at, s);
     else start_scores<false>(p, grid, blocks, at, s);
   }
-  // (2048 pages take 10.8 us with 256 threads, 10.3 with 1024: the barriers; the fewer leave room for other rows)
+  // (128 rows of 2048 pages take 9.4 us with 256 threads and with 1024: the barriers; the fewer leave room for other rows)
   const int threads = p.pages <= 4096 ? 256 : 1024;
   const int64_t rows = kMostThreads / threads;
   for (int64_t at = 0; at < units; at += rows) {

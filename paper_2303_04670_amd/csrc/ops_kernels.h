@@ -103,7 +103,6 @@ void launch_attend_pieces_fp4(const AttendParams& p, hipStream_t s);
 struct SelectParams {
   evconv_select_args a;
   int dp, log, share;
-  bool vec;
   int64_t most;   // as above
   int pages;      // pages of a sequence at most, the row length of `score`
   int len;        // tokens of every sequence, or -1

@@ -360,6 +360,25 @@ def test_select_of_equal_pages_takes_the_lower_ones():
     assert got == [[[0, 2, 3, 99], [0, 2, 50, 99]]]
 
 
+@pytest.mark.parametrize("close", [1, 2, 255, 256, 257, 400])
+def test_select_among_close_scores(close):
+    """The last page chosen is one of some that lie close together, most of them equal to others, between few that lie far above and below."""
+    torch, ops = torch_ops()
+    rng = np.random.default_rng(close)
+    values = np.concatenate([1 + rng.integers(0, 4, close) / 128, 2.0 ** rng.integers(8, 30, 40), -2.0 ** rng.integers(8, 30, 200)])  # exact in bf16
+    rng.shuffle(values)
+    values = np.append(values, 0)  # the newest page, always chosen
+    n_pages = len(values)
+    cache = ops.cache_new(n_pages, 1, 32, page=32, device="cuda")
+    cache.bounds[:, 0] = torch.from_numpy(values).float().cuda()[:, None, None].expand(-1, 2, 32).to(torch.bfloat16)
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    past = torch.tensor([32 * n_pages - 1], dtype=torch.int32, device="cuda")
+    q = torch.ones(1, 1, 32, device="cuda")
+    for count in sorted({41, 42, 41 + close // 2, 40 + close, 41 + close, 42 + close}):
+        got = ops.cache_select(q, cache, table, past, count, first=0).cpu().tolist()[0][0]
+        assert got == ops_ref.choose(32 * values, count, 0, 1), count
+
+
 @pytest.mark.parametrize("n_pages", [5, 1500, 5000])
 def test_select_of_many_pages(n_pages):
     """Scores that repeat, and a choice among thousands."""
