@@ -455,7 +455,13 @@ def _packer(args):
     pack = struct.Struct("@" + "".join({_i32: "i", _i64: "q", _f32: "f", _vp: "Q"}[kind] for _, kind in flat._fields_)).pack
     assert len(pack(*[0] * len(flat._fields_))) <= ctypes.sizeof(flat)  # (but for the padding at the end)
     rest = b"\0" * (ctypes.sizeof(flat) - len(pack(*[0] * len(flat._fields_))))
-    return (lambda *fields: pack(*fields) + rest) if rest else pack
+
+    def packed(*fields):
+        try:
+            return pack(*fields) + rest
+        except struct.error as reason:
+            _refuse(ERR_INVALID_ARG, f"{args.__name__}: a number that does not fit its field ({reason})")
+    return packed
 
 
 _append_args, _read_args, _attend_args, _select_args = (_packer(a) for a in (AppendArgs, ReadArgs, AttendArgs, SelectArgs))
@@ -548,6 +554,8 @@ def cache_append(cache, k, v, table, past, q=None, *, seq_offsets=None, q_norm=N
 
 def cache_read(cache, table, past, n, *, seq_offsets=None, dtype=torch.float32):
     """Keys and values of `n` tokens from position past[s] on of the sequences, as rows [n, heads, d] (evconv_cache_read)."""
+    if n < 0:
+        _refuse(ERR_SHAPE, f"cache read: {n} tokens")
     gpu = table.get_device()
     if gpu < 0:
         _explain(table, "table", gpu, torch.int32, table.shape)
@@ -611,6 +619,8 @@ def cache_select(q, cache, table, past, count, *, seq_offsets=None, first=1, las
 
     The `first` pages of the sequence and the `last` ones up to the token's own, then those whose keys' bounds allow the highest scores.
     q as it goes to cache_attend; the rest as of cache_attend."""
+    if not 1 <= count <= 65536:
+        _refuse(ERR_SHAPE if count < 1 else ERR_UNSUPPORTED, f"cache select: count {count}: 1 to 65536")
     if q.dim() != 3:
         _refuse(ERR_SHAPE, f"q {tuple(q.shape)}: expected [tokens, heads, d]")
     gpu, dtype, shape = q.get_device(), q.dtype, q.shape

@@ -141,6 +141,27 @@ def test_binding_refuses_before_the_library():
 
 # ---- the references
 
+def test_numbers_out_of_range_are_refused_by_the_binding():
+    """What would fail in an allocation or does not fit its field is refused like any other argument."""
+    torch = pytest.importorskip("torch")
+    q, cache = torch.zeros(1, 4, 64), ops.Cache(*[torch.zeros(1)] * 5, 64)
+    table, past = torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    for count, status in ((-1, ev.ERR_SHAPE), (0, ev.ERR_SHAPE), (65537, ev.ERR_UNSUPPORTED), (1 << 40, ev.ERR_UNSUPPORTED)):
+        with pytest.raises(ev.EvConvError) as e:
+            ops.cache_select(q, cache, table, past, count)
+        assert e.value.status == status and "count" in str(e.value)
+    with pytest.raises(ev.EvConvError) as e:
+        ops.cache_read(cache, table, past, -1)
+    assert e.value.status == ev.ERR_SHAPE
+    fields = [0] * len(ops._flat(ops.AttendArgs)._fields_)
+    window = [name for name, _ in ops._flat(ops.AttendArgs)._fields_].index("window")
+    assert len(ops._attend_args(*fields)) == ctypes.sizeof(ops.AttendArgs)
+    fields[window] = 1 << 31
+    with pytest.raises(ev.EvConvError) as e:
+        ops._attend_args(*fields)
+    assert e.value.status == ev.ERR_INVALID_ARG
+
+
 def test_fp4_reference_against_a_search():
     rng = np.random.default_rng(1)
     x = np.concatenate([rng.standard_normal((50, 32)), np.zeros((1, 32)), rng.integers(-24, 25, (50, 32)) / 4]).astype(np.float32)
