@@ -6,12 +6,12 @@
 // them, whose values come from LDS; so the conversions are made once for all heads.
 #include <algorithm>
 
+#include "cache_choice.h"
 #include "cache_device.h"
 
 namespace evk {
 namespace {
 
-constexpr unsigned kForced = 0xffffffffu, kNotANumber = 0xfffffffeu;
 constexpr int kHeads = 16;  // query heads whose values are in LDS at once
 constexpr int kHeld = 2;    // pages that a lane holds
 constexpr int kRounds = 2;  // of a workgroup
@@ -211,8 +211,8 @@ __device__ __forceinline__ void range_of(unsigned& lo, unsigned& hi, unsigned (*
 // other: 59 us against 14.7 for 15626 pages, before the few were ranked.)
 template <bool HELD>
 __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t unit0) {
-  constexpr int kParts = 2048, kFew = 256;
-  __shared__ int s_parts[kParts], s_found[3];
+  constexpr int kFew = 256;
+  __shared__ int s_parts[kKeyParts], s_found[3];
   __shared__ unsigned s_few[kFew];  // keys of a part
   __shared__ int s_few_at[kFew];    // and their pages
   __shared__ Two s_wave[16];
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
     range_of(lo, hi, s_range);
     edge = kForced;  // (none but them)
     while (need > 0) {
-      const int bits = 32 - __builtin_clz(max(hi - lo, 1u)), shift = max(bits - 11, 0), parts = (int)((hi - lo) >> shift) + 1;
+      const int shift = part_shift({lo, hi}), parts = part_count({lo, hi}, shift);
       for (int i = t; i < parts; i += threads) s_parts[i] = 0;
       __syncthreads();
       each([&](int, unsigned k) {
@@ -283,14 +283,15 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
           before += c;
         }
       __syncthreads();
-      lo += (unsigned)s_found[0] << shift;
+      const KeyRange part = part_range({lo, hi}, shift, s_found[0]);
+      lo = part.lo;
+      hi = part.hi;
       need = s_found[1];
       if (shift == 0) {
         edge = lo;
         equal = need;
         break;
       }
-      hi = min(hi, lo + ((1u << shift) - 1));
       const int few = s_found[2];
       __syncthreads();
       if (few <= kFew) {  // as few as that are ranked at once
@@ -334,7 +335,8 @@ __global__ __launch_bounds__(1024) void choose_pages(SelectParams p, int64_t uni
   Two before = sums_before(found, s_wave, &all);
   each([&](int i, unsigned k) {
     const bool above = k > edge, same = k == edge && edge != 0;
-    if (above || (same && before.b < equal)) out[before.a + min(before.b, equal)] = i;
+    const int at = before.a + min(before.b, equal);
+    if ((above || (same && before.b < equal)) && at < a.count) out[at] = i;
     before.a += above;
     before.b += same;
   });

@@ -702,3 +702,29 @@ def test_tokens_behind_max_len_are_not_seen(news, kind):
     position = np.concatenate([p + np.arange(n) for p, n in zip(past, news)])
     for row, p in zip(chosen[:, 0], position):
         assert [c for c in row if c >= 0] == list(range(min(p, 129) // 32 + 1))
+
+
+@pytest.mark.parametrize("n_pages,count,first,last", [(40, 3, 1, 1), (2000, 64, 1, 1), (2000, 600, 0, 3), (5000, 128, 2, 2), (20000, 128, 1, 1)])
+def test_select_among_pages_that_score_no_number(n_pages, count, first, last):
+    """0, need - 1, need, need + 1 and all pages NaN, of one head these and of the other those: whole rows, and nothing written behind them."""
+    torch, ops = torch_ops()
+    rng, need = np.random.default_rng(n_pages + count), count - first - last
+    cache = ops.cache_new(n_pages, 2, 32, page=32, device="cuda")
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    past = torch.tensor([32 * n_pages - 3], dtype=torch.int32, device="cuda")
+    q = torch.ones(3, 4, 32, device="cuda")
+    numbers = sorted({0, need - 1, need, need + 1, n_pages})
+    for bads in zip(numbers, numbers[1:] + numbers[:1]):
+        for values in (rng.standard_normal(n_pages), -2.0 ** rng.integers(8, 100, n_pages)):
+            scores = np.tile(to_bf16(values).float().numpy(), (2, 1))
+            for head, bad in enumerate(bads):
+                scores[head, first + rng.permutation(n_pages - first - last)[:bad] if bad < n_pages else slice(None)] = np.nan
+            cache.bounds[:] = torch.from_numpy(scores.T.copy()).cuda().to(torch.bfloat16)[:, :, None, None].expand(-1, -1, 2, 32)
+            room = torch.full((1 << 16,), 7, dtype=torch.int32, device="cuda")
+            out = room[1 << 12:][:3 * 2 * count].view(3, 2, count)
+            got = ops.cache_select(q, cache, table, past, count, first=first, last=last, out=out).cpu().numpy()
+            assert room[:1 << 12].eq(7).all() and room[(1 << 12) + out.numel():].eq(7).all(), bads
+            for head in range(2):
+                want = ops_ref.choose(32 * scores[head], count, first, last)
+                for token in range(3):
+                    assert got[token, head].tolist() == want, (bads, head, token)
