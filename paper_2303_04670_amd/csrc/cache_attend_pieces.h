@@ -63,32 +63,35 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendPa
   const int64_t total = (int64_t)piece.count * p.share, row0 = (int64_t)piece.at * ROWS;
   if (piece.at < 0 || row0 >= total || total <= p.few) return;
   const int past = tk.past[piece.seq];
-  const int last = (int)min(row0 + ROWS, total) - 1;
+  // (rows of a sequence may pass 32 bits: they are counted from the workgroup's first one on)
+  const int last = (int)min(total - row0, (int64_t)ROWS) - 1;
+  const int token0 = (int)(row0 / p.share), rest0 = (int)(row0 - (int64_t)token0 * p.share);
+  auto token_of = [&](int row) __attribute__((always_inline)) { return token0 + (rest0 + row) / p.share; };
   int lo_min, hi_max, other;
-  seen_by(p, past, (int)(row0 / p.share), lo_min, other);
-  seen_by(p, past, last / p.share, other, hi_max);
+  seen_by(p, past, token0, lo_min, other);
+  seen_by(p, past, token_of(last), other, hi_max);
   const int chunk = p.pieces.chunk;
   const int base0 = stretch_base(lo_min);
   const int64_t begin = max(base0 + (int64_t)split * chunk, (int64_t)lo_min) & ~(int64_t)(TT - 1), end = min(base0 + (int64_t)(split + 1) * chunk, (int64_t)hi_max);
   if (begin >= end && split != 0) return;
   // of this wave: its first and last row, what all of them and what any of them sees
-  const int64_t wave_row = row0 + wave * 16 * CT;
-  const bool working = wave_row < total;
+  const int wave_row = wave * 16 * CT;
+  const bool working = wave_row <= last;
   int wave_lo_min = 0, wave_hi_min = 0, wave_lo_max = 0, wave_hi_max = 0;
   if (working) {
-    seen_by(p, past, (int)(wave_row / p.share), wave_lo_min, wave_hi_min);
-    seen_by(p, past, (int)(min(wave_row + 16 * CT, total) - 1) / p.share, wave_lo_max, wave_hi_max);
+    seen_by(p, past, token_of(wave_row), wave_lo_min, wave_hi_min);
+    seen_by(p, past, token_of(min(wave_row + 16 * CT - 1, last)), wave_lo_max, wave_hi_max);
   }
   int lo[CT], hi[CT], token[CT], q_head[CT];
   bool live[CT];
   b16x8 q[CT][STEPS][PARTS];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const int64_t r = wave_row + 16 * ct + n;
-    live[ct] = r < total;
-    const int within = live[ct] ? (int)(r / p.share) : 0;
+    const int r = wave_row + 16 * ct + n;
+    live[ct] = r <= last;
+    const int within = live[ct] ? token_of(r) : 0;
     token[ct] = piece.first + within;
-    q_head[ct] = head * p.share + (live[ct] ? (int)(r - (int64_t)within * p.share) : 0);
+    q_head[ct] = head * p.share + (live[ct] ? rest0 + r - (within - token0) * p.share : 0);
     lo[ct] = hi[ct] = 0;
     if (live[ct]) seen_by(p, past, within, lo[ct], hi[ct]);
 #pragma unroll

@@ -728,3 +728,20 @@ def test_select_among_pages_that_score_no_number(n_pages, count, first, last):
                 want = ops_ref.choose(32 * scores[head], count, first, last)
                 for token in range(3):
                     assert got[token, head].tolist() == want, (bads, head, token)
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_rows_behind_31_bits(ragged):
+    """A sequence of more than 2^31 tokens x query heads of a key head: every token sees the same 32 tokens of one page."""
+    torch, ops = torch_ops()
+    n, heads = (1 << 21) + 3, 1024
+    st = Streams(8, [32], [0], 1, 1, "bf16", 32).fill()
+    q = torch.linspace(-3, 3, heads).to(torch.bfloat16).view(1, heads, 1)
+    table, past = torch.from_numpy(st.table[:, :1].copy()).cuda(), torch.tensor([31], dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda") if ragged else None
+    got = ops.cache_attend(q.cuda().expand(n, -1, -1), st.cache, table, past, seq_offsets=offsets)
+    x = q.float().numpy().astype(np.float64)[0]
+    want, spread = ops_ref.attend(x, st.k[0][:, 0], st.v[0][:, 0], 1.0, np.ones((heads, 32), bool))
+    check_attention(got[:1], want[None], spread[None], "bf16")
+    for at in range(0, n, 1 << 18):
+        assert got[at:at + (1 << 18)].eq(got[:1]).all(), at
