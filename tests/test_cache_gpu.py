@@ -745,3 +745,26 @@ def test_rows_behind_31_bits(ragged):
     check_attention(got[:1], want[None], spread[None], "bf16")
     for at in range(0, n, 1 << 18):
         assert got[at:at + (1 << 18)].eq(got[:1]).all(), at
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window", [1000, 1500, 1999])
+@pytest.mark.parametrize("past,news,hq,hk,page", [
+    ([3100, 4999, 700], [1, 1, 1], 4, 2, 64), ([4200, 900, 3333], [5, 5, 5], 6, 2, 32), ([3000, 4000, 990], [200, 200, 200], 4, 2, 64), ([3333], [70], 5, 1, 128),
+    ([3300, 0, 4100, 1200, 5, 2999, 3001, 4500], [1, 1, 100, 1, 0, 1, 130, 3], 2, 1, 64)])
+def test_windows_whose_tokens_several_workgroups_share(past, news, hq, hk, page, window, dtype, kind, monkeypatch):
+    """Stretches begin where the first of a workgroup's rows begins to see; the join has to find the same places, of sequences of few rows
+    and of many, also in one call."""
+    torch, ops = torch_ops()
+    sizes, enqueue = [], ops._enqueue
+
+    def spy(call, args, gpu, workspace_of=None):
+        n = ops.ctypes.c_size_t(0)
+        assert workspace_of(args, ops.ctypes.byref(n)) == ev.OK
+        sizes.append(n.value)
+        return enqueue(call, args, gpu, workspace_of)
+    monkeypatch.setattr(ops, "_enqueue", spy)
+    st = whole(past, news, 11, hk, 64, kind, page)
+    check_attention(*attend_case(st, hq, dtype, equal=len(set(news)) == 1, window=window), dtype)
+    assert sizes[0] > 0, "nothing is joined"
