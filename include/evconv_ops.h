@@ -247,9 +247,10 @@ evconv_status evconv_cache_read(const evconv_read_args* args, void* hip_stream);
  * sees none gets zeros.  Query head h uses key head h / (heads_q / cache.heads).  Seen are, of the query's sequence, tokens 0 .. its own
  * position (causal: of the last `window` ones of them), or all past[s] (else); of those the ones in chosen pages, if `selected`
  * is given.  Products with bf16 queries are exact; fp32 queries and the weights of fp32 calls enter them as three bf16 parts
- * (24 bits); the weights of bf16 calls as two (16 bits) where a sequence has up to 16 tokens x query heads of a key head, otherwise rounded
- * to bf16, which is a rounding of the output's own size.  Weights go up to 2^8, and are divided by their sum last: values whose 2^8-fold sum is
- * beyond fp32 are too large.  A finite query value of 3.39e38 and more counts as infinite. */
+ * (24 bits).  The weights of bf16 calls enter as two (16 bits) with chosen pages, and for sequences of up to 16 rows (tokens x query heads
+ * of a key head) unless the call has seq_offsets and 64 rows to a sequence or more on average; otherwise rounded to bf16, which is a
+ * rounding of the output's own size (sequences of few rows then too: what a row sees is the same, its last bits may hang on the call).
+ * Weights go up to 2^8, and are divided by their sum last: values whose 2^8-fold sum is beyond fp32 are too large.  A finite query value of 3.39e38 and more counts as infinite. */
 typedef struct {
   int32_t abi_version;
   int32_t dtype;    /* of q and o: EVCONV_F32 or EVCONV_BF16 */

@@ -38,6 +38,8 @@ struct Whole {
 template <bool FP4, bool BF16, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_pieces(AttendParams p, int64_t block0) {
   using Tile = PieceTile<DP>;
+  // (weights of bf16 calls are rounded to bf16, by up to 2^-8 of themselves as the output is: 8 x 4096 tokens are 0.0022 of the norm off instead
+  // of 0.0016, and take 594 us instead of 756 with two parts, 512 tokens on 32768 in 4 bits 193 instead of 233)
   constexpr int PARTS = BF16 ? 1 : 3, CT = BF16 ? 2 : 1, ROWS = BF16 ? kPieceRowsBf16 : kPieceRowsF32, STEPS = DP / 32, VT = DP / 16, TT = Tile::kTokens, HALVES = Tile::kHalves;
   extern __shared__ __align__(16) char s_mem[];
   char* const s_k = s_mem;

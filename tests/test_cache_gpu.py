@@ -768,3 +768,24 @@ def test_windows_whose_tokens_several_workgroups_share(past, news, hq, hk, page,
     st = whole(past, news, 11, hk, 64, kind, page)
     check_attention(*attend_case(st, hq, dtype, equal=len(set(news)) == 1, window=window), dtype)
     assert sizes[0] > 0, "nothing is joined"
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+@pytest.mark.parametrize("how", ["step", "ragged", "chosen"])
+@pytest.mark.parametrize("hq,hk,d", [(4, 2, 64), (8, 1, 128), (3, 3, 37)])
+def test_few_rows_of_bf16_hold_their_weights_in_16_bits(hq, hk, d, how, kind):
+    """Single tokens, short sequences beside each other, chosen pages: half a step of the result, and 2^-15 of the weights' sum over |v|.
+    (Two bf16 parts leave 2^-16 of a weight; scores of a few are off by 2^-19, the exponential of fp32 by 2^-20.)"""
+    past, news = ([5, 700, 2500], [1, 1, 1]) if how == "step" else ([5, 700, 2500, 40], [1, 2, 0, 1])
+    st = whole(past, news, 13, hk, d, kind, 64)
+    selected = None
+    if how == "chosen":
+        selected = np.full((sum(news), hk, 5), -1, np.int32)
+        for i in range(len(selected)):
+            for h in range(hk):
+                selected[i, h] = st.rng.permutation(st.width)[:5]
+        selected[:, :, 0] = [0]
+        selected[:, :, 1:][selected[:, :, 1:] == 0] = -1
+    got, want, spread = attend_case(st, hq, "bf16", equal=how == "step", selected=selected)
+    diff, slack = np.abs(got.float().cpu().numpy() - want), 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * spread
+    assert (diff <= slack).all(), (diff / slack).max()
