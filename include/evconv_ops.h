@@ -275,8 +275,9 @@ evconv_status evconv_cache_attend(const evconv_attend_args* args, void* workspac
 /* Which `count` pages of its sequence each query (and key head) looks at, ascending, then -1.  With c the page of the query's
  * own position: the first `first` pages and the last `last` ones up to c; then, of the others below c, those of the highest
  *   score = max over the query heads of the key head of  sum over channels of max(q lo, q hi)
- * (no query . key product of the page is larger), taken in 64 bits and rounded to fp32; ties: the lower page.  A score that is
- * NaN is the highest.  A page that is not there is not chosen. */
+ * (no query . key product of the page is larger with its keys as bf16, which the bounds are of; with those that a cache in 4 bits holds
+ * one may be, by their rounding: of a key's value about a sixth of its row's largest at most), taken in 64 bits and rounded to fp32;
+ * ties: the lower page.  A score that is NaN is the highest.  A page that is not there is not chosen. */
 typedef struct {
   int32_t abi_version;
   int32_t dtype;   /* of q */

@@ -789,3 +789,29 @@ def test_few_rows_of_bf16_hold_their_weights_in_16_bits(hq, hk, d, how, kind):
     got, want, spread = attend_case(st, hq, "bf16", equal=how == "step", selected=selected)
     diff, slack = np.abs(got.float().cpu().numpy() - want), 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * spread
     assert (diff <= slack).all(), (diff / slack).max()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp4"])
+def test_what_the_bounds_hold_for(kind):
+    """Keys in bf16 lie inside; keys in 4 bits may lie outside, by their own rounding: half the widest gap of two codes, a sixth of the row's
+    largest value, and half a step of bf16."""
+    torch, ops = torch_ops()
+    d, page = 48, 64
+    k = torch.randn(3 * page + 1, 2, d, generator=torch.Generator().manual_seed(5))
+    k[-1, 0, :] = 0.3
+    k[-1, 0, 0] = 6  # (0.3 becomes 0.5, alone on the last page)
+    cache = ops.cache_new(4, 2, d, page=page, kind=kind)
+    table, past = torch.arange(4, dtype=torch.int32, device="cuda")[None], torch.zeros(1, dtype=torch.int32, device="cuda")
+    ops.cache_append(cache, k.cuda(), k.cuda(), table, past)
+    for rows, place in ((k[:3 * page], np.arange(3 * page) // page), (k[-1:], np.array([3]))):
+        at = torch.tensor([int(place[0]) * page], dtype=torch.int32, device="cuda")
+        held, _ = ops.cache_read(cache, table, at, len(rows))
+        held, bounds = held.cpu().numpy(), cache.bounds.float().cpu().numpy()[place]
+        lo, hi = bounds[:, :, 0, :d], bounds[:, :, 1, :d]
+        over = np.maximum(held - hi, lo - held)
+        if kind == "bf16":
+            assert (over <= 0).all()
+        else:
+            m = rows.abs().amax(-1, keepdim=True).numpy()
+            assert (over <= m * (1 / 6 + 2.0 ** -8)).all()
+            assert len(rows) > 1 or (held[0, 0, 1:] == 0.5).all() and (over[0, 0, 1:] > 0.19).all()
