@@ -522,6 +522,8 @@ def cache_append(cache, k, v, table, past, q=None, *, seq_offsets=None, q_norm=N
     the places in the sequence.  q_out: where the queries go, may be q."""
     if k.dim() != 3 or (q is not None and q.dim() != 3):
         _refuse(ERR_SHAPE, f"k {tuple(k.shape)}: expected [tokens, heads, d], q alike")
+    if q is None and q_out is not None:
+        _refuse(ERR_INVALID_ARG, "cache append: q_out without q")
     gpu, dtype, shape = k.get_device(), k.dtype, k.shape
     if gpu < 0:
         _explain(k, "k", gpu, dtype, shape)

@@ -191,3 +191,13 @@ def test_attend_reference_against_a_loop():
     for i in range(4):
         w = np.array([np.exp(0.5 * q[i] @ k[t]) for t in range(i)])
         assert np.allclose(got[i], (w[:, None] * v[:i]).sum(0) / w.sum() if i else 0)
+
+
+def test_a_place_for_queries_needs_queries():
+    """q_out without q would come back unwritten."""
+    torch = pytest.importorskip("torch")
+    x, cache = torch.zeros(1, 2, 40), ops.Cache(*[torch.zeros(1)] * 5, 40)
+    table, past = torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ev.EvConvError) as e:
+        ops.cache_append(cache, x, x, table, past, q_out=torch.zeros_like(x))
+    assert e.value.status == ev.ERR_INVALID_ARG and "q_out" in str(e.value)
