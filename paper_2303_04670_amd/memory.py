@@ -51,14 +51,14 @@ class Memory:
     and layer: fp32 [n_streams, heads_v, d_k, d_v], zero at first.
 
     recall: numbers of the layers that look back, heads_v query heads on heads_k key heads of d_v channels, into a cache of kind
-    recall_kind.  They see the last recall_windows windows of a stream, for up to `lifetime` windows since it began; or, with recall_pages,
+    recall_kind.  They see the last recall_windows windows of a stream, however long it is; or, with recall_pages,
     that many pages of 64 windows among the first recall_windows ones, which are all that is kept.  A call brings `longest` windows at
-    most (what the pages that go round have room for beside the windows that are seen)."""
+    most (what the pages that go round have room for beside the windows that are seen).  lifetime: of no effect."""
 
     PAGE = 64
 
     def __init__(self, dim, n_streams, n_out, layers=2, heads_k=2, heads_v=4, d_k=64, d_v=64, dtype=torch.bfloat16, device="cuda:0",
-                 seed=0, recall=(), recall_kind="fp4", recall_windows=1024, recall_pages=None, longest=1024, lifetime=1 << 18):
+                 seed=0, recall=(), recall_kind="fp4", recall_windows=1024, recall_pages=None, longest=1024, lifetime=None):
         self.dim, self.n_streams, self.dtype, self.device = dim, n_streams, dtype, torch.device(device)
         self.heads_k, self.heads_v, self.d_k, self.d_v = heads_k, heads_v, d_k, d_v
         rng = np.random.default_rng(seed)
@@ -71,7 +71,7 @@ class Memory:
         if self.recall - set(range(layers)):
             raise EvConvError(ERR_INVALID_ARG, f"layers {sorted(self.recall)} of {layers} look back")
         if self.recall:
-            self._make_pages(lifetime)
+            self._make_pages()
         for i in range(layers):
             if i in self.recall:
                 self._recall_layer(rng, recall_kind)
@@ -88,15 +88,19 @@ class Memory:
         self.norm, self.bias = self._of(self.weights[-1]["norm"]), self._of(self.weights[-1]["bias"])
         self.head = self._rows(self.weights[-1]["head"])
 
-    def _make_pages(self, lifetime):
-        """Every stream's own pages: the last windows' in turns, or those of the first ones."""
+    def _make_pages(self):
+        """Every stream's own pages: the last windows' in turns, or those of the first ones.  Pages that go round stand in the table twice: once
+        a stream's place is so far on that its windows fill a round and what is seen, it goes back by a round, to the same pages, with as
+        much behind it as is seen.  `windows` goes on, for the angles."""
         page, n = self.PAGE, self.n_streams
         own = -(-self.recall_windows // page) if self.recall_pages else -(-(self.recall_windows + self.longest) // page) + 1
-        width = own if self.recall_pages else max(-(-lifetime // page), own)
+        width = own if self.recall_pages else 2 * own
+        self.round = own * page
         entry = torch.arange(width, dtype=torch.int32, device=self.device) % own
         self.n_pages = n * own
         self.table = (torch.arange(n, dtype=torch.int32, device=self.device)[:, None] * own + entry).contiguous()
-        self.past = torch.zeros(n, dtype=torch.int32, device=self.device)
+        self.past = torch.zeros(n, dtype=torch.int32, device=self.device)  # tokens in the table's places
+        self.windows = torch.zeros(n, dtype=torch.int64, device=self.device)  # since each stream began
         self.freqs = self._of(10000.0 ** (-np.arange(0, self.d_v // 2 * 2, 2) / max(self.d_v, 1)))
 
     def _recall_layer(self, rng, kind):
@@ -121,7 +125,7 @@ class Memory:
 
     def forget(self, slots=None):
         """Streams (all of them) begin anew.  slots: as in a window's call, or whatever else indexes the streams."""
-        states = [s for s in self.states if s is not None] + ([self.past] if self.recall else [])
+        states = [s for s in self.states if s is not None] + ([self.past, self.windows] if self.recall else [])
         if slots is None or isinstance(slots, slice) or torch.is_tensor(slots) and slots.dtype == torch.bool:
             for state in states:
                 state[slots if slots is not None else slice(None)] = 0
@@ -173,22 +177,28 @@ class Memory:
         return x, rows
 
     def _whose(self, x, slots, seq_offsets):
-        """(table, past, offsets) of the call's sequences; one that is no stream's has no pages."""
+        """(table, past, offsets, numbers of the windows) of the call's sequences; one that is no stream's has no pages."""
         n = slots.numel() if slots is not None else seq_offsets.numel() - 1 if seq_offsets is not None else self.n_streams
         if n > self.n_streams or (seq_offsets is None and x.dim() == 2 and x.shape[0] != n) or (seq_offsets is not None and seq_offsets.numel() != n + 1):
             raise EvConvError(ERR_SHAPE, f"{tuple(x.shape)} windows of {n} sequences, {self.n_streams} streams")
-        if slots is None:
-            return self.table[:n], self.past[:n], seq_offsets
-        inside = (slots >= 0) & (slots < self.n_streams)
-        at = slots.clamp(0, self.n_streams - 1).long()
-        return torch.where(inside[:, None], self.table[at], -1), torch.where(inside, self.past[at], 0), seq_offsets
+        table, past, number = self.table[:n], self.past[:n], self.windows[:n]
+        if slots is not None:
+            inside = (slots >= 0) & (slots < self.n_streams)
+            at = slots.clamp(0, self.n_streams - 1).long()
+            table, past, number = torch.where(inside[:, None], self.table[at], -1), torch.where(inside, self.past[at], 0), torch.where(inside, self.windows[at], 0)
+        if seq_offsets is not None:
+            window = torch.arange(x.shape[0], dtype=torch.int32, device=self.device)
+            whose = torch.searchsorted(seq_offsets[1:], window, right=True).clamp_(max=n - 1)
+            number = number[whose] + (window - seq_offsets[whose])
+        return table, past, seq_offsets, number
 
-    def _look_back(self, layer, p, table, past, seq_offsets):
+    def _look_back(self, layer, p, table, past, seq_offsets, number):
         """(o, z) of a layer over a cache."""
         wide, narrow = self.heads_v * self.d_v, self.heads_k * self.d_v
         q, k, v, z = (p[:, a:b] for a, b in ((0, wide), (wide, wide + narrow), (wide + narrow, wide + 2 * narrow), (wide + 2 * narrow, 2 * (wide + narrow))))
         q, k, v = (t.unflatten(1, (-1, self.d_v)) for t in (q, k, v))
-        q = ops.cache_append(layer.cache, k, v, table, past, q, seq_offsets=seq_offsets, q_norm=layer.q_norm, k_norm=layer.k_norm, freqs=self.freqs)
+        q = ops.cache_append(layer.cache, k, v, table, past, q, seq_offsets=seq_offsets, q_norm=layer.q_norm, k_norm=layer.k_norm, freqs=self.freqs,
+                             positions=number)
         if self.recall_pages:
             pages = ops.cache_select(q, layer.cache, table, past, self.recall_pages, seq_offsets=seq_offsets)
             return ops.cache_attend(q, layer.cache, table, past, seq_offsets=seq_offsets, selected=pages), z
@@ -196,13 +206,21 @@ class Memory:
 
     def _move_on(self, whose, slots):
         """The call's windows are past."""
-        _, past, seq_offsets = whose
+        seq_offsets = whose[2]
         new = 1 if seq_offsets is None else seq_offsets[1:] - seq_offsets[:-1]
-        if slots is None:
-            past += new
-            return
-        inside = (slots >= 0) & (slots < self.n_streams)
-        self.past.index_add_(0, slots.clamp(0, self.n_streams - 1).long(), torch.where(inside, new, 0).to(torch.int32))
+        inside = at = None
+        if slots is not None:
+            inside, at = (slots >= 0) & (slots < self.n_streams), slots.clamp(0, self.n_streams - 1).long()
+            new = torch.where(inside, new, 0)
+        for count in (self.past, self.windows):
+            if slots is not None:
+                count.index_add_(0, at, new.to(count.dtype))
+            else:
+                count[:len(whose[0])] += new
+        if self.recall_pages:
+            self.past.clamp_(max=self.round)  # (all that is kept)
+        else:
+            self.past.add_(self.past >= self.round + self.recall_windows, alpha=-self.round)
 
 
 def main():

@@ -153,3 +153,71 @@ def test_a_window_in_a_graph():
         assert torch.equal(y, other(x))
     torch.cuda.synchronize()
     assert memory.past.tolist() == other.past.tolist() == [71] * 4
+
+
+@pytest.mark.parametrize("kind", ["fp4", "bf16"])
+@pytest.mark.parametrize("how", ["pieces", "slots"])
+def test_a_stream_that_goes_round_many_times(how, kind):
+    """Pages go round every 256 windows here, again and again; what is seen stays the last 64 windows."""
+    torch, memory = make(recall_windows=64, longest=100, n_streams=3, recall_kind=kind, lifetime=320)
+    n, x = 1400, torch.randn(2 * 1400, 96, device="cuda")
+    want = reference(memory, x.cpu().numpy(), [(0, n), (n, n)], kind)
+    slots = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    got, at = torch.empty(2, n, 11, device="cuda"), 0
+    for step in [50, 1, 37, 1] * 100:  # (no step brings the round's end to the same place)
+        step = min(step, n - at)
+        if not step:
+            break
+        rows = torch.cat([x[at:at + step], x[n + at:n + at + step]])
+        if how == "slots" and step == 1:
+            got[:, at] = memory(rows, slots=slots)
+        else:
+            got[:, at:at + step] = memory(rows, slots=slots, seq_offsets=torch.tensor([0, step, 2 * step], dtype=torch.int32, device="cuda")).view(2, step, 11)
+        at += step
+    near(got.view(2 * n, 11), want)
+    assert memory.windows.tolist() == [n, 0, n] and memory.past[1] == 0 and 64 <= int(memory.past.max()) < memory.round + 64
+    assert 64 * memory.table.shape[1] == 2 * memory.round
+
+
+def test_angles_far_on(monkeypatch):
+    """A stream whose windows are numbered from 2^33 on."""
+    torch, memory = make(recall_windows=64, longest=100, n_streams=1)
+    memory.windows += 1 << 33
+    x, rows = torch.randn(300, 96, device="cuda"), ops_ref.head_rows
+    monkeypatch.setattr(ops_ref, "head_rows", lambda y, weight, eps, freqs, pairs, at: rows(y, weight, eps, freqs, pairs, at + (1 << 33)))
+    want = reference(memory, x.cpu().numpy(), [(0, 300)])
+    offsets = torch.tensor([0, 100], dtype=torch.int32, device="cuda")
+    near(torch.cat([memory(x[at:at + 100], seq_offsets=offsets) for at in (0, 100, 200)]), want)
+
+
+def test_pages_that_are_kept_are_the_first_ones():
+    """Windows behind them look at what is kept, however far behind."""
+    torch, memory = make(recall_windows=128, recall_pages=2, n_streams=2)
+    x = torch.randn(2, 96, device="cuda")
+    for i in range(150):
+        memory(torch.randn(2, 96, device="cuda"))
+    assert memory.past.tolist() == [128, 128] and memory.windows.tolist() == [150, 150]
+    kept = [t.clone() for layer in memory.layers for t in layer.cache[:5]]
+    a = memory(x)
+    memory.past[:], memory.windows[:] = 100000, 150
+    assert torch.equal(memory(x), a) and torch.isfinite(a).all()
+    for t, u in zip(kept, (t for layer in memory.layers for t in layer.cache[:5])):
+        assert torch.equal(t.view(torch.uint8), u.view(torch.uint8))
+
+
+def test_rounds_in_a_graph():
+    torch, memory = make(recall=(0,), recall_windows=64, longest=64, n_streams=2)
+    _, other = make(recall=(0,), recall_windows=64, longest=64, n_streams=2)
+    x = torch.randn(2, 96, device="cuda")
+    memory(x)
+    other(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = memory(x)
+    for _ in range(600):
+        x.normal_()
+        graph.replay()
+        assert torch.equal(y, other(x))
+    torch.cuda.synchronize()
+    assert memory.past.tolist() == other.past.tolist() and memory.windows.tolist() == [601, 601] and int(memory.past[0]) < 601
