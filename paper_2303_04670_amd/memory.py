@@ -147,13 +147,15 @@ class Memory:
         if self.recall and x.dim() == 2 and x.shape[0] > self.longest and seq_offsets is not None:
             raise EvConvError(ERR_SHAPE, f"{x.shape[0]} windows in a call: at most {self.longest}")
         to = self.columns
-        whose = self._whose(x, slots, seq_offsets) if self.recall else None
+        if self.recall:
+            whose = self._whose(x, slots, seq_offsets)
+            seq_offsets = whose[2]
         n_seq = None if slots is not None or seq_offsets is not None else self.n_streams
         rows = ops.block_norm(x, pre_norm=True, pre_weight=self.layers[0].pre_norm, want="q").q
         for i, layer in enumerate(self.layers):
             p = ops.quant_matmul(rows, layer.w_in, out_dtype=self.dtype)
             if layer.cache is not None:
-                o, z = self._look_back(layer, p, *whose)
+                o, z = self._look_back(layer, p, *whose[:4])
                 x, rows = self._behind(i, x, o, z)
                 continue
             q, k, v, z, a, b = (p[:, to[j]:to[j + 1]] for j in range(6))
@@ -163,7 +165,7 @@ class Memory:
                                   a_scale=layer.a_scale, dt_bias=layer.dt_bias)
             x, rows = self._behind(i, x, o, z)
         if self.recall:
-            self._move_on(whose, slots)
+            self._move_on(whose[4], slots)
         return ops.quant_matmul(rows, self.head, bias=self.bias)
 
     def _behind(self, i, x, o, z):
@@ -177,7 +179,7 @@ class Memory:
         return x, rows
 
     def _whose(self, x, slots, seq_offsets):
-        """(table, past, offsets, numbers of the windows) of the call's sequences; one that is no stream's has no pages."""
+        """(table, past, offsets, numbers of the windows, new windows) of the call's sequences; one that is no stream's has no pages."""
         n = slots.numel() if slots is not None else seq_offsets.numel() - 1 if seq_offsets is not None else self.n_streams
         if n > self.n_streams or (seq_offsets is None and x.dim() == 2 and x.shape[0] != n) or (seq_offsets is not None and seq_offsets.numel() != n + 1):
             raise EvConvError(ERR_SHAPE, f"{tuple(x.shape)} windows of {n} sequences, {self.n_streams} streams")
@@ -186,11 +188,15 @@ class Memory:
             inside = (slots >= 0) & (slots < self.n_streams)
             at = slots.clamp(0, self.n_streams - 1).long()
             table, past, number = torch.where(inside[:, None], self.table[at], -1), torch.where(inside, self.past[at], 0), torch.where(inside, self.windows[at], 0)
+        new = 1
         if seq_offsets is not None:
+            # (what is out of range is cut off there, a pair that descends is an empty sequence: all layers have the same windows, and as many are past)
+            seq_offsets = seq_offsets.clamp(0, x.shape[0]).cummax(0).values
+            new = seq_offsets[1:] - seq_offsets[:-1]
             window = torch.arange(x.shape[0], dtype=torch.int32, device=self.device)
             whose = torch.searchsorted(seq_offsets[1:], window, right=True).clamp_(max=n - 1)
             number = number[whose] + (window - seq_offsets[whose])
-        return table, past, seq_offsets, number
+        return table, past, seq_offsets, number, new
 
     def _look_back(self, layer, p, table, past, seq_offsets, number):
         """(o, z) of a layer over a cache."""
@@ -204,11 +210,8 @@ class Memory:
             return ops.cache_attend(q, layer.cache, table, past, seq_offsets=seq_offsets, selected=pages), z
         return ops.cache_attend(q, layer.cache, table, past, seq_offsets=seq_offsets, window=self.recall_windows), z
 
-    def _move_on(self, whose, slots):
+    def _move_on(self, new, slots):
         """The call's windows are past."""
-        seq_offsets = whose[2]
-        new = 1 if seq_offsets is None else seq_offsets[1:] - seq_offsets[:-1]
-        inside = at = None
         if slots is not None:
             inside, at = (slots >= 0) & (slots < self.n_streams), slots.clamp(0, self.n_streams - 1).long()
             new = torch.where(inside, new, 0)
@@ -216,7 +219,7 @@ class Memory:
             if slots is not None:
                 count.index_add_(0, at, new.to(count.dtype))
             else:
-                count[:len(whose[0])] += new
+                count[:len(new) if torch.is_tensor(new) else None] += new
         if self.recall_pages:
             self.past.clamp_(max=self.round)  # (all that is kept)
         else:

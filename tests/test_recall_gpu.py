@@ -221,3 +221,20 @@ def test_rounds_in_a_graph():
         assert torch.equal(y, other(x))
     torch.cuda.synchronize()
     assert memory.past.tolist() == other.past.tolist() and memory.windows.tolist() == [601, 601] and int(memory.past[0]) < 601
+
+
+@pytest.mark.parametrize("offsets,good", [([0, 2, 9], [0, 2, 3]), ([-4, 2, 3], [0, 2, 3]), ([0, 3, 1], [0, 3, 3]), ([7, 9, 8], [3, 3, 3])])
+def test_offsets_out_of_range_are_cut_off(offsets, good):
+    """What is behind the windows of a call is nobody's: streams move on by the windows that they had."""
+    torch, memory = make()
+    _, other = make()
+    x, slots = torch.randn(3, 96, device="cuda"), torch.tensor([3, 1], dtype=torch.int32, device="cuda")
+    first = torch.randn(4, 96, device="cuda")
+    y = [m(x, slots=slots, seq_offsets=torch.tensor(o, dtype=torch.int32, device="cuda")) for m, o in ((memory, offsets), (other, good)) if m(first) is not None]
+    if good[0] == 0 and good[2] == 3:
+        assert torch.equal(*y)
+    assert memory.past.tolist() == other.past.tolist() == [1, 1 + good[2] - good[1], 1, 1 + good[1] - good[0]] and torch.equal(memory.windows, other.windows)
+    for _ in range(3):
+        x = torch.randn(4, 96, device="cuda")
+        a, b = memory(x), other(x)
+        assert torch.equal(a, b) and torch.isfinite(a).all()
