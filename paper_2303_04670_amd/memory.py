@@ -59,6 +59,9 @@ class Memory:
 
     def __init__(self, dim, n_streams, n_out, layers=2, heads_k=2, heads_v=4, d_k=64, d_v=64, dtype=torch.bfloat16, device="cuda:0",
                  seed=0, recall=(), recall_kind="fp4", recall_windows=1024, recall_pages=None, longest=1024, lifetime=None):
+        self.recall, self.recall_windows, self.recall_pages, self.longest = frozenset(recall), recall_windows, recall_pages, longest
+        if self.recall:  # (nothing of a window may be refused behind the layers that have rewritten their states and caches)
+            self._check_recall(layers, heads_k, heads_v)
         self.dim, self.n_streams, self.dtype, self.device = dim, n_streams, dtype, torch.device(device)
         self.heads_k, self.heads_v, self.d_k, self.d_v = heads_k, heads_v, d_k, d_v
         rng = np.random.default_rng(seed)
@@ -67,9 +70,6 @@ class Memory:
         padded = -(-self.columns[-1] // 8) * 8  # (rows of p whose slices can be read in vectors)
         self.weights = []  # of every layer in fp32 on the host, by name: what the quantised ones were made from
         self.layers, self.states = [], []
-        self.recall, self.recall_windows, self.recall_pages, self.longest = frozenset(recall), recall_windows, recall_pages, longest
-        if self.recall - set(range(layers)):
-            raise EvConvError(ERR_INVALID_ARG, f"layers {sorted(self.recall)} of {layers} look back")
         if self.recall:
             self._make_pages()
         for i in range(layers):
@@ -87,16 +87,34 @@ class Memory:
             ("norm", rng.uniform(0.5, 1.5, dim)), ("head", rng.standard_normal((n_out, dim)) / np.sqrt(dim)), ("bias", np.zeros(n_out)))})
         self.norm, self.bias = self._of(self.weights[-1]["norm"]), self._of(self.weights[-1]["bias"])
         self.head = self._rows(self.weights[-1]["head"])
+        if self.recall:  # what the calls themselves refuse: a call of no windows
+            self(torch.empty(0, dim, dtype=dtype, device=self.device), seq_offsets=torch.zeros(n_streams + 1, dtype=torch.int32, device=self.device))
+
+    def _check_recall(self, layers, heads_k, heads_v):
+        if self.recall - set(range(layers)):
+            raise EvConvError(ERR_INVALID_ARG, f"layers {sorted(self.recall)} of {layers} look back")
+        if self.recall_windows < 1 or self.longest < 1:
+            raise EvConvError(ERR_INVALID_ARG, f"recall_windows {self.recall_windows}, longest {self.longest}: at least 1")
+        if self.recall_pages is not None and not 2 <= self.recall_pages <= 65536:  # (the first and the newest are always among them)
+            raise EvConvError(ERR_INVALID_ARG, f"recall_pages {self.recall_pages}: 2 to 65536, None for the last windows")
+        if heads_k < 1 or heads_v < 1 or heads_v % heads_k:
+            raise EvConvError(ERR_SHAPE, f"{heads_v} heads on {heads_k} key heads")
+        if self._entries() * self.PAGE >= 1 << 30:
+            raise EvConvError(ERR_SHAPE, f"recall_windows {self.recall_windows}, longest {self.longest}: a stream's pages have room for less than 2^30")
+
+    def _own_pages(self):
+        return -(-self.recall_windows // self.PAGE) if self.recall_pages is not None else -(-(self.recall_windows + self.longest) // self.PAGE) + 1
+
+    def _entries(self):
+        return self._own_pages() * (1 if self.recall_pages is not None else 2)
 
     def _make_pages(self):
         """Every stream's own pages: the last windows' in turns, or those of the first ones.  Pages that go round stand in the table twice: once
         a stream's place is so far on that its windows fill a round and what is seen, it goes back by a round, to the same pages, with as
         much behind it as is seen.  `windows` goes on, for the angles."""
-        page, n = self.PAGE, self.n_streams
-        own = -(-self.recall_windows // page) if self.recall_pages else -(-(self.recall_windows + self.longest) // page) + 1
-        width = own if self.recall_pages else 2 * own
-        self.round = own * page
-        entry = torch.arange(width, dtype=torch.int32, device=self.device) % own
+        n, own = self.n_streams, self._own_pages()
+        self.round = own * self.PAGE
+        entry = torch.arange(self._entries(), dtype=torch.int32, device=self.device) % own
         self.n_pages = n * own
         self.table = (torch.arange(n, dtype=torch.int32, device=self.device)[:, None] * own + entry).contiguous()
         self.past = torch.zeros(n, dtype=torch.int32, device=self.device)  # tokens in the table's places
@@ -114,7 +132,7 @@ class Memory:
         self.weights.append({n: a.astype(np.float32) for n, a in w.items()})
         self.layers.append(Layer(**{n: self._rows(a) if n.startswith("w_") else self._of(a) for n, a in self.weights[-1].items()},
                                  a_scale=None, dt_bias=None, cache=ops.cache_new(self.n_pages, hk, d, page=self.PAGE, kind=kind,
-                                                                                 bounds=bool(self.recall_pages), device=self.device)))
+                                                                                 bounds=self.recall_pages is not None, device=self.device)))
         self.states.append(None)
 
     def _of(self, a):
@@ -205,7 +223,7 @@ class Memory:
         q, k, v = (t.unflatten(1, (-1, self.d_v)) for t in (q, k, v))
         q = ops.cache_append(layer.cache, k, v, table, past, q, seq_offsets=seq_offsets, q_norm=layer.q_norm, k_norm=layer.k_norm, freqs=self.freqs,
                              positions=number)
-        if self.recall_pages:
+        if self.recall_pages is not None:
             pages = ops.cache_select(q, layer.cache, table, past, self.recall_pages, seq_offsets=seq_offsets)
             return ops.cache_attend(q, layer.cache, table, past, seq_offsets=seq_offsets, selected=pages), z
         return ops.cache_attend(q, layer.cache, table, past, seq_offsets=seq_offsets, window=self.recall_windows), z
@@ -220,7 +238,7 @@ class Memory:
                 count.index_add_(0, at, new.to(count.dtype))
             else:
                 count[:len(new) if torch.is_tensor(new) else None] += new
-        if self.recall_pages:
+        if self.recall_pages is not None:
             self.past.clamp_(max=self.round)  # (all that is kept)
         else:
             self.past.add_(self.past >= self.round + self.recall_windows, alpha=-self.round)

@@ -238,3 +238,12 @@ def test_offsets_out_of_range_are_cut_off(offsets, good):
         x = torch.randn(4, 96, device="cuda")
         a, b = memory(x), other(x)
         assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+@pytest.mark.parametrize("bad", [dict(d_v=4), dict(d_v=300), dict(recall=(1,), d_k=300), dict(dtype="float16"), dict(recall_kind="int4"), dict(dim=20000)])
+def test_sizes_that_a_call_would_refuse_are_refused_when_the_memory_is_made(bad):
+    import torch
+    from paper_2303_04670_amd import evconv as ev
+    with pytest.raises(ev.EvConvError):
+        make(**{k: getattr(torch, v) if k == "dtype" else v for k, v in bad.items()})
+    torch.cuda.synchronize()
