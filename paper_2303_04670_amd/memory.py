@@ -199,8 +199,10 @@ class Memory:
     def _whose(self, x, slots, seq_offsets):
         """(table, past, offsets, numbers of the windows, new windows) of the call's sequences; one that is no stream's has no pages."""
         n = slots.numel() if slots is not None else seq_offsets.numel() - 1 if seq_offsets is not None else self.n_streams
-        if n > self.n_streams or (seq_offsets is None and x.dim() == 2 and x.shape[0] != n) or (seq_offsets is not None and seq_offsets.numel() != n + 1):
+        if n > self.n_streams or x.dim() != 2 or (seq_offsets is None and x.shape[0] != n) or (seq_offsets is not None and seq_offsets.numel() != n + 1):
             raise EvConvError(ERR_SHAPE, f"{tuple(x.shape)} windows of {n} sequences, {self.n_streams} streams")
+        for t, name, size in ((slots, "slots", n), (seq_offsets, "seq_offsets", n + 1)):
+            ops._packed(t, name, x.get_device(), torch.int32, (size,))
         table, past, number = self.table[:n], self.past[:n], self.windows[:n]
         if slots is not None:
             inside = (slots >= 0) & (slots < self.n_streams)

@@ -247,3 +247,21 @@ def test_sizes_that_a_call_would_refuse_are_refused_when_the_memory_is_made(bad)
     with pytest.raises(ev.EvConvError):
         make(**{k: getattr(torch, v) if k == "dtype" else v for k, v in bad.items()})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("recall", [(0,), (1,), (0, 1)])
+def test_slots_and_offsets_are_refused_before_anything_is_rewritten(recall):
+    torch, memory = make(recall=recall)
+    from paper_2303_04670_amd import evconv as ev
+    x = torch.randn(4, 96, device="cuda")
+    memory(x)
+    everything = lambda: [t for layer in memory.layers if layer.cache for t in layer.cache[:5] if t is not None] + [s for s in memory.states if s is not None] + [memory.past, memory.windows]
+    before = [t.clone() for t in everything()]
+    slots, offsets = torch.arange(4, dtype=torch.int32, device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda")
+    for call in (lambda: memory(x, slots=slots.long()), lambda: memory(x, slots=slots.cpu()), lambda: memory(x, slots=slots[:, None]), lambda: memory(x, slots=slots.float()),
+                 lambda: memory(x, seq_offsets=offsets.long()), lambda: memory(x, seq_offsets=offsets.cpu()), lambda: memory(x, slots=slots, seq_offsets=offsets[:4]),
+                 lambda: memory(x, slots=torch.stack([slots, slots], 1)[:, 0]), lambda: memory(x[0], seq_offsets=offsets), lambda: memory(x[0, 0], seq_offsets=offsets)):
+        with pytest.raises(ev.EvConvError):
+            call()
+        for a, b in zip(before, everything()):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
