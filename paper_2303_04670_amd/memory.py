@@ -46,14 +46,25 @@ class Layer(NamedTuple):
     k_norm: Optional[torch.Tensor] = None
 
 
+class Windows(NamedTuple):
+    """Whose the windows of a call are, for the layers that look back."""
+    table: torch.Tensor  # of every sequence; one that is no stream's has no pages
+    past: torch.Tensor
+    seq_offsets: Optional[torch.Tensor]
+    slots: Optional[torch.Tensor]
+    number: torch.Tensor  # of every window, since its stream began
+    new: object  # windows of every sequence, or 1
+    left_out: Optional[torch.Tensor]  # windows of streams that bring too many
+
+
 class Memory:
     """`layers` layers over features of `dim` values, then a linear head of `n_out` values.  One state per stream
     and layer: fp32 [n_streams, heads_v, d_k, d_v], zero at first.
 
     recall: numbers of the layers that look back, heads_v query heads on heads_k key heads of d_v channels, into a cache of kind
     recall_kind.  They see the last recall_windows windows of a stream, however long it is; or, with recall_pages,
-    that many pages of 64 windows among the first recall_windows ones, which are all that is kept.  A call brings `longest` windows at
-    most (what the pages that go round have room for beside the windows that are seen).  lifetime: of no effect."""
+    that many pages of 64 windows among the first recall_windows ones, which are all that is kept.  A stream brings `longest` windows at
+    most in a call (what the pages that go round have room for beside the windows that are seen).  lifetime: of no effect."""
 
     PAGE = 64
 
@@ -159,21 +170,20 @@ class Memory:
     def __call__(self, x, slots=None, seq_offsets=None):
         """Features [windows, dim] -> [windows, n_out].  By default one window of every stream, in their order; with
         slots (int32 [n], a stream at most once; negative: nothing is remembered) one window of each of those; with
-        seq_offsets (int32 [n + 1]) windows seq_offsets[i] .. seq_offsets[i + 1] are the next ones of stream slots[i]."""
+        seq_offsets (int32 [n + 1]) windows seq_offsets[i] .. seq_offsets[i + 1] are the next ones of stream slots[i].  (With layers that look
+        back a stream that brings more than `longest` of them is left as it was and its windows answered by NaN; more than n times `longest` are refused.)"""
         if x.dtype != self.dtype:  # (found by the last call of a layer only, behind the one that rewrites its states)
             raise EvConvError(ERR_INVALID_ARG, f"features are {x.dtype}, the memory's {self.dtype}")
-        if self.recall and x.dim() == 2 and x.shape[0] > self.longest and seq_offsets is not None:
-            raise EvConvError(ERR_SHAPE, f"{x.shape[0]} windows in a call: at most {self.longest}")
         to = self.columns
         if self.recall:
             whose = self._whose(x, slots, seq_offsets)
-            seq_offsets = whose[2]
+            seq_offsets, slots = whose.seq_offsets, whose.slots
         n_seq = None if slots is not None or seq_offsets is not None else self.n_streams
         rows = ops.block_norm(x, pre_norm=True, pre_weight=self.layers[0].pre_norm, want="q").q
         for i, layer in enumerate(self.layers):
             p = ops.quant_matmul(rows, layer.w_in, out_dtype=self.dtype)
             if layer.cache is not None:
-                o, z = self._look_back(layer, p, *whose[:4])
+                o, z = self._look_back(layer, p, whose)
                 x, rows = self._behind(i, x, o, z)
                 continue
             q, k, v, z, a, b = (p[:, to[j]:to[j + 1]] for j in range(6))
@@ -182,9 +192,12 @@ class Memory:
                                   seq_offsets=seq_offsets, slots=slots, n_seq=n_seq, normalize=True,
                                   a_scale=layer.a_scale, dt_bias=layer.dt_bias)
             x, rows = self._behind(i, x, o, z)
+        y = ops.quant_matmul(rows, self.head, bias=self.bias)
         if self.recall:
-            self._move_on(whose[4], slots)
-        return ops.quant_matmul(rows, self.head, bias=self.bias)
+            self._move_on(whose.new, slots)
+            if whose.left_out is not None:
+                y.masked_fill_(whose.left_out[:, None], float("nan"))
+        return y
 
     def _behind(self, i, x, o, z):
         """What of a layer comes behind its heads: (x', 8-bit rows of the next layer's norm)."""
@@ -197,29 +210,36 @@ class Memory:
         return x, rows
 
     def _whose(self, x, slots, seq_offsets):
-        """(table, past, offsets, numbers of the windows, new windows) of the call's sequences; one that is no stream's has no pages."""
         n = slots.numel() if slots is not None else seq_offsets.numel() - 1 if seq_offsets is not None else self.n_streams
         if n > self.n_streams or x.dim() != 2 or (seq_offsets is None and x.shape[0] != n) or (seq_offsets is not None and seq_offsets.numel() != n + 1):
             raise EvConvError(ERR_SHAPE, f"{tuple(x.shape)} windows of {n} sequences, {self.n_streams} streams")
         for t, name, size in ((slots, "slots", n), (seq_offsets, "seq_offsets", n + 1)):
             ops._packed(t, name, x.get_device(), torch.int32, (size,))
-        table, past, number = self.table[:n], self.past[:n], self.windows[:n]
-        if slots is not None:
-            inside = (slots >= 0) & (slots < self.n_streams)
-            at = slots.clamp(0, self.n_streams - 1).long()
-            table, past, number = torch.where(inside[:, None], self.table[at], -1), torch.where(inside, self.past[at], 0), torch.where(inside, self.windows[at], 0)
-        new = 1
+        new, left_out = 1, None
         if seq_offsets is not None:
+            if x.shape[0] > n * self.longest:
+                raise EvConvError(ERR_SHAPE, f"{x.shape[0]} windows of {n} sequences in a call: at most {self.longest} of each")
             # (what is out of range is cut off there, a pair that descends is an empty sequence: all layers have the same windows, and as many are past)
             seq_offsets = seq_offsets.clamp(0, x.shape[0]).cummax(0).values
             new = seq_offsets[1:] - seq_offsets[:-1]
             window = torch.arange(x.shape[0], dtype=torch.int32, device=self.device)
             whose = torch.searchsorted(seq_offsets[1:], window, right=True).clamp_(max=n - 1)
+            if x.shape[0] > self.longest:  # (one of them may bring too many, which only the GPU knows)
+                many = new > self.longest
+                slots = torch.where(many, -1, torch.arange(n, dtype=torch.int32, device=self.device) if slots is None else slots)
+                left_out = many[whose]
+        table, past, number = self.table[:n], self.past[:n], self.windows[:n]
+        if slots is not None:
+            inside = (slots >= 0) & (slots < self.n_streams)
+            at = slots.clamp(0, self.n_streams - 1).long()
+            table, past, number = torch.where(inside[:, None], self.table[at], -1), torch.where(inside, self.past[at], 0), torch.where(inside, self.windows[at], 0)
+        if seq_offsets is not None:
             number = number[whose] + (window - seq_offsets[whose])
-        return table, past, seq_offsets, number, new
+        return Windows(table, past, seq_offsets, slots, number, new, left_out)
 
-    def _look_back(self, layer, p, table, past, seq_offsets, number):
+    def _look_back(self, layer, p, whose):
         """(o, z) of a layer over a cache."""
+        table, past, seq_offsets, number = whose.table, whose.past, whose.seq_offsets, whose.number
         wide, narrow = self.heads_v * self.d_v, self.heads_k * self.d_v
         q, k, v, z = (p[:, a:b] for a, b in ((0, wide), (wide, wide + narrow), (wide + narrow, wide + 2 * narrow), (wide + 2 * narrow, 2 * (wide + narrow))))
         q, k, v = (t.unflatten(1, (-1, self.d_v)) for t in (q, k, v))

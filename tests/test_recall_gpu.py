@@ -265,3 +265,39 @@ def test_slots_and_offsets_are_refused_before_anything_is_rewritten(recall):
             call()
         for a, b in zip(before, everything()):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_every_stream_brings_up_to_the_longest():
+    """The limit is each stream's; one above it is left as it was, the others are not concerned."""
+    torch, memory = make()
+    lens = [250, 300, 290, 1]
+    first = np.concatenate([[0], np.cumsum(lens)])
+    x = torch.randn(sum(lens), 96, device="cuda")
+    near(memory(x, seq_offsets=torch.tensor(first, dtype=torch.int32, device="cuda")), reference(memory, x.cpu().numpy(), [(int(a), n) for a, n in zip(first, lens)]))
+    assert memory.past.tolist() == memory.windows.tolist() == lens
+
+
+@pytest.mark.parametrize("named", [False, True])
+def test_a_stream_that_brings_too_many_windows_is_left_as_it_was(named):
+    torch, memory = make(recall=(1,), layers=3)
+    _, other = make(recall=(1,), layers=3)
+    start, slots = torch.randn(4, 96, device="cuda"), torch.tensor([2, 0, 3], dtype=torch.int32, device="cuda")
+    order = [2, 0, 3] if named else [0, 1, 2]
+    for m in (memory, other):
+        m(start)
+    many, few = torch.randn(20 + 310 + 290, 96, device="cuda"), [20, 310, 290]
+    bounds = torch.tensor([0, 20, 330, 620], dtype=torch.int32, device="cuda")
+    y = memory(many, seq_offsets=bounds, slots=slots if named else None)
+    # the same without the stream of 310
+    rest = torch.cat([many[:20], many[330:]])
+    z = other(rest, seq_offsets=torch.tensor([0, 20, 20, 310], dtype=torch.int32, device="cuda"), slots=slots if named else None)
+    assert y[20:330].isnan().all() and torch.isfinite(z).all()
+    near(torch.cat([y[:20], y[330:]]), z.double().cpu().numpy())  # (sums may be cut otherwise)
+    want = [1, 1, 1, 1]
+    want[order[0]] += 20
+    want[order[2]] += 290
+    assert memory.past.tolist() == memory.windows.tolist() == want
+    x = torch.randn(4, 96, device="cuda")
+    a, b = memory(x), other(x)
+    near(a, b.double().cpu().numpy())
+    assert torch.equal(a[order[1]], b[order[1]])
