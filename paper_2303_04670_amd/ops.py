@@ -459,7 +459,7 @@ def _packer(args):
     def packed(*fields):
         try:
             return pack(*fields) + rest
-        except (struct.error, OverflowError) as reason:  # (the second of a float)
+        except struct.error as reason:
             _refuse(ERR_INVALID_ARG, f"{args.__name__}: a number that does not fit its field ({reason})")
     return packed
 

@@ -201,13 +201,3 @@ def test_a_place_for_queries_needs_queries():
     with pytest.raises(ev.EvConvError) as e:
         ops.cache_append(cache, x, x, table, past, q_out=torch.zeros_like(x))
     assert e.value.status == ev.ERR_INVALID_ARG and "q_out" in str(e.value)
-
-
-@pytest.mark.parametrize("number", [1e39, -1e300, 1 << 2000, "1"])
-def test_a_scale_that_fits_no_float_is_refused(number):
-    pack = ops._attend_args
-    fields = [0] * len(ops._flat(ops.AttendArgs)._fields_)
-    fields[[name for name, _ in ops._flat(ops.AttendArgs)._fields_].index("scale")] = number
-    with pytest.raises(ev.EvConvError) as e:
-        pack(*fields)
-    assert e.value.status == ev.ERR_INVALID_ARG
