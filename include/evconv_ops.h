@@ -169,7 +169,7 @@ evconv_status evconv_quant_matmul(const evconv_quant_args* args, void* hip_strea
  * token i of sequence s has position past[s] + i.  past is only read: who appends moves it on, once for all layers.
  * A table entry outside [0, n_pages), a negative position and one of width * page and more hold nothing: what is appended
  * there is dropped, what looks there sees nothing.  Pages may be read by several sequences; a page that a call appends to must be
- * one sequence's alone.
+ * one sequence's alone, and stand once among the entries that it appends to (elsewhere in the row as often as one likes: pages may go round).
  *
  * Channels are padded to dp = 32, 64, 96, 128, 192 or 256 with zeros.  All tensors are contiguous, at 16-byte addresses:
  *   EVCONV_CACHE_BF16   k [n_pages][heads][page][dp], v [n_pages][heads][dp][page]  (channels of v in rows: both are

@@ -5,8 +5,8 @@
 // are permuted within a row such that the operands' reads meet no bank twice; codes of 4 bits are turned into bf16 on the way, once for
 // all waves.  A wave has 16 or 32 rows of its own, with S' = K Q' and O' = V' P' as cache_attend_rows.h has them: weights stay in the lane that
 // made them.  Few workgroups over many tokens share a row's tokens and join what they found.
-//   8 sequences of 4096 tokens, 16 heads on 4 of 128 in bf16: 573 us, 960 TFLOP/s, where a large library product reaches 1215; matrix
-// instructions 40 %, vector ones (exponentials a third of them) as much.  Operands read ahead instead of where they are wanted 710 -> 661 us,
+//   8 sequences of 4096 tokens, 16 heads on 4 of 128 in bf16: 584 us, 940 TFLOP/s, where a large library product reaches 1215; matrix
+// instructions in 42 % of the cycles, vector ones (exponentials a third of them) in as many.  Operands read ahead instead of where they are wanted 710 -> 661 us,
 // addresses made once 661 -> 624, priority to the matrix instructions 624 -> 611.  512 tokens on 32768 in 4 bits: 175 us, 790 TFLOP/s.
 #pragma once
 

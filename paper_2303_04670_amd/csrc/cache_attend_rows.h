@@ -12,7 +12,7 @@
 // value its weights.
 //   Bound by the bytes of the cache: one token of 32 heads on 8 over 262144 in bf16 5.8 TB/s, 64 tokens over up to 16384 in 4 bits 4.2 TB/s
 // (there half of the time is vector and matrix instructions, of which 16 rows would take no more than the four there are).  Tiles in 4 bits of
-// 64 tokens instead of 128, which leave registers for a third wave of a SIMD: 158 -> 118 us; table entries a tile ahead: 158 -> 143.
+// 64 tokens instead of 128, which leave registers for a third wave of a SIMD: 158 -> 121 us; table entries a tile ahead: 158 -> 143.
 #pragma once
 
 #include "cache_device.h"
