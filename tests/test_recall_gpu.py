@@ -301,3 +301,29 @@ def test_a_stream_that_brings_too_many_windows_is_left_as_it_was(named):
     a, b = memory(x), other(x)
     near(a, b.double().cpu().numpy())
     assert torch.equal(a[order[1]], b[order[1]])
+
+
+@pytest.mark.parametrize("sizes", [dict(recall=(0,)), dict(recall=(0, 1), recall_windows=128, recall_pages=2), dict(recall=(1,), longest=30)])
+def test_ragged_windows_in_a_graph(sizes):
+    """Recorded once, replayed with other offsets, slots and windows; in the last case a stream brings too many of them now and then."""
+    torch, memory = make(**sizes)
+    _, other = make(**sizes)
+    x, offsets, slots = torch.randn(80, 96, device="cuda"), torch.tensor([0, 20, 50, 80], dtype=torch.int32, device="cuda"), torch.tensor([3, 0, 1], dtype=torch.int32, device="cuda")
+    memory(x, slots=slots, seq_offsets=offsets)
+    other(x, slots=slots, seq_offsets=offsets)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = memory(x, slots=slots, seq_offsets=offsets)
+    for bounds, named in (([0, 20, 50, 80], [3, 0, 1]), ([0, 0, 60, 80], [2, -1, 1]), ([0, 33, 33, 80], [0, 1, 2]), ([0, 30, 55, 80], [1, 2, 3]), ([0, 1, 2, 80], [3, 2, 0])):
+        x.normal_()
+        offsets.copy_(torch.tensor(bounds))
+        slots.copy_(torch.tensor(named))
+        graph.replay()
+        want = other(x, slots=slots, seq_offsets=offsets)
+        assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+        assert torch.isfinite(y).all() or "longest" in sizes
+        torch.cuda.synchronize()
+        assert torch.equal(memory.past, other.past) and torch.equal(memory.windows, other.windows)
+    memory.forget([3])
+    assert memory.past[3] == 0 and memory.windows[3] == 0 and torch.equal(memory.windows[:3], other.windows[:3])
